@@ -382,6 +382,159 @@ int gmm_set_stats_chunk_limit(int32_t max_chunks);
 int gmm_timing_enable(int on);
 int gmm_timing_read(double* ms, int32_t n_phases, int64_t* calls);
 
+/* ------------------------------------------------------------------------
+ * Paged key/value cache: attention over vectors that are kept in pages, and
+ * the selection of the pages that a query reads.  A softmax attention row is
+ * a point's responsibilities over equal isotropic components at the keys, so
+ * this is the E-step's online log-sum-exp with a value in place of the
+ * statistics; the selection is to pages what gmm_assign_topk is to components.
+ *
+ * The calls keep this header's conventions (device pointers, caller's memory
+ * and stream, checks on the host, no state between calls, every result
+ * bitwise reproducible); the two structs are read on the host during the call.
+ *
+ * Types: keys, values, queries and results are GMM_BF16 or GMM_F16 (gmm_rope:
+ * GMM_F32 too).  Head widths: d a multiple of 16, 16 <= d <= 256; pages of 32,
+ * 64, 128 or 256 keys (a 32-key matrix step lies in one page).  Query heads
+ * are a multiple of the cache's heads, at most GMM_KV_MAX_GROUP times as many; query head j reads cache head
+ * j / (hq / heads).
+ * ---------------------------------------------------------------------- */
+
+typedef enum { GMM_F32 = 0, GMM_BF16 = 1, GMM_F16 = 2 } gmm_dtype;
+
+#define GMM_KV_MAX_D 256
+#define GMM_KV_MAX_HEADS 1024
+#define GMM_KV_MAX_GROUP 64
+#define GMM_KV_MAX_KEEP 4096
+
+typedef struct {
+  void* k;          /* [pages, heads, page, d] */
+  void* v;          /* [pages, heads, d, page]: a page holds its values transposed */
+  int8_t* box;      /* [pages, heads, 2, d] upper, then lower bounds of the page's keys in */
+  float* box_scale; /* [pages, heads] ... units of box_scale; both may be null */
+  int32_t pages, heads, page, d;
+  int32_t dtype;    /* gmm_dtype of k and v */
+} gmm_kv_cache;
+
+/* New tokens of `batch` sequences: rows cu[b] .. cu[b+1]-1 (cu[0] = 0,
+ * cu[batch] = the call's `tokens`) belong to sequence b, which holds total[b]
+ * keys with them; they are its last ones, in order.  Key t of sequence b is
+ * slot t % page of page pages[b * pages_stride + t / page].  A sequence may
+ * have no new token.  total[b] <= max_pages * page and every page number of a
+ * used entry in [0, cache pages) are the caller's duty; keys beyond the table
+ * and pages out of range are left out (never read or written). */
+typedef struct {
+  const int32_t* cu;     /* [batch + 1] */
+  const int32_t* total;  /* [batch] */
+  const int32_t* pages;  /* [batch, max_pages], rows pages_stride apart */
+  int32_t batch, max_pages;
+  int64_t pages_stride;
+} gmm_kv_batch;
+
+/*
+ * Rotation table: table[p * 2 half + i] = scale cos(p freq[i]) and
+ * table[p * 2 half + half + i] = scale sin(p freq[i]) for the positions
+ * 0 <= p < positions, computed in fp64.  freq [half] fp64 (device) carries a
+ * model's base and its scaling for long contexts; scale its magnitude factor.
+ */
+int gmm_rope_table(const double* freq, int32_t half, double scale, int32_t positions,
+                   float* table, hipStream_t stream);
+
+/*
+ * Rotary positions: for every token t, head h and pair i < rot / 2 of x
+ *   a' = a c - b s,  b' = b c + a s,   c, s = table row pos[t]
+ * with (a, b) = (x_i, x_{i + rot/2}), or (x_{2i}, x_{2i+1}) if `interleaved`;
+ * inverse: a' = a c + b s, b' = b c - a s, the gradient of the rotation (and,
+ * for scale 1, its inverse).  Dimensions rot .. d - 1 are copied.  Computed in
+ * fp32 (products and sum rounded one by one), rounded once to dtype.
+ *   x, out [tokens, heads, d], rows of d contiguous, strides in elements
+ *   (out may be x itself with the same strides)
+ *   pos [tokens] int32; table [positions, rot] (gmm_rope_table), 2 <= rot <= d
+ * A token with pos < 0 is copied unrotated (padding); pos >= positions gives NaN.
+ * Any d >= 2, even rot.
+ */
+int gmm_rope(const void* x, int64_t x_token_stride, int64_t x_head_stride, void* out,
+             int64_t out_token_stride, int64_t out_head_stride, int64_t tokens, int32_t heads,
+             int32_t d, int32_t dtype, const int32_t* pos, const float* table, int32_t positions,
+             int32_t rot, int32_t interleaved, int32_t inverse, hipStream_t stream);
+
+/*
+ * Appends the new tokens' keys and values to the cache, the keys rotated on
+ * the way, and (if the cache has boxes) renews the boxes of the pages touched:
+ * hi_j = max, lo_j = min of the page's keys as stored, u = max |.| * (1/127
+ * in fp32), box = min(127, ceil(hi_j / u)) and max(-127, floor(lo_j / u)),
+ * box_scale = u.  A page with a NaN or infinite key gets box 0 and
+ * box_scale +inf, and is ranked before all others by gmm_kv_select.
+ * With q, also rotates the new tokens' queries into q_out.
+ *   k, v [tokens, heads, d], q / q_out [tokens, hq, d] (q null: hq ignored),
+ *   rows of d contiguous, strides in elements; q_out may be q
+ *   pos [tokens] rotation positions, null: a token's slot in its sequence
+ *   table null: no rotation (rot, positions, interleaved ignored; q must be null)
+ * Tokens whose slot is negative, beyond the table or in a page out of range
+ * are not stored (their queries are rotated all the same).
+ */
+int gmm_kv_append(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t tokens,
+                  const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
+                  int64_t v_token_stride, int64_t v_head_stride, const int32_t* pos,
+                  const float* table, int32_t positions, int32_t rot, int32_t interleaved,
+                  const void* q, int64_t q_token_stride, int64_t q_head_stride, void* q_out,
+                  int64_t qo_token_stride, int64_t qo_head_stride, int32_t hq,
+                  hipStream_t stream);
+
+/*
+ * Workspace of gmm_kv_select and gmm_kv_attend for `tokens` new tokens of
+ * `batch` sequences with hq query heads and page tables of max_pages entries:
+ * the page scores (tokens * heads * max_pages floats), or the partial results
+ * of the key ranges that long contexts are split into, whichever is larger.
+ * 0 when the shape is unsupported.
+ */
+size_t gmm_kv_workspace_bytes(const gmm_kv_cache* cache, int64_t tokens, int32_t hq,
+                              int32_t batch, int32_t max_pages);
+
+/*
+ * Selection of pages: for every new token and cache head, the m pages with the
+ * largest score among the pages that hold a key the token sees.  The score is
+ * an upper bound of the inner products in 8-bit numbers: with
+ * t_j = max |q_j| * (1/127 in fp32) and Q_j = round(q_j / t_j) for query head j
+ *   u_jp = (t_j * box_scale_p) * sum_e (max(Q_je, 0) hi_pe + min(Q_je, 0) lo_pe)
+ * and the largest u_jp of the cache head's query heads counts.  The sum is of
+ * whole numbers and exact, so the ranking does not depend on an order of
+ * summation; ties go to the lower page.  The first keep_first and the last
+ * keep_last visible pages are always taken (keep_last >= 1: the page that holds
+ * the token itself may hold later tokens of the same call, whose keys are in
+ * its box).
+ *   q [tokens, hq, d], rows contiguous, strides in elements
+ *   idx [tokens, heads, m] int32: indexes into the sequence's page table,
+ *   ascending, -1 behind the last where fewer than m pages are visible
+ * 1 <= m <= GMM_KV_MAX_KEEP, keep_first >= 0, keep_first + keep_last <= m.
+ */
+int gmm_kv_select(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t tokens,
+                  const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t hq,
+                  int32_t m, int32_t keep_first, int32_t keep_last, int32_t* idx, void* ws,
+                  size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Attention of the new tokens over the cache (their own keys appended before):
+ * out = sum_t softmax_t(scale q . k_t) v_t over the keys t of the token's
+ * sequence with t <= its slot and, if window > 0, t > slot - window; with sel,
+ * over the keys t <= slot of the listed pages only (window must be 0).
+ *   q [tokens, hq, d], rows contiguous, strides in elements
+ *   out [tokens, hq, d] contiguous; lse [tokens, hq] fp32 or null: the natural
+ *   log of sum_t exp(scale q . k_t)
+ *   sel [tokens, heads, m] or null (m = 0): gmm_kv_select's lists, or any other
+ *   lists of pages in range; entries < 0 are skipped, a page listed twice
+ *   counts twice
+ * A row without a visible key gives zeros and lse = -inf.  Inner products and
+ * sums are fp32, the softmax weights are rounded to dtype for the second
+ * product.  What slots past a sequence's last key hold does not matter; a NaN
+ * or infinite value at a key that one token sees can reach the rows of earlier
+ * tokens of the same call.
+ */
+int gmm_kv_attend(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t tokens,
+                  const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t hq,
+                  float scale, int32_t window, const int32_t* sel, int32_t m, void* out,
+                  float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,7 +1,7 @@
 """Python binding of ``libflashgmm.so``: the fused diagonal-GMM EM iteration on MI355X.
 
 Argument marshalling only: every step of the computation runs in the HIP
-kernels of ``csrc/flashgmm.hip``.  PyTorch provides the device memory (CUDA
+kernels of ``csrc/flashgmm.hip`` and ``csrc/kvcache.hip``.  PyTorch provides the device memory (CUDA
 tensors on ROCm) and the stream (``torch.cuda.current_stream()``); the entry
 points take the same names and arguments as the C ABI in
 ``include/flashgmm.h``.  There is no CPU fallback: without the built library
@@ -33,7 +33,9 @@ EXPORTS = ("gmm_status_string", "gmm_workspace_bytes", "gmm_estep_accumulate", "
            "gmm_estep_accumulate_iso", "gmm_mstep_iso", "gmm_fit_iso", "gmm_timing_enable",
            "gmm_timing_read", "gmm_estep_accumulate_screened", "gmm_fit_screened",
            "gmm_set_stats_chunk_limit", "gmm_estep_accumulate_static",
-           "gmm_estep_accumulate_ring", "gmm_fill_pageable")
+           "gmm_estep_accumulate_ring", "gmm_fill_pageable",
+           "gmm_rope_table", "gmm_rope", "gmm_kv_append", "gmm_kv_workspace_bytes",
+           "gmm_kv_select", "gmm_kv_attend")
 
 _lib = None
 
@@ -107,6 +109,7 @@ def load_library():
     lib.gmm_estep_accumulate_static.restype = ctypes.c_int
     lib.gmm_set_stats_chunk_limit.argtypes = [i32]
     lib.gmm_set_stats_chunk_limit.restype = ctypes.c_int
+    kv.bind(lib)
     _lib = lib
     return lib
 
@@ -446,3 +449,9 @@ def gmm_estep_accumulate_static(x, weights, means, variances, nk, s, q, loglik, 
         _ptr(_dev(q, torch.float64, "q", k * d)), _ptr(_dev(loglik, torch.float64, "loglik", 1)),
         _stream(stream))
     _check("gmm_estep_accumulate_static", rc)
+
+
+# the paged key/value cache (kv.py imports the helpers above)
+from . import kv  # noqa: E402
+from .kv import (KVCache, gmm_kv_append, gmm_kv_attend, gmm_kv_select, gmm_rope,  # noqa: E402,F401
+                 gmm_rope_table, kv_cache, kv_workspace, kv_workspace_bytes, rope_frequencies)

@@ -4,10 +4,12 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRC = os.path.join(HERE, "csrc", "flashgmm.hip")
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("flashgmm.hip", "kvcache.hip")]
 LIB = os.path.join(HERE, "libflashgmm.so")
 INCLUDE = os.path.join(ROOT, "include")
 
@@ -16,7 +18,6 @@ HIPCC_FLAGS = [
     "-O3",
     "-std=c++17",
     "-fPIC",
-    "-shared",
     # packed fp32 VALU instructions are kept out of every kernel
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
@@ -28,15 +29,29 @@ def hipcc() -> str:
     return cand if os.path.exists(cand) else "hipcc"
 
 
-def build(verbose: bool = False) -> str:
-    tmp = LIB + ".tmp"
-    cmd = [hipcc(), *HIPCC_FLAGS, "-I", INCLUDE, "-o", tmp, SRC]
-    res = subprocess.run(cmd, capture_output=True, text=True)
+def _compile(src: str, obj: str) -> str:
+    """Compiles one source; returns what the compiler printed."""
+    res = subprocess.run([hipcc(), *HIPCC_FLAGS, "-I", INCLUDE, "-c", "-o", obj, src],
+                         capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("hipcc failed building libflashgmm.so")
+        raise RuntimeError(f"hipcc failed compiling {os.path.basename(src)}")
+    return res.stderr
+
+
+def build(verbose: bool = False) -> str:
+    with tempfile.TemporaryDirectory() as tmpdir:
+        objs = [os.path.join(tmpdir, os.path.basename(s) + ".o") for s in SOURCES]
+        with ThreadPoolExecutor(len(SOURCES)) as pool:
+            printed = list(pool.map(_compile, SOURCES, objs))
+        tmp = LIB + ".tmp"
+        res = subprocess.run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", "-o", tmp,
+                              *objs], capture_output=True, text=True)
+        if res.returncode != 0:
+            sys.stderr.write(res.stdout + res.stderr)
+            raise RuntimeError("hipcc failed linking libflashgmm.so")
     if verbose:
-        sys.stderr.write(res.stderr)
+        sys.stderr.write("".join(printed) + res.stderr)
     os.replace(tmp, LIB)
     return LIB
 

@@ -1,0 +1,1347 @@
+// Paged key/value cache for AMD Instinct MI355X (gfx950): rotary positions, appending,
+// selection of pages by a cheap score, attention of new tokens over the cache.
+//
+// Attention is the E-step's pattern with other operands: a row's softmax weights are
+// responsibilities of equal isotropic components at the keys, formed with a running maximum
+// and sum (base 2) and contracted with the values in the same pass; the rows x keys matrix is
+// never stored.
+//
+// Cache layout.  A page holds its keys as rows [page, d] and its values transposed, [d, page].
+// Both products then take their cache operand in the register order of the matrix
+// instructions straight from memory, 16 bytes a lane, with nothing exchanged between lanes:
+//   S^T = K Q^T      A rows = keys: lane l holds 8 consecutive dimensions of key l % 16
+//   O^T = V^T P^T    A rows = dimensions: lane l holds 8 consecutive keys of dimension l % 16
+// The accumulator of the first product (lane: one query row, 4 keys) is the B operand of the
+// second (lane: one query row, 8 keys) when the keys of two 16-key tiles are interleaved in
+// groups of 4: row r of tile t is key 8 (r / 4) + 4 t + r % 4 of the 32.
+//
+// Results are bitwise reproducible: key ranges are fixed by the sizes, their partial results
+// are joined in order.  The only atomics are integer counts in LDS.
+
+#include <hip/hip_runtime.h>
+
+#include <float.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "flashgmm.h"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+// 1/127 rounded to fp32
+constexpr float kInv127 = 1.0f / 127.0f;
+// a launch has fewer than 2^32 threads
+constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 1;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+template <typename T> struct Vec8;
+template <> struct Vec8<__bf16> { typedef bf16x8 type; };
+template <> struct Vec8<_Float16> { typedef f16x8 type; };
+
+// 16x16x32: lane l holds A[l % 16][8 (l / 16) + e] and B[8 (l / 16) + e][l % 16], e = 0..7,
+// and D[4 (l / 16) + i][l % 16], i = 0..3
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ __forceinline__ float log2_fast(float v) { return __builtin_amdgcn_logf(v); }
+
+template <typename V>
+__device__ __forceinline__ V load16(const void* p) {
+  static_assert(sizeof(V) == 16, "16 bytes");
+  const uint4 u = *reinterpret_cast<const uint4*>(p);
+  return __builtin_bit_cast(V, u);
+}
+
+// 8 elements of a caller's row; vec: its rows allow 16-byte loads
+template <typename T>
+__device__ __forceinline__ typename Vec8<T>::type load_row8(const T* p, int vec) {
+  typedef typename Vec8<T>::type V8;
+  if (vec) return load16<V8>(p);
+  V8 v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = p[e];
+  return v;
+}
+
+__host__ __device__ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// ---------------------------------------------------------------- sequences
+struct Seqs {
+  const int32_t* cu;
+  const int32_t* total;
+  const int32_t* pages;
+  int64_t stride;
+  int batch, max_pages;
+  int page_shift;   // log2 of the page size
+  int cache_pages;
+};
+
+// Work items are numbered over all sequences without a table made beforehand: sequence b's
+// items start at first(b) = floor(cu[b] mul / div) + slack b, which leaves room for
+// ceil(n mul / div) items (slack 1), or one more (slack 2), for its n tokens.  The sequence of
+// an item is the last b with first(b) <= item: a search by the whole wave, 64 sequences a step.
+__device__ __forceinline__ int64_t first_item(const Seqs& s, int b, int mul, int div, int slack) {
+  return (int64_t)s.cu[b] * mul / div + (int64_t)slack * b;
+}
+__device__ __forceinline__ int find_seq(const Seqs& s, int64_t item, int mul, int div, int slack) {
+  int lo = 0, hi = s.batch;            // the answer is in [lo, hi)
+  const int lane = threadIdx.x & 63;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64;
+    const int b = lo + lane * step;
+    const bool in = b < hi && first_item(s, b, mul, div, slack) <= item;
+    const int cnt = __popcll(__ballot(in));    // first() grows with b: a prefix of the lanes
+    lo += (cnt > 0 ? cnt - 1 : 0) * step;
+    hi = min(hi, lo + step);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// physical page of a sequence's logical page, -1 if there is none
+__device__ __forceinline__ int phys_page(const Seqs& s, int b, int lp) {
+  if (lp < 0 || lp >= s.max_pages) return -1;
+  const int p = s.pages[(int64_t)b * s.stride + lp];
+  return (unsigned)p < (unsigned)s.cache_pages ? p : -1;
+}
+
+// ---------------------------------------------------------------- rotation
+// A head's row is handled in units of 2 W elements: pair units (W pairs each), then units of
+// the dimensions past rot.  A unit is two runs of W elements, at o0 and o1.
+struct RopeShape {
+  const float* table;
+  int positions, rot, inverse;
+};
+
+template <int W>
+struct Unit {
+  int o0, o1;
+  int pair;       // first pair, -1 for a unit past rot
+  __device__ __forceinline__ Unit(int u, int rot, bool inter) {
+    const int h = rot >> 1, hu = h / W;
+    if (u < hu && !inter) {
+      o0 = u * W;
+      o1 = h + u * W;
+    } else {
+      o0 = u * 2 * W;                 // hu pair units cover 2 W hu = rot dimensions
+      o1 = o0 + W;
+    }
+    pair = u < hu ? u * W : -1;
+  }
+};
+
+// a unit's elements, as one vector: an array that two branches fill would be kept in memory
+template <typename T, int W>
+using UnitV = T __attribute__((ext_vector_type(2 * W)));
+
+// W elements at p into / from the elements `at` .. at + W - 1 of v
+template <typename T, int W, typename V>
+__device__ __forceinline__ void load_run(const T* p, V& v, int at) {
+  if constexpr (W == 1) {
+    v[at] = p[0];
+  } else {
+    constexpr int E = 16 / sizeof(T);
+    typedef T Run __attribute__((ext_vector_type(E)));
+#pragma unroll
+    for (int i = 0; i < W / E; ++i) {
+      const Run r = load16<Run>(p + i * E);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[at + i * E + e] = r[e];
+    }
+  }
+}
+template <typename T, int W, typename V>
+__device__ __forceinline__ void store_run(T* p, const V& v, int at) {
+  if constexpr (W == 1) {
+    p[0] = v[at];
+  } else {
+    constexpr int E = 16 / sizeof(T);
+    typedef T Run __attribute__((ext_vector_type(E)));
+#pragma unroll
+    for (int i = 0; i < W / E; ++i) {
+      Run r;
+#pragma unroll
+      for (int e = 0; e < E; ++e) r[e] = v[at + i * E + e];
+      *reinterpret_cast<uint4*>(p + i * E) = __builtin_bit_cast(uint4, r);
+    }
+  }
+}
+
+// v: the unit's 2 W elements, in place.  Products and sums are rounded one by one, as the
+// formula is written, so that the result does not depend on where a compiler contracts.  The
+// layout is a template argument: with a run-time one the compiler joins both branches into
+// one with run-time indexes into v.
+template <typename T, int W, bool INTER>
+__device__ __forceinline__ void rotate_unit(UnitV<T, W>& v, int pair, int pos, const RopeShape& r) {
+#pragma clang fp contract(off)
+  if (pair < 0 || pos < 0) return;
+  UnitV<float, W> cs;                       // cosines, then sines
+  if (pos < r.positions) {
+    const float* row = r.table + (int64_t)pos * r.rot + pair;
+    load_run<float, W>(row, cs, 0);
+    load_run<float, W>(row + (r.rot >> 1), cs, W);
+  } else {
+    cs = UnitV<float, W>(__builtin_nanf(""));
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : i + W;
+    const float a = (float)v[ia], b = (float)v[ib], c = cs[i];
+    const float sn = r.inverse ? -cs[W + i] : cs[W + i];
+    v[ia] = (T)(a * c - b * sn);
+    v[ib] = (T)(b * c + a * sn);
+  }
+}
+
+template <typename T, int W, bool INTER>
+__device__ __forceinline__ void rope_unit(const T* x, T* out, int u, int pos, const RopeShape& r) {
+  const Unit<W> un(u, r.rot, INTER);
+  UnitV<T, W> v;
+  load_run<T, W>(x + un.o0, v, 0);
+  load_run<T, W>(x + un.o1, v, W);
+  rotate_unit<T, W, INTER>(v, un.pair, pos, r);
+  store_run<T, W>(out + un.o0, v, 0);
+  store_run<T, W>(out + un.o1, v, W);
+}
+
+__global__ __launch_bounds__(256) void k_rope_table(const double* __restrict__ freq, int half,
+                                                    double scale, int64_t positions,
+                                                    float* __restrict__ table) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= positions * half) return;
+  const int64_t p = i / half;
+  const int j = (int)(i - p * half);
+  double s, c;
+  sincos((double)p * freq[j], &s, &c);
+  table[p * 2 * half + j] = (float)(scale * c);
+  table[p * 2 * half + half + j] = (float)(scale * s);
+}
+
+// One token a workgroup row (grid.x), 256 units of its heads a workgroup (grid.y); a unit is
+// 16 elements (W = 8: 16-byte accesses) where rot, d, the strides and the addresses allow it,
+// else one pair.  An odd count of dimensions past rot ends in a unit of its own (W = 1).
+template <typename T, int W, bool INTER>
+__global__ __launch_bounds__(256) void k_rope(const T* x, int64_t xt, int64_t xh, T* out,
+                                              int64_t ot, int64_t oh, int heads, int d,
+                                              const int32_t* __restrict__ pos, RopeShape r) {
+  const int64_t t = blockIdx.x;
+  const int units = (d + 2 * W - 1) / (2 * W);
+  const int i = blockIdx.y * 256 + threadIdx.x;
+  if (i >= heads * units) return;
+  const int h = i / units, u = i - h * units;
+  const T* xr = x + t * xt + (int64_t)h * xh;
+  T* orow = out + t * ot + (int64_t)h * oh;
+  if (W == 1 && 2 * u + 1 >= d && u >= (r.rot >> 1)) {
+    orow[d - 1] = xr[d - 1];
+    return;
+  }
+  rope_unit<T, W, INTER>(xr, orow, u, pos[t], r);
+}
+
+// ---------------------------------------------------------------- append
+struct AppendArgs {
+  Seqs s;
+  void* ck;
+  void* cv;
+  int8_t* box;
+  float* box_scale;
+  int heads, page, d;
+  const void* k;
+  int64_t kt, kh;
+  const void* v;
+  int64_t vt, vh;
+  int v_vec;                 // value rows can be read 16 bytes at a time
+  const int32_t* pos;
+  RopeShape rope;            // table null: no rotation
+  const void* q;
+  int64_t qt, qh;
+  void* qo;
+  int64_t qot, qoh;
+  int hq;
+  int64_t page_blocks;       // workgroups of pages; the rest rotate queries
+  int q_blocks;              // workgroups a token's queries take
+};
+
+// One workgroup a (page touched, head): the page's new keys are rotated and stored, its new
+// values stored transposed, and its box formed from all its keys, the older ones read back
+// (a page of 64 keys of 128 dimensions is 16 KB, so a single new token moves 8 KB on average
+// for a box that saves reading that page in every later step in which it is not selected).
+// The queries' rotation rides along in workgroups of its own: one launch for the step.
+template <typename T, int W, bool INTER>
+__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
+  const int tid = threadIdx.x;
+  if ((int64_t)blockIdx.x >= a.page_blocks) {
+    const int64_t qb = (int64_t)blockIdx.x - a.page_blocks;
+    const int64_t t = qb / a.q_blocks;
+    const int units = a.d / (2 * W);
+    int p;
+    if (a.pos) {
+      p = a.pos[t];
+    } else {
+      // the sequence of row t is the last with cu[b] <= t that is not empty there
+      const int b = find_seq(a.s, t, 1, 1, 0);
+      p = a.s.total[b] - (a.s.cu[b + 1] - (int)t);
+    }
+    const int i = (int)(qb - t * a.q_blocks) * 256 + tid;
+    if (i >= a.hq * units) return;
+    const int h = i / units, u = i - h * units;
+    rope_unit<T, W, INTER>((const T*)a.q + t * a.qt + (int64_t)h * a.qh,
+                    (T*)a.qo + t * a.qot + (int64_t)h * a.qoh, u, p, a.rope);
+    return;
+  }
+  __shared__ T red[256 * 2 * W * 2];
+  __shared__ float wmax[4];
+  const int head = blockIdx.x % a.heads;
+  const int64_t item = blockIdx.x / a.heads;
+  const int P = a.page, d = a.d;
+  const int b = find_seq(a.s, item, 1, P, 2);
+  const int row0 = a.s.cu[b], n = a.s.cu[b + 1] - row0, total = a.s.total[b];
+  if (n <= 0) return;
+  const int64_t s0l = (int64_t)total - n;
+  const int s0 = s0l < 0 ? 0 : (int)s0l;                 // first new slot that exists
+  const int64_t lp64 = (s0 >> a.s.page_shift) + (item - first_item(a.s, b, 1, P, 2));
+  if ((lp64 << a.s.page_shift) >= total) return;
+  const int lp = (int)lp64;
+  const int phys = phys_page(a.s, b, lp);
+  if (phys < 0) return;
+  const int first = lp << a.s.page_shift;                // first slot of the page
+  const int filled = min(P, total - first);
+  const int begin = max(0, s0 - first);                  // new keys: begin .. filled - 1
+  const int64_t ph = (int64_t)phys * a.heads + head;
+  const int64_t in0 = row0 + ((int64_t)first - s0l);     // input row of the page's slot 0
+
+  // keys
+  T* ckp = (T*)a.ck + ph * P * d;
+  const int units = d / (2 * W), groups = 256 / units;
+  const int u = tid % units, g = tid / units;
+  const Unit<W> un(u, a.rope.rot, INTER);
+  UnitV<float, W> hi = -INFINITY, lo = INFINITY;
+  bool bad = false;
+  const int from = a.box ? 0 : begin;
+  if (g < groups) {
+    for (int s = from + g; s < filled; s += groups) {
+      UnitV<T, W> v;
+      if (s < begin) {
+        load_run<T, W>(ckp + (int64_t)s * d + un.o0, v, 0);
+        load_run<T, W>(ckp + (int64_t)s * d + un.o1, v, W);
+      } else {
+        const int64_t r = in0 + s;
+        const T* kr = (const T*)a.k + r * a.kt + (int64_t)head * a.kh;
+        load_run<T, W>(kr + un.o0, v, 0);
+        load_run<T, W>(kr + un.o1, v, W);
+        if (a.rope.table) rotate_unit<T, W, INTER>(v, un.pair, a.pos ? a.pos[r] : first + s, a.rope);
+        store_run<T, W>(ckp + (int64_t)s * d + un.o0, v, 0);
+        store_run<T, W>(ckp + (int64_t)s * d + un.o1, v, W);
+      }
+      if (a.box) {
+#pragma unroll
+        for (int e = 0; e < 2 * W; ++e) {
+          const float f = (float)v[e];
+          bad |= !(fabsf(f) <= FLT_MAX);
+          hi[e] = fmaxf(hi[e], f);
+          lo[e] = fminf(lo[e], f);
+        }
+      }
+    }
+  }
+
+  // values: 8 slots x 8 dimensions a thread, slots fastest over the lanes, so that a
+  // dimension's run of slots is written in whole lines
+  {
+    T* cvp = (T*)a.cv + ph * d * P;
+    const int g0 = begin >> 3, ng = ((filled + 7) >> 3) - g0, nc = d >> 3;
+    for (int i = tid; i < ng * nc; i += 256) {
+      const int c = i / ng, sg = (g0 + i - c * ng) << 3;
+      typename Vec8<T>::type blk[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int s = sg + j;
+        if (s >= begin && s < filled) {
+          const T* vr = (const T*)a.v + (in0 + s) * a.vt + (int64_t)head * a.vh + c * 8;
+          blk[j] = load_row8(vr, a.v_vec);
+        } else {
+          blk[j] = typename Vec8<T>::type((T)0.0f);
+        }
+      }
+      const bool whole = sg >= begin && sg + 8 <= filled;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        T* dst = cvp + (int64_t)(c * 8 + e) * P + sg;
+        if (whole) {
+          typename Vec8<T>::type col;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) col[j] = blk[j][e];
+          *reinterpret_cast<uint4*>(dst) = __builtin_bit_cast(uint4, col);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (sg + j >= begin && sg + j < filled) dst[j] = blk[j][e];
+        }
+      }
+    }
+  }
+  if (!a.box) return;
+
+  // box: the keys are of type T, so their bounds are kept in T without rounding
+  T* rhi = red;
+  T* rlo = red + 256 * 2 * W;
+  if (g < groups) {
+#pragma unroll
+    for (int e = 0; e < 2 * W; ++e) {
+      const int dim = (e < W ? un.o0 : un.o1 - W) + e;
+      rhi[g * d + dim] = (T)hi[e];
+      rlo[g * d + dim] = (T)lo[e];
+    }
+  }
+  const int any_bad = __syncthreads_or(bad);
+  float h = -INFINITY, l = INFINITY, m = 0.0f;
+  if (tid < d) {
+    for (int j = 0; j < groups; ++j) {
+      h = fmaxf(h, (float)rhi[j * d + tid]);
+      l = fminf(l, (float)rlo[j * d + tid]);
+    }
+    m = fmaxf(fabsf(h), fabsf(l));
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  if ((tid & 63) == 0) wmax[tid >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
+  const float unit = any_bad ? INFINITY : m * kInv127;
+  if (tid < d) {
+    float bh = 0.0f, bl = 0.0f;
+    if (!any_bad && unit > 0.0f) {
+      bh = fminf(127.0f, ceilf(__fdiv_rn(h, unit)));
+      bl = fmaxf(-127.0f, floorf(__fdiv_rn(l, unit)));
+    }
+    a.box[ph * 2 * d + tid] = (int8_t)(int)fmaxf(-127.0f, bh);
+    a.box[ph * 2 * d + d + tid] = (int8_t)(int)fminf(127.0f, bl);
+  }
+  if (tid == 0) a.box_scale[ph] = unit;
+}
+
+// ---------------------------------------------------------------- selection
+struct SelectArgs {
+  Seqs s;
+  const int8_t* box;
+  const float* box_scale;
+  const void* q;
+  int64_t qt, qh;
+  int q_vec;
+  int heads, group, d;
+  int col_shift;             // log2 of the columns a token takes in a 16-column tile
+  int col_tiles;             // 16-column tiles a token takes (1 unless group > 16)
+  float* score;              // [tokens * heads][row]
+  int64_t row;
+  int chunk_tiles;           // 16-page tiles a wave scores
+  int parts;                 // workgroups a row of tiles takes
+};
+
+__device__ __forceinline__ float score_of(float query_unit, float page_unit, int dot) {
+#pragma clang fp contract(off)
+  return query_unit * page_unit * (float)dot + 0.0f;      // -0 becomes 0
+}
+
+// Scores: [pages x 2 d] . [2 d x (token, query head)] in 8-bit integers on 16x16x64 MFMA, the
+// boxes (upper | lower bounds) straight from memory in operand order, the queries (positive |
+// negative parts) from LDS.  Bound by the boxes' bytes: 2 d + 4 a (page, head).
+template <typename T>
+__global__ __launch_bounds__(256) void k_select_score(SelectArgs a) {
+  extern __shared__ int8_t q8[];            // [col_tiles][16][2 d], then the units [.][16]
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = 16 >> a.col_shift;        // tokens a tile holds
+  const int part_no = blockIdx.x % a.parts;
+  const int head = blockIdx.x / a.parts % a.heads;
+  const int64_t item = blockIdx.x / a.parts / a.heads;
+  const int b = find_seq(a.s, item, 1, per, 1);
+  const int row0 = a.s.cu[b], n = a.s.cu[b + 1] - row0;
+  const int tok0 = (int)(item - first_item(a.s, b, 1, per, 1)) * per;
+  if (tok0 >= n) return;
+  const int toks = min(per, n - tok0);
+  const int64_t total = min((int64_t)a.s.total[b], (int64_t)a.s.max_pages << a.s.page_shift);
+  const int64_t last = min(total - 1, (int64_t)a.s.total[b] - n + tok0 + toks - 1);
+  const int visible = last < 0 ? 0 : (int)(last >> a.s.page_shift) + 1;
+  const int tile0 = (part_no * 4 + wave) * a.chunk_tiles;
+  if (part_no * 4 * a.chunk_tiles * 16 >= visible) return;
+
+  // queries in 8 bits: 16 threads a column, 16 columns at a time
+  const int d = a.d, cols = a.col_tiles * 16;
+  float* unit = reinterpret_cast<float*>(q8 + (size_t)cols * 2 * d);
+  for (int c0 = 0; c0 < cols; c0 += 16) {
+    const int c = c0 + (tid >> 4), part = tid & 15;
+    const int tt = (c & 15) >> a.col_shift, hh = c0 + (c & ((1 << a.col_shift) - 1));
+    const bool live = tt < toks && hh < a.group;
+    const T* qr = (const T*)a.q + (int64_t)(row0 + tok0 + (live ? tt : 0)) * a.qt +
+                  (int64_t)(head * a.group + (live ? hh : 0)) * a.qh;
+    float m = 0.0f;
+    bool bad = false;
+    for (int e = part; e < d; e += 16) {
+      const float f = live ? fabsf((float)qr[e]) : 0.0f;
+      bad |= !(f <= FLT_MAX);
+      m = fmaxf(m, f);
+    }
+    int ib = bad;
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      m = fmaxf(m, __shfl_xor(m, o));
+      ib |= __shfl_xor(ib, o);
+    }
+    const float un = ib ? INFINITY : m * kInv127;
+    const bool zero = ib || !(un > 0.0f);
+    for (int e = part; e < d; e += 16) {
+      const float f = live && !zero ? rintf(__fdiv_rn((float)qr[e], un)) : 0.0f;
+      q8[(size_t)c * 2 * d + e] = (int8_t)(int)fmaxf(f, 0.0f);
+      q8[(size_t)c * 2 * d + d + e] = (int8_t)(int)fminf(f, 0.0f);
+    }
+    if (part == 0) unit[c] = live ? un : -1.0f;          // -1: no query in this column
+  }
+  __syncthreads();
+
+  const int n16 = lane & 15, g = lane >> 4;
+  const int steps = (2 * d + 63) / 64;
+  for (int t = 0; t < a.chunk_tiles; ++t) {
+    const int p0 = (tile0 + t) * 16;
+    if (p0 >= visible) break;
+    const int lp = p0 + n16;
+    const int phys = lp < visible ? phys_page(a.s, b, lp) : -1;
+    const int64_t rec = (int64_t)max(phys, 0) * a.heads + head;
+    const float sp = a.box_scale[rec];
+    i32x4 bx[8];
+#pragma unroll
+    for (int st = 0; st < 8; ++st) {
+      if (st >= steps) break;
+      const int off = min(64 * st + 16 * g, 2 * d - 16);  // past the end: times 0 below
+      bx[st] = load16<i32x4>(a.box + rec * 2 * d + off);
+    }
+    float best[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) best[i] = -INFINITY;
+    for (int ct = 0; ct < a.col_tiles; ++ct) {
+      i32x4 acc = {0, 0, 0, 0};
+      const int8_t* qc = q8 + (size_t)(ct * 16 + n16) * 2 * d;
+#pragma unroll
+      for (int st = 0; st < 8; ++st) {
+        if (st >= steps) break;
+        const int off = 64 * st + 16 * g;
+        i32x4 qv = {0, 0, 0, 0};
+        if (off < 2 * d) qv = *reinterpret_cast<const i32x4*>(qc + off);
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(bx[st], qv, acc, 0, 0, 0);
+      }
+      const float un = unit[ct * 16 + n16];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float spi = __shfl(sp, 4 * g + i);
+        float v = score_of(un, spi, acc[i]);
+        v = v != v ? INFINITY : v;         // a page or query that has no bound comes first
+        best[i] = un < 0.0f ? best[i] : fmaxf(best[i], v);
+      }
+    }
+    for (int o = 1; o < (1 << a.col_shift); o <<= 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) best[i] = fmaxf(best[i], __shfl_xor(best[i], o));
+    const int tt = n16 >> a.col_shift;
+    if ((n16 & ((1 << a.col_shift) - 1)) == 0 && tt < toks && p0 + 4 * g < a.row) {
+      const int64_t r = (int64_t)(row0 + tok0 + tt) * a.heads + head;
+      *reinterpret_cast<float4*>(a.score + r * a.row + p0 + 4 * g) =
+          make_float4(best[0], best[1], best[2], best[3]);
+    }
+  }
+}
+
+// order-preserving integer of a score
+__device__ __forceinline__ uint32_t score_key(float v) {
+  const uint32_t u = __float_as_uint(v);
+  return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
+}
+
+// The m best pages of a row, one workgroup a row: the m-th largest key by four 8-bit digit
+// counts from the top, then the pages above it and the lowest ones equal to it in page order.
+__global__ __launch_bounds__(256) void k_select_top(Seqs s, const float* __restrict__ score,
+                                                    int64_t row, int heads, int m, int keep_first,
+                                                    int keep_last, int32_t* __restrict__ idx) {
+  __shared__ int hist[256];
+  __shared__ int wsum[4][2];
+  __shared__ uint32_t sh_prefix;
+  __shared__ int sh_left;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t r = blockIdx.x, t = r / heads;
+  const int b = find_seq(s, t, 1, 1, 0);
+  const int64_t slot = (int64_t)s.total[b] - (s.cu[b + 1] - t);
+  const int64_t nv64 = slot < 0 ? 0 : (slot >> s.page_shift) + 1;
+  const int nv = (int)min(nv64, (int64_t)s.max_pages);
+  int32_t* out = idx + r * m;
+  if (nv <= m) {
+    for (int i = tid; i < m; i += 256) out[i] = i < nv ? i : -1;
+    return;
+  }
+  const float* sc = score + r * row;
+  const auto key = [&](int p) {
+    return p < keep_first || p >= nv - keep_last ? 0xFFFFFFFFu : score_key(sc[p]);
+  };
+  uint32_t prefix = 0;
+  int left = m;                       // rank of the wanted key among those with the prefix
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    hist[tid] = 0;
+    __syncthreads();
+    for (int p = tid; p < nv; p += 256) {
+      const uint32_t k = key(p);
+      if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1);
+    }
+    __syncthreads();
+    // counts of the digits above this thread's
+    const int digit = 255 - tid;
+    const int c = hist[digit];
+    int incl = c;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(incl, o);
+      if (lane >= o) incl += v;
+    }
+    if (lane == 63) wsum[wave][0] = incl;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) incl += wsum[w][0];
+    if (incl >= left && incl - c < left) {
+      sh_prefix = (prefix << 8) | digit;
+      sh_left = left - (incl - c);
+    }
+    __syncthreads();
+    prefix = sh_prefix;
+    left = sh_left;
+  }
+  // `left` pages with exactly this key are taken, the lowest ones
+  int done = 0, eq_done = 0;
+  for (int p0 = 0; p0 < nv; p0 += 256) {
+    const int p = p0 + tid;
+    const uint32_t k = p < nv ? key(p) : 0;
+    const bool gt = p < nv && k > prefix, eq = p < nv && k == prefix;
+    const uint64_t meq = __ballot(eq), below = ((uint64_t)1 << lane) - 1;
+    __syncthreads();
+    if (lane == 0) wsum[wave][0] = __popcll(meq);
+    __syncthreads();
+    int eq_rank = eq_done + __popcll(meq & below);
+    for (int w = 0; w < wave; ++w) eq_rank += wsum[w][0];
+    const bool take = gt || (eq && eq_rank < left);
+    const uint64_t mt = __ballot(take);
+    if (lane == 0) wsum[wave][1] = __popcll(mt);
+    __syncthreads();
+    int at = done + __popcll(mt & below);
+    for (int w = 0; w < wave; ++w) at += wsum[w][1];
+    if (take && at < m) out[at] = p;
+    for (int w = 0; w < 4; ++w) {
+      eq_done += wsum[w][0];
+      done += wsum[w][1];
+    }
+  }
+}
+
+// ---------------------------------------------------------------- attention
+struct AttendArgs {
+  Seqs s;
+  const void* k;
+  const void* v;
+  int heads, group, d;
+  const void* q;
+  int64_t qt, qh;
+  int q_vec;
+  float scale2;              // scale log2(e)
+  int window;
+  const int32_t* sel;
+  int m;
+  void* out;
+  float* lse;
+  int hq;
+  int64_t tokens;
+  int chunk;                 // keys (or list entries) a workgroup takes
+  int splits;                // 1: results go to out, else partial results
+  float* part_o;             // [splits][tokens * hq][d], not divided by the sum
+  float* part_ml;            // [splits][tokens * hq][2]: maximum (base 2), sum
+  int tiles_token;           // selection: row tiles a (token, head) takes
+};
+
+// A few query rows (16 RT: tokens x heads of a group) against a range of keys; 4 waves take
+// every fourth step of 32 keys each, straight from memory into matrix operands, and are
+// joined at the end.  Every byte of the cache is read by one wave once, so LDS would only add
+// a trip; the next step's 16 KB (d = 128) are in flight while one is computed.  Bound by the
+// cache's bytes.
+template <typename T, int NS, int RT, bool SEL>
+__global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
+  typedef typename Vec8<T>::type V8;
+  constexpr int ND = 2 * NS;                 // 16-dimension tiles of the result
+  constexpr int R = 16 * RT;
+  __shared__ float sm[4][R], sl[4][R];
+  __shared__ f32x4 so[2][ND][64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n16 = lane & 15, g = lane >> 4;
+  const int head = blockIdx.x % a.heads;
+  const int64_t item = blockIdx.x / a.heads;
+  const int split = blockIdx.y;
+  const int P = 1 << a.s.page_shift, d = a.d, G = a.group;
+
+  int b, r0, rows, row0, n;
+  int64_t tok = 0;
+  if constexpr (SEL) {
+    tok = item / a.tiles_token;
+    b = find_seq(a.s, tok, 1, 1, 0);
+    row0 = a.s.cu[b];
+    n = a.s.cu[b + 1] - row0;
+    r0 = (int)(tok - row0) * G + (int)(item - tok * a.tiles_token) * R;
+    rows = min(R, (int)(tok - row0 + 1) * G - r0);
+  } else {
+    b = find_seq(a.s, item, G, R, 1);
+    row0 = a.s.cu[b];
+    n = a.s.cu[b + 1] - row0;
+    const int64_t rr = (item - first_item(a.s, b, G, R, 1)) * R;
+    if (rr >= (int64_t)n * G) return;
+    r0 = (int)rr;
+    rows = (int)min((int64_t)R, (int64_t)n * G - rr);
+  }
+  // keys that exist for this sequence, and slots of the rows
+  const int total = a.s.total[b];
+  const int64_t held = min((int64_t)total, (int64_t)a.s.max_pages << a.s.page_shift);
+  int64_t lim[RT], low[RT];
+  V8 qf[RT][NS];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = rt * 16 + n16;
+    const bool live = r < rows;
+    const int rr = r0 + (live ? r : 0), ti = rr / G, hh = rr - ti * G;
+    const int64_t slot = (int64_t)total - n + ti;
+    lim[rt] = live ? min(slot, held - 1) : -1;
+    low[rt] = a.window > 0 ? slot - a.window + 1 : 0;
+    const T* qr = (const T*)a.q + (int64_t)(row0 + ti) * a.qt + (int64_t)(head * G + hh) * a.qh;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const int dim = 32 * s + 8 * g;
+      V8 v = load_row8(qr + min(dim, d - 8), a.q_vec);
+      if (dim >= d)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (T)0.0f;
+      qf[rt][s] = v;
+    }
+  }
+  // the tile's keys: [klo, khi)
+  const int64_t khi = min(held, (int64_t)total - n + (r0 + rows - 1) / G + 1);
+  const int64_t klo = a.window > 0 ? max((int64_t)0, (int64_t)total - n + r0 / G - a.window + 1) : 0;
+  // steps of 32 keys: [st0, st1) in units of 32 keys, or of (list entry, part of its page)
+  int64_t st0, st1;
+  const int sub_shift = a.s.page_shift - 5;
+  if constexpr (SEL) {
+    st0 = ((int64_t)split * a.chunk) << sub_shift;
+    st1 = min(((int64_t)(split + 1) * a.chunk), (int64_t)a.m) << sub_shift;
+  } else {
+    const int64_t c0 = (int64_t)split * a.chunk, c1 = c0 + a.chunk;
+    if (c0 >= khi || c1 <= klo) {
+      if (a.splits > 1 || khi > klo) return;
+      st0 = st1 = 0;                        // rows that see no key: zeros
+    } else {
+      st0 = max(c0, klo) >> 5;
+      st1 = (min(c1, khi) + 31) >> 5;
+    }
+  }
+  const int32_t* list = SEL ? a.sel + (tok * a.heads + head) * a.m : nullptr;
+  const T* kc = (const T*)a.k;
+  const T* vc = (const T*)a.v;
+  const int krow = 8 * (n16 >> 2) + (n16 & 3);
+
+  // a step's page and first key; page -1: nothing to read
+  const auto locate = [&](int64_t st, int& phys, int64_t& key) {
+    int lp, sub;
+    if constexpr (SEL) {
+      lp = list[st >> sub_shift];
+      sub = (int)(st & ((1 << sub_shift) - 1));
+      key = ((int64_t)lp << a.s.page_shift) + 32 * sub;
+      phys = lp >= 0 && key < khi ? phys_page(a.s, b, lp) : -1;
+    } else {
+      key = st << 5;
+      phys = phys_page(a.s, b, (int)(key >> a.s.page_shift));
+    }
+    phys = __builtin_amdgcn_readfirstlane(phys);
+  };
+  V8 kf[2][NS], vf[ND];
+  const auto load = [&](int phys, int64_t key) {
+    const int64_t rec = ((int64_t)phys * a.heads + head) * P * d;
+    const int off = (int)(key & (P - 1));
+    const T* kp = kc + rec + (int64_t)off * d;
+    const T* vp = vc + rec + off;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+        kf[t][s] = load16<V8>(kp + (krow + 4 * t) * d + min(32 * s + 8 * g, d - 8));
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+      vf[dt] = load16<V8>(vp + min(16 * dt + n16, d - 1) * P + 8 * g);
+  };
+
+  f32x4 o[RT][ND];
+  float mx[RT], sum[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    mx[rt] = -INFINITY;
+    sum[rt] = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) o[rt][dt] = f32x4{0, 0, 0, 0};
+  }
+
+  for (int64_t st = st0 + wave; st < st1; st += 4) {
+    int phys;
+    int64_t key;
+    locate(st, phys, key);
+    if (phys < 0) continue;
+    load(phys, key);
+    if (key + 32 > khi) {
+      // slots past the last key may hold anything: 0 x NaN must not reach the sums
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (key + 8 * g + e >= khi) vf[dt][e] = (T)0.0f;
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      f32x4 sc[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        sc[t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < NS; ++s) sc[t] = mfma16(kf[t][s], qf[rt][s], sc[t]);
+      }
+      float m = mx[rt];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int64_t kk = key + 8 * g + 4 * t + i;
+          const float v = sc[t][i] * a.scale2;
+          sc[t][i] = kk <= lim[rt] && kk >= low[rt] ? v : -INFINITY;
+          m = fmaxf(m, sc[t][i]);
+        }
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      const float base = m == -INFINITY ? 0.0f : m;
+      const float alpha = exp2_fast(mx[rt] - base);
+      mx[rt] = m;
+      V8 p;
+      float z = 0.0f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = exp2_fast(sc[t][i] - base);
+          z += e;
+          p[4 * t + i] = (T)e;           // weights in [0, 1], rounded for the matrix product
+        }
+      sum[rt] = sum[rt] * alpha + z;
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) {
+        o[rt][dt] *= alpha;
+        o[rt][dt] = mfma16(vf[dt], p, o[rt][dt]);
+      }
+    }
+  }
+
+  // join the four waves
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    sum[rt] += __shfl_xor(sum[rt], 16);
+    sum[rt] += __shfl_xor(sum[rt], 32);
+    if (g == 0) {
+      sm[wave][rt * 16 + n16] = mx[rt];
+      sl[wave][rt * 16 + n16] = sum[rt];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int c = rt * 16 + n16;
+    const float mm = fmaxf(fmaxf(sm[0][c], sm[1][c]), fmaxf(sm[2][c], sm[3][c]));
+    const float base = mm == -INFINITY ? 0.0f : mm;
+    float z = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) z += sl[w][c] * exp2_fast(sm[w][c] - base);
+    const float f = exp2_fast(mx[rt] - base);
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) o[rt][dt] *= f;
+    if (wave >= 2)
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) so[wave - 2][dt][lane] = o[rt][dt];
+    __syncthreads();
+    if (wave < 2)
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) o[rt][dt] += so[wave][dt][lane];
+    __syncthreads();
+    if (wave == 1)
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) so[0][dt][lane] = o[rt][dt];
+    __syncthreads();
+    if (wave == 0 && c < rows) {
+      const int rr = r0 + c, ti = rr / G, hh = rr - ti * G;
+      const int64_t orow = (int64_t)(row0 + ti) * a.hq + head * G + hh;
+      const float inv = z > 0.0f ? 1.0f / z : 0.0f;
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) {
+        const f32x4 v = o[rt][dt] + so[0][dt][lane];
+        const int dim = 16 * dt + 4 * g;
+        if (dim >= d) continue;
+        if (a.splits == 1) {
+          alignas(8) T w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = (T)(z > 0.0f ? v[i] * inv : z);
+          *reinterpret_cast<uint2*>((T*)a.out + orow * d + dim) = *reinterpret_cast<uint2*>(w);
+        } else {
+          const int64_t pr = (int64_t)split * a.tokens * a.hq + orow;
+          *reinterpret_cast<f32x4*>(a.part_o + pr * d + dim) = v;
+        }
+      }
+      if (g == 0) {
+        if (a.splits == 1) {
+          if (a.lse) a.lse[orow] = z > 0.0f ? (mm + log2_fast(z)) * kLn2 : (z == 0.0f ? -INFINITY : z);
+        } else {
+          float* ml = a.part_ml + ((int64_t)split * a.tokens * a.hq + orow) * 2;
+          ml[0] = mm;
+          ml[1] = z;
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the partial results of the key ranges, in their order: a wave a row.
+template <typename T, bool SEL>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t orow = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t nrows = a.tokens * a.hq;
+  if (orow >= nrows) return;
+  const int64_t t = orow / a.hq;
+  const int b = find_seq(a.s, t, 1, 1, 0);
+  const int64_t total = a.s.total[b];
+  const int64_t held = min(total, (int64_t)a.s.max_pages << a.s.page_shift);
+  const int64_t slot = total - (a.s.cu[b + 1] - t);
+  const int64_t hi = min(slot, held - 1);
+  const int64_t lo = a.window > 0 ? max((int64_t)0, slot - a.window + 1) : 0;
+  int c0 = 0, c1 = a.splits;
+  if constexpr (!SEL) {
+    c0 = (int)(lo / a.chunk);
+    c1 = hi < lo ? c0 : (int)(hi / a.chunk) + 1;
+  }
+  float mm = -INFINITY;
+  for (int c = c0 + lane; c < c1; c += 64)
+    mm = fmaxf(mm, a.part_ml[((int64_t)c * nrows + orow) * 2]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o));
+  const float base = mm == -INFINITY ? 0.0f : mm;
+  float z = 0.0f;
+  f32x4 acc = {0, 0, 0, 0};
+  for (int c = c0; c < c1; ++c) {
+    const int64_t pr = (int64_t)c * nrows + orow;
+    const float f = exp2_fast(a.part_ml[pr * 2] - base);
+    z += a.part_ml[pr * 2 + 1] * f;
+    if (lane * 4 < a.d) acc += f * *reinterpret_cast<const f32x4*>(a.part_o + pr * a.d + lane * 4);
+  }
+  if (lane * 4 < a.d) {
+    alignas(8) T w[4];
+    const float inv = 1.0f / z;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (T)(z > 0.0f ? acc[i] * inv : z);
+    *reinterpret_cast<uint2*>((T*)a.out + orow * a.d + lane * 4) = *reinterpret_cast<uint2*>(w);
+  }
+  if (lane == 0 && a.lse)
+    a.lse[orow] = z > 0.0f ? (mm + log2_fast(z)) * kLn2 : (z == 0.0f ? -INFINITY : z);
+}
+
+// ---------------------------------------------------------------- host
+int launch_status() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? GMM_OK : GMM_ERR_DEVICE;
+}
+
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+inline bool is_pow2(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }
+inline int log2i(int v) {
+  int s = 0;
+  while ((1 << s) < v) ++s;
+  return s;
+}
+
+int check_cache(const gmm_kv_cache* c) {
+  if (!c || !c->k || !c->v) return GMM_ERR_INVALID_ARG;
+  if (c->pages < 1 || c->heads < 1 || c->page < 1 || c->d < 1) return GMM_ERR_INVALID_ARG;
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->box)) return GMM_ERR_INVALID_ARG;
+  if ((c->box == nullptr) != (c->box_scale == nullptr)) return GMM_ERR_INVALID_ARG;
+  if (c->dtype != GMM_BF16 && c->dtype != GMM_F16) return GMM_ERR_UNSUPPORTED;
+  if (c->d % 16 || c->d > GMM_KV_MAX_D || !is_pow2(c->page) || c->page < 32 || c->page > 256 ||
+      c->heads > GMM_KV_MAX_HEADS)
+    return GMM_ERR_UNSUPPORTED;
+  return GMM_OK;
+}
+
+int check_seqs(const gmm_kv_cache* c, const gmm_kv_batch* s, int64_t tokens, Seqs* o) {
+  if (!s || !s->cu || !s->total || !s->pages) return GMM_ERR_INVALID_ARG;
+  if (s->batch < 1 || s->max_pages < 1 || s->pages_stride < s->max_pages || tokens < 0)
+    return GMM_ERR_INVALID_ARG;
+  // slots are 32-bit; rows (tokens x heads) too
+  if ((int64_t)s->max_pages * c->page > INT32_MAX || tokens > (1 << 24) || s->batch > (1 << 20))
+    return GMM_ERR_UNSUPPORTED;
+  *o = Seqs{s->cu, s->total, s->pages, s->pages_stride, s->batch, s->max_pages, log2i(c->page),
+            c->pages};
+  return GMM_OK;
+}
+
+int check_heads(const gmm_kv_cache* c, int32_t hq) {
+  if (hq < 1 || hq % c->heads) return GMM_ERR_INVALID_ARG;
+  if (hq > GMM_KV_MAX_HEADS || hq / c->heads > GMM_KV_MAX_GROUP) return GMM_ERR_UNSUPPORTED;
+  return GMM_OK;
+}
+
+// Row tiles and key ranges of an attention call.
+struct Plan {
+  int rt;                  // k_attend_few: 16 rt rows a tile
+  int64_t items;           // row tiles of a head
+  int tiles_token;
+  int chunk, splits;
+};
+
+// Workgroups wanted: 256 CUs hold 2 each; four rounds of them even out ragged lengths.
+constexpr int64_t kWantGroups = 2048;
+constexpr int kMaxSplits = 1024;
+
+// 64 rows keep 64 registers of queries, results and keys each above 128 dimensions: too many
+int few_rows(int64_t rows, int d) { return rows <= 16 ? 1 : rows <= 32 || d > 128 ? 2 : 4; }
+
+Plan plan_dense(int heads, int page, int d, int64_t tokens, int32_t batch, int group,
+                int32_t max_pages) {
+  Plan p;
+  p.rt = few_rows(cdiv(tokens, batch) * group, d);
+  p.items = tokens * group / (16 * p.rt) + batch;
+  p.tiles_token = 0;
+  const int64_t keys = (int64_t)max_pages * page;
+  int64_t want = cdiv(kWantGroups, p.items * heads);
+  if (want > kMaxSplits) want = kMaxSplits;
+  // at least 128 keys: a step of 32 for every wave
+  int64_t chunk = cdiv(cdiv(keys, want), 128) * 128;
+  p.chunk = (int)chunk;
+  p.splits = (int)cdiv(keys, chunk);
+  return p;
+}
+
+Plan plan_sel(int heads, int page, int d, int64_t tokens, int group, int32_t m) {
+  Plan p;
+  p.rt = few_rows(group, d);
+  p.tiles_token = (int)cdiv(group, 16 * p.rt);
+  p.items = tokens * p.tiles_token;
+  int64_t want = cdiv(kWantGroups, p.items * heads);
+  if (want > kMaxSplits) want = kMaxSplits;
+  const int least = page >= 128 ? 1 : 128 / page;
+  int64_t chunk = cdiv(m, want);
+  if (chunk < least) chunk = least;
+  p.chunk = (int)chunk;
+  p.splits = (int)cdiv(m, chunk);
+  return p;
+}
+
+int64_t part_bytes(int64_t tokens, int hq, int d, int splits) {
+  return splits <= 1 ? 0 : (int64_t)splits * tokens * hq * (d + 2) * 4;
+}
+
+int64_t score_row(int32_t max_pages) { return cdiv(max_pages, 4) * 4; }
+
+int64_t ws_need(const gmm_kv_cache* c, int64_t tokens, int hq, int32_t batch, int32_t max_pages) {
+  const int group = hq / c->heads;
+  int64_t need = tokens * c->heads * score_row(max_pages) * 4;
+  const Plan pd = plan_dense(c->heads, c->page, c->d, tokens, batch, group, max_pages);
+  const Plan ps = plan_sel(c->heads, c->page, c->d, tokens, group, GMM_KV_MAX_KEEP);
+  const int64_t a = part_bytes(tokens, hq, c->d, pd.splits);
+  const int64_t b = part_bytes(tokens, hq, c->d, ps.splits);
+  if (a > need) need = a;
+  if (b > need) need = b;
+  return cdiv(need + 256, 256) * 256;
+}
+
+int check_kv_ws(void* ws, size_t have, int64_t need) {
+  if (!ws || ((uintptr_t)ws & 255) || (int64_t)have < need) return GMM_ERR_WORKSPACE;
+  return GMM_OK;
+}
+
+template <typename T>
+void launch_append(const AppendArgs& a, bool vec, bool inter, int64_t blocks, hipStream_t st) {
+  const dim3 grid((unsigned)blocks);
+  if (vec && inter) hipLaunchKernelGGL((k_kv_append<T, 8, true>), grid, dim3(256), 0, st, a);
+  else if (vec) hipLaunchKernelGGL((k_kv_append<T, 8, false>), grid, dim3(256), 0, st, a);
+  else if (inter) hipLaunchKernelGGL((k_kv_append<T, 1, true>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_kv_append<T, 1, false>), grid, dim3(256), 0, st, a);
+}
+
+template <typename T, int NS, int RT>
+void launch_few(const AttendArgs& a, const Plan& p, hipStream_t st) {
+  const dim3 grid((unsigned)(p.items * a.heads), (unsigned)p.splits);
+  if (a.sel)
+    hipLaunchKernelGGL((k_attend_few<T, NS, RT, true>), grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((k_attend_few<T, NS, RT, false>), grid, dim3(256), 0, st, a);
+}
+
+template <typename T, int NS>
+void launch_few_rt(const AttendArgs& a, const Plan& p, hipStream_t st) {
+  if (p.rt == 1) launch_few<T, NS, 1>(a, p, st);
+  else if (p.rt == 2) launch_few<T, NS, 2>(a, p, st);
+  else if constexpr (NS <= 4) launch_few<T, NS, 4>(a, p, st);
+}
+
+template <typename T>
+void launch_attend(const AttendArgs& a, const Plan& p, hipStream_t st) {
+  if (a.d <= 64) launch_few_rt<T, 2>(a, p, st);
+  else if (a.d <= 128) launch_few_rt<T, 4>(a, p, st);
+  else if (a.d <= 192) launch_few_rt<T, 6>(a, p, st);
+  else launch_few_rt<T, 8>(a, p, st);
+  if (a.splits > 1) {
+    const dim3 grid((unsigned)cdiv(a.tokens * a.hq, 4));
+    if (a.sel)
+      hipLaunchKernelGGL((k_attend_join<T, true>), grid, dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((k_attend_join<T, false>), grid, dim3(256), 0, st, a);
+  }
+}
+
+template <typename T>
+int launch_rope(const void* x, int64_t xt, int64_t xh, void* out, int64_t ot, int64_t oh,
+                int64_t tokens, int heads, int d, const int32_t* pos, const RopeShape& r, bool inter,
+                hipStream_t st) {
+  const bool vec = r.rot % 16 == 0 && d % 16 == 0 && aligned16(x) && aligned16(out) &&
+                   aligned16(r.table) && (xt | xh | ot | oh) % 8 == 0;
+  const int w = vec ? 8 : 1;
+  const int64_t per = cdiv((int64_t)heads * cdiv(d, 2 * w), 256);
+  if (per > 65535 || tokens * per > kMaxBlocks) return GMM_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)tokens, (unsigned)per);
+  const auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, (const T*)x, xt, xh, (T*)out, ot, oh,
+                       heads, d, pos, r);
+  };
+  if (vec && inter) run(k_rope<T, 8, true>);
+  else if (vec) run(k_rope<T, 8, false>);
+  else if (inter) run(k_rope<T, 1, true>);
+  else run(k_rope<T, 1, false>);
+  return launch_status();
+}
+
+}  // namespace
+
+extern "C" {
+
+int gmm_rope_table(const double* freq, int32_t half, double scale, int32_t positions,
+                   float* table, hipStream_t stream) {
+  if (!freq || !table || half < 1 || positions < 1 || !isfinite(scale)) return GMM_ERR_INVALID_ARG;
+  const int64_t blocks = cdiv((int64_t)positions * half, 256);
+  if (half > GMM_MAX_D / 2 || blocks > kMaxBlocks) return GMM_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL(k_rope_table, dim3((unsigned)blocks), dim3(256), 0, stream, freq, half,
+                     scale, (int64_t)positions, table);
+  return launch_status();
+}
+
+int gmm_rope(const void* x, int64_t x_token_stride, int64_t x_head_stride, void* out,
+             int64_t out_token_stride, int64_t out_head_stride, int64_t tokens, int32_t heads,
+             int32_t d, int32_t dtype, const int32_t* pos, const float* table, int32_t positions,
+             int32_t rot, int32_t interleaved, int32_t inverse, hipStream_t stream) {
+  if (tokens < 0 || heads < 1 || d < 2 || positions < 1 || rot < 2 || rot > d || rot % 2)
+    return GMM_ERR_INVALID_ARG;
+  if (dtype != GMM_F32 && dtype != GMM_BF16 && dtype != GMM_F16) return GMM_ERR_UNSUPPORTED;
+  if (d > GMM_MAX_D || heads > GMM_KV_MAX_HEADS || tokens > (1 << 24)) return GMM_ERR_UNSUPPORTED;
+  if (tokens == 0) return GMM_OK;
+  if (!x || !out || !pos || !table) return GMM_ERR_INVALID_ARG;
+  const RopeShape r{table, positions, rot, inverse != 0};
+  if (dtype == GMM_F32)
+    return launch_rope<float>(x, x_token_stride, x_head_stride, out, out_token_stride,
+                              out_head_stride, tokens, heads, d, pos, r, interleaved != 0,
+                               stream);
+  if (dtype == GMM_BF16)
+    return launch_rope<__bf16>(x, x_token_stride, x_head_stride, out, out_token_stride,
+                               out_head_stride, tokens, heads, d, pos, r, interleaved != 0,
+                               stream);
+  return launch_rope<_Float16>(x, x_token_stride, x_head_stride, out, out_token_stride,
+                               out_head_stride, tokens, heads, d, pos, r, interleaved != 0,
+                               stream);
+}
+
+int gmm_kv_append(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t tokens,
+                  const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
+                  int64_t v_token_stride, int64_t v_head_stride, const int32_t* pos,
+                  const float* table, int32_t positions, int32_t rot, int32_t interleaved,
+                  const void* q, int64_t q_token_stride, int64_t q_head_stride, void* q_out,
+                  int64_t qo_token_stride, int64_t qo_head_stride, int32_t hq,
+                  hipStream_t stream) {
+  int rc = check_cache(cache);
+  if (rc != GMM_OK) return rc;
+  AppendArgs a{};
+  rc = check_seqs(cache, seqs, tokens, &a.s);
+  if (rc != GMM_OK) return rc;
+  const int d = cache->d;
+  if (table && (positions < 1 || rot < 2 || rot > d || rot % 2)) return GMM_ERR_INVALID_ARG;
+  if (q) {
+    if (!table || !q_out) return GMM_ERR_INVALID_ARG;
+    rc = check_heads(cache, hq);
+    if (rc != GMM_OK) return rc;
+  }
+  if (tokens == 0) return GMM_OK;
+  if (!k || !v) return GMM_ERR_INVALID_ARG;
+  a.ck = cache->k;
+  a.cv = cache->v;
+  a.box = cache->box;
+  a.box_scale = cache->box_scale;
+  a.heads = cache->heads;
+  a.page = cache->page;
+  a.d = d;
+  a.k = k;
+  a.kt = k_token_stride;
+  a.kh = k_head_stride;
+  a.v = v;
+  a.vt = v_token_stride;
+  a.vh = v_head_stride;
+  a.v_vec = aligned16(v) && (v_token_stride | v_head_stride) % 8 == 0;
+  a.pos = pos;
+  a.rope = RopeShape{table, table ? positions : 0, table ? rot : 0, 0};
+  a.q = q;
+  a.qt = q_token_stride;
+  a.qh = q_head_stride;
+  a.qo = q_out;
+  a.qot = qo_token_stride;
+  a.qoh = qo_head_stride;
+  a.hq = q ? hq : 0;
+  // 16-byte accesses where the rotated width, strides and addresses allow them, else single
+  // pairs
+  const bool vec = a.rope.rot % 16 == 0 && aligned16(k) &&
+                   (k_token_stride | k_head_stride) % 8 == 0 && aligned16(table) &&
+                   (!q || (aligned16(q) && aligned16(q_out) &&
+                           (q_token_stride | q_head_stride | qo_token_stride | qo_head_stride) % 8 == 0));
+  const int w = vec ? 8 : 1;
+  a.q_blocks = q ? (int)cdiv((int64_t)hq * (d / (2 * w)), 256) : 0;
+  a.page_blocks = (tokens / cache->page + 2 * (int64_t)seqs->batch) * cache->heads;
+  const int64_t blocks = a.page_blocks + tokens * a.q_blocks;
+  if (blocks > kMaxBlocks) return GMM_ERR_UNSUPPORTED;
+  const bool inter = table && interleaved;
+  if (cache->dtype == GMM_BF16) launch_append<__bf16>(a, vec, inter, blocks, stream);
+  else launch_append<_Float16>(a, vec, inter, blocks, stream);
+  return launch_status();
+}
+
+size_t gmm_kv_workspace_bytes(const gmm_kv_cache* cache, int64_t tokens, int32_t hq,
+                              int32_t batch, int32_t max_pages) {
+  if (check_cache(cache) != GMM_OK || check_heads(cache, hq) != GMM_OK) return 0;
+  if (tokens < 0 || tokens > (1 << 24) || batch < 1 || batch > (1 << 20) || max_pages < 1 ||
+      (int64_t)max_pages * cache->page > INT32_MAX)
+    return 0;
+  return (size_t)ws_need(cache, tokens, hq, batch, max_pages);
+}
+
+int gmm_kv_select(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t tokens,
+                  const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t hq,
+                  int32_t m, int32_t keep_first, int32_t keep_last, int32_t* idx, void* ws,
+                  size_t ws_bytes, hipStream_t stream) {
+  int rc = check_cache(cache);
+  if (rc != GMM_OK) return rc;
+  SelectArgs a{};
+  rc = check_seqs(cache, seqs, tokens, &a.s);
+  if (rc != GMM_OK) return rc;
+  rc = check_heads(cache, hq);
+  if (rc != GMM_OK) return rc;
+  if (!cache->box || m < 1 || keep_first < 0 || keep_last < 1) return GMM_ERR_INVALID_ARG;
+  if (m > GMM_KV_MAX_KEEP) return GMM_ERR_UNSUPPORTED;
+  if ((int64_t)keep_first + keep_last > m) return GMM_ERR_INVALID_ARG;
+  if (tokens == 0) return GMM_OK;
+  if (!q || !idx) return GMM_ERR_INVALID_ARG;
+  rc = check_kv_ws(ws, ws_bytes, ws_need(cache, tokens, hq, seqs->batch, seqs->max_pages));
+  if (rc != GMM_OK) return rc;
+  a.box = cache->box;
+  a.box_scale = cache->box_scale;
+  a.q = q;
+  a.qt = q_token_stride;
+  a.qh = q_head_stride;
+  a.heads = cache->heads;
+  a.group = hq / cache->heads;
+  a.d = cache->d;
+  a.col_shift = a.group >= 16 ? 4 : log2i(a.group);
+  a.col_tiles = (int)cdiv(a.group, 16);
+  a.score = (float*)ws;
+  a.row = score_row(seqs->max_pages);
+  const int per = 16 >> a.col_shift;
+  const int64_t items = tokens / per + seqs->batch;
+  const int64_t tiles = cdiv(seqs->max_pages, 16);
+  a.chunk_tiles = 4;
+  a.parts = (int)cdiv(tiles, 4 * a.chunk_tiles);
+  const int64_t blocks = a.parts * items * cache->heads;
+  if (blocks > kMaxBlocks || tokens * cache->heads > kMaxBlocks) return GMM_ERR_UNSUPPORTED;
+  const size_t lds = (size_t)a.col_tiles * 16 * (2 * a.d + 4);
+  const dim3 grid((unsigned)blocks);
+  if (cache->dtype == GMM_BF16)
+    hipLaunchKernelGGL((k_select_score<__bf16>), grid, dim3(256), lds, stream, a);
+  else
+    hipLaunchKernelGGL((k_select_score<_Float16>), grid, dim3(256), lds, stream, a);
+  hipLaunchKernelGGL(k_select_top, dim3((unsigned)(tokens * cache->heads)), dim3(256), 0, stream,
+                     a.s, a.score, a.row, a.heads, m, keep_first, keep_last, idx);
+  return launch_status();
+}
+
+int gmm_kv_attend(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t tokens,
+                  const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t hq,
+                  float scale, int32_t window, const int32_t* sel, int32_t m, void* out,
+                  float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+  int rc = check_cache(cache);
+  if (rc != GMM_OK) return rc;
+  AttendArgs a{};
+  rc = check_seqs(cache, seqs, tokens, &a.s);
+  if (rc != GMM_OK) return rc;
+  rc = check_heads(cache, hq);
+  if (rc != GMM_OK) return rc;
+  if (!isfinite(scale) || window < 0 || (sel ? m < 1 || window != 0 : m != 0))
+    return GMM_ERR_INVALID_ARG;
+  if (m > GMM_KV_MAX_KEEP) return GMM_ERR_UNSUPPORTED;
+  if (tokens == 0) return GMM_OK;
+  if (!q || !out || ((uintptr_t)out & 7)) return GMM_ERR_INVALID_ARG;
+  rc = check_kv_ws(ws, ws_bytes, ws_need(cache, tokens, hq, seqs->batch, seqs->max_pages));
+  if (rc != GMM_OK) return rc;
+  a.k = cache->k;
+  a.v = cache->v;
+  a.heads = cache->heads;
+  a.group = hq / cache->heads;
+  a.d = cache->d;
+  a.q = q;
+  a.qt = q_token_stride;
+  a.qh = q_head_stride;
+  a.q_vec = aligned16(q) && (q_token_stride | q_head_stride) % 8 == 0;
+  a.scale2 = scale * kLog2e;
+  a.window = window;
+  a.sel = sel;
+  a.m = m;
+  a.out = out;
+  a.lse = lse;
+  a.hq = hq;
+  a.tokens = tokens;
+  const Plan p = sel ? plan_sel(a.heads, cache->page, a.d, tokens, a.group, m)
+                     : plan_dense(a.heads, cache->page, a.d, tokens, seqs->batch, a.group,
+                                  seqs->max_pages);
+  a.chunk = p.chunk;
+  a.splits = p.splits;
+  a.tiles_token = p.tiles_token;
+  a.part_o = (float*)ws;
+  a.part_ml = a.part_o + (int64_t)p.splits * tokens * hq * a.d;
+  if (p.items * a.heads * p.splits > kMaxBlocks || p.splits > 65535 ||
+      cdiv(tokens * hq, 4) > kMaxBlocks)
+    return GMM_ERR_UNSUPPORTED;
+  if (cache->dtype == GMM_BF16) launch_attend<__bf16>(a, p, stream);
+  else launch_attend<_Float16>(a, p, stream);
+  return launch_status();
+}
+
+}  // extern "C"
