@@ -24,6 +24,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "flashgmm.h"
 
 namespace {
@@ -52,6 +54,15 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
 }
 __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// 32x32x16: lane l holds A[l % 32][8 (l / 32) + e] and B[8 (l / 32) + e][l % 32], e = 0..7, and
+// D[8 (i / 4) + 4 (l / 32) + i % 4][l % 32], i = 0..15
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma32(f16x8 a, f16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
@@ -919,6 +930,339 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
   }
 }
 
+// Many query rows (4 waves x 32 CT) against a range of keys.  The steps of 32 keys pass through
+// LDS, where the four waves share them; a wave holds its queries (B operands) and results in
+// registers, so that one operand read from LDS serves CT matrix instructions.
+//
+// A step's three parts, scores S^T = K Q^T, weights, and O^T += V^T P^T, are those of three
+// successive steps in one turn of the loop: the scores of step p + 1 and the products of step
+// p - 1 occupy the matrix unit while the vector unit forms the weights of step p.  Keys are
+// therefore needed two turns before values; each has two LDS slots, filled from registers that
+// were loaded a turn earlier.
+//
+// The running maximum is only moved (and the results rescaled) when a score exceeds it by 2^8:
+// a common factor cancels in the end, and weights up to 2^8 are as exact as those up to 1.
+//
+// Rows of the score tile are keys in the order that makes its accumulator the B operand of the
+// second product: row r is key r with bits 2 and 3 exchanged.
+template <typename T, int ND, int CT>
+__global__ __launch_bounds__(256) void k_attend_tile(AttendArgs a) {
+  typedef typename Vec8<T>::type V8;
+  constexpr int CD = 4 * ND;                      // 16-byte chunks of a key's row
+  constexpr int CK = (CD + 7) / 8 * 8;            // and the LDS row's
+  constexpr int NS = 2 * ND;                      // 16-dimension steps of the scores
+  constexpr int KCH = 32 * CD;                    // chunks of a step's keys, and of its values
+  constexpr int PER = (KCH + 255) / 256;
+  constexpr int R = 128 * CT;
+  __shared__ V8 ks[2][32 * CK];
+  __shared__ V8 vs[2][KCH];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c32 = lane & 31, half = lane >> 5;
+  const int head = blockIdx.x % a.heads;
+  // later tiles see more keys: they start first
+  const int64_t item = (int64_t)(gridDim.x / a.heads) - 1 - blockIdx.x / a.heads;
+  const int split = blockIdx.y;
+  const int P = 1 << a.s.page_shift, d = a.d, G = a.group;
+
+  const int b = find_seq(a.s, item, G, R, 1);
+  const int row0 = a.s.cu[b], n = a.s.cu[b + 1] - row0, total = a.s.total[b];
+  const int64_t rr0 = (item - first_item(a.s, b, G, R, 1)) * R;
+  if (rr0 >= (int64_t)n * G) return;
+  const int r0 = (int)rr0;
+  const int rows = (int)min((int64_t)R, (int64_t)n * G - rr0);
+  const int64_t held = min((int64_t)total, (int64_t)a.s.max_pages << a.s.page_shift);
+  const int64_t khi = min(held, (int64_t)total - n + (r0 + rows - 1) / G + 1);
+  const int64_t klo = a.window > 0 ? max((int64_t)0, (int64_t)total - n + r0 / G - a.window + 1) : 0;
+  const int64_t k0 = (int64_t)split * a.chunk, k1 = k0 + a.chunk;
+  int p0 = 0, steps = 0;                          // steps of 32 keys from key 32 p0
+  if (k0 < khi && k1 > klo) {
+    p0 = (int)(max(k0, klo) >> 5);
+    steps = (int)((min(k1, khi) + 31) >> 5) - p0;
+  } else if (a.splits > 1 || khi > klo) {
+    return;
+  }
+
+  // queries, slots of this wave's rows
+  V8 qf[CT][NS];
+  int lim[CT], low[CT];
+  const int wr0 = wave * 32 * CT;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int r = wr0 + ct * 32 + c32;
+    const bool live = r < rows;
+    const int rr = r0 + (live ? r : 0), ti = rr / G, hh = rr - ti * G;
+    const int64_t slot = (int64_t)total - n + ti;
+    lim[ct] = live ? (int)max((int64_t)-1, min(slot, held - 1)) : -1;
+    low[ct] = a.window > 0 && live ? (int)max((int64_t)0, slot - a.window + 1) : 0;
+    const T* qr = (const T*)a.q + (int64_t)(row0 + ti) * a.qt + (int64_t)(head * G + hh) * a.qh;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const int dim = 16 * s + 8 * half;
+      V8 v = load_row8(qr + min(dim, d - 8), a.q_vec);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = dim < d ? (a.scale2 < 0.0f ? -v[e] : v[e]) : (T)0.0f;
+      qf[ct][s] = v;
+    }
+  }
+  const float sc2 = fabsf(a.scale2);
+  // steps in which every row of the wave sees every key need no mask
+  int wlim, wlow;
+  {
+    const int first = min(wr0, rows - 1), last = min(wr0 + 32 * CT, rows) - 1;
+    const int64_t s_first = (int64_t)total - n + (r0 + first) / G;
+    const int64_t s_last = (int64_t)total - n + (r0 + max(last, 0)) / G;
+    wlim = (int)max((int64_t)-1, min(s_first, held - 1));
+    wlow = a.window > 0 ? (int)max((int64_t)0, s_last - a.window + 1) : 0;
+    if (last < wr0) wlim = -1;
+  }
+
+  // where this thread's chunks of a step's keys and values come from and go to
+  const T* kc = (const T*)a.k;
+  const T* vc = (const T*)a.v;
+  int kg[PER], kl[PER], vg[PER], vl[PER], vkey[PER];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int i = min(tid + 256 * j, KCH - 1);
+    const int key = i / CD, c = i - key * CD;
+    const int row = (key & 0x13) | ((key & 4) << 1) | ((key & 8) >> 1);
+    kg[j] = key * d + min(8 * c, d - 8);
+    kl[j] = row * CK + (c ^ (row & 7));
+    const int dim = i >> 2, cv = i & 3;
+    vg[j] = min(dim, d - 1) * P + 8 * cv;
+    vl[j] = dim * 4 + (cv ^ ((dim >> 1) & 3));
+    vkey[j] = 8 * cv;
+  }
+  V8 kreg[PER], vreg[PER];
+  const auto page_of = [&](int p) {
+    const int key = (p0 + min(p, steps - 1)) << 5;
+    return phys_page(a.s, b, key >> a.s.page_shift);
+  };
+  const auto base_of = [&](int p, int phys) {     // element of the step's first key slot
+    const int key = (p0 + min(p, steps - 1)) << 5;
+    return ((int64_t)max(phys, 0) * a.heads + head) * P * d + (int64_t)(key & (P - 1));
+  };
+  const auto load_k = [&](int p, int phys) {
+    const int off = ((p0 + min(p, steps - 1)) << 5) & (P - 1);
+    const T* kp = kc + ((int64_t)max(phys, 0) * a.heads + head) * P * d + (int64_t)off * d;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) kreg[j] = load16<V8>(kp + kg[j]);
+  };
+  const auto load_v = [&](int p, int phys) {
+    const T* vp = vc + base_of(p, phys);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) vreg[j] = load16<V8>(vp + vg[j]);
+  };
+  const auto store_k = [&](int slot) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      if (KCH % 256 == 0 || tid + 256 * j < KCH) ks[slot][kl[j]] = kreg[j];
+  };
+  // `live` keys of the step exist; the others' slots may hold anything and become 0
+  const auto store_v = [&](int slot, int live) {
+    if (live < 32) {
+#pragma unroll
+      for (int j = 0; j < PER; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vreg[j][e] = vkey[j] + e < live ? vreg[j][e] : (T)0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      if (KCH % 256 == 0 || tid + 256 * j < KCH) vs[slot][vl[j]] = vreg[j];
+  };
+  const auto live_keys = [&](int p, int phys) {
+    const int64_t key = (int64_t)(p0 + p) << 5;
+    return phys < 0 || p >= steps ? 0 : (int)min((int64_t)32, khi - key);
+  };
+  const auto frag_k = [&](int slot, int s) {
+    return ks[slot][c32 * CK + ((2 * s + half) ^ (c32 & 7))];
+  };
+  const auto frag_v = [&](int slot, int dt, int u) {
+    return vs[slot][(32 * dt + c32) * 4 + ((2 * u + half) ^ ((c32 >> 1) & 3))];
+  };
+
+  f32x16 o[CT][ND], sa[CT], sb[CT];
+  V8 pw[CT][2];
+  float mx[CT], sum[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    mx[ct] = -INFINITY;
+    sum[ct] = 0.0f;
+    pw[ct][0] = pw[ct][1] = V8((T)0.0f);
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) o[ct][dt] = f32x16(0.0f);
+  }
+
+  if (steps > 0) {
+    int ph0 = page_of(0), ph1 = page_of(1), ph2 = page_of(2), ph3 = page_of(3);
+    load_k(0, ph0);
+    load_v(0, ph0);
+    store_k(0);
+    load_k(1, ph1);
+    store_k(1);
+    // the values of "step -1" are read before any are written: zeros
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      if (KCH % 256 == 0 || tid + 256 * j < KCH) vs[1][vl[j]] = V8((T)0.0f);
+    load_k(2, ph2);
+    __syncthreads();
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) sa[ct] = f32x16(0.0f);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const V8 kf = frag_k(0, s);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) sa[ct] = mfma32(kf, qf[ct][s], sa[ct]);
+    }
+    __syncthreads();
+
+    // one turn: sc the scores of step p, sn those of step p + 1, cur = p % 2
+    const auto turn = [&](int p, auto slot, f32x16(&sc)[CT], f32x16(&sn)[CT]) {
+      constexpr int cur = decltype(slot)::value, nxt = cur ^ 1;
+      // slot cur: keys of step p (used) become those of p + 2, values of p - 2 those of p
+      store_k(cur);
+      const int live = live_keys(p, ph0);
+      store_v(cur, live);
+      load_k(p + 3, ph3);
+      load_v(p + 1, ph1);
+      ph0 = ph1;
+      ph1 = ph2;
+      ph2 = ph3;
+      ph3 = page_of(p + 4);
+
+      const int key0 = (p0 + p) << 5;
+      if (live < 32 || key0 + 31 > wlim || key0 < wlow) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int kk = 16 * (i >> 3) + 8 * half + (i & 7);
+            const bool see = kk < live && key0 + kk <= lim[ct] && key0 + kk >= low[ct];
+            sc[ct][i] = see ? sc[ct][i] : -INFINITY;
+          }
+      }
+      float top[CT];
+      bool grow = false;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        float m = sc[ct][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) m = fmaxf(m, sc[ct][i]);
+        top[ct] = m * sc2;
+        grow |= top[ct] > mx[ct] + 8.0f;
+      }
+      if (__ballot(grow) != 0) {
+        // the products still open are at the old maximum: close them, then move it
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int dt = 0; dt < ND; ++dt) {
+            const V8 vf = frag_v(nxt, dt, u);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) o[ct][dt] = mfma32(vf, pw[ct][u], o[ct][dt]);
+          }
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          const float m = fmaxf(mx[ct], fmaxf(top[ct], __shfl_xor(top[ct], 32)));
+          const float f = m == -INFINITY ? 1.0f : exp2_fast(mx[ct] - m);
+          mx[ct] = m;
+          sum[ct] *= f;
+          pw[ct][0] = pw[ct][1] = V8((T)0.0f);
+#pragma unroll
+          for (int dt = 0; dt < ND; ++dt) o[ct][dt] *= f;
+        }
+      }
+
+      V8 pn[CT][2];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) sn[ct] = f32x16(0.0f);
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const V8 kf = frag_k(nxt, s);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) sn[ct] = mfma32(kf, qf[ct][s], sn[ct]);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) {
+          const V8 vf = frag_v(nxt, dt, u);
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) o[ct][dt] = mfma32(vf, pw[ct][u], o[ct][dt]);
+        }
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        const float base = mx[ct] == -INFINITY ? 0.0f : mx[ct];
+        float z = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float e = exp2_fast(__fmaf_rn(sc[ct][i], sc2, -base));
+          z += e;
+          pn[ct][i >> 3][i & 7] = (T)e;      // rounded for the matrix product
+        }
+        sum[ct] += z;
+      }
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        pw[ct][0] = pn[ct][0];
+        pw[ct][1] = pn[ct][1];
+      }
+      __syncthreads();
+    };
+    // an odd count ends in a step without keys
+    for (int p = 0; p < steps; p += 2) {
+      turn(p, std::integral_constant<int, 0>{}, sa, sb);
+      turn(p + 1, std::integral_constant<int, 1>{}, sb, sa);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) {
+        const V8 vf = frag_v(1, dt, u);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) o[ct][dt] = mfma32(vf, pw[ct][u], o[ct][dt]);
+      }
+  }
+
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const float z = sum[ct] + __shfl_xor(sum[ct], 32);
+    const int r = wr0 + ct * 32 + c32;
+    if (r >= rows) continue;
+    const int rr = r0 + r, ti = rr / G, hh = rr - ti * G;
+    const int64_t orow = (int64_t)(row0 + ti) * a.hq + head * G + hh;
+    const int64_t pr = (int64_t)split * a.tokens * a.hq + orow;
+    const float inv = z > 0.0f ? 1.0f / z : 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const int dim = 32 * dt + 8 * i4 + 4 * half;
+        if (dim >= d) continue;
+        if (a.splits == 1) {
+          alignas(8) T w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = (T)(z > 0.0f ? o[ct][dt][4 * i4 + i] * inv : z);
+          *reinterpret_cast<uint2*>((T*)a.out + orow * d + dim) = *reinterpret_cast<uint2*>(w);
+        } else {
+          f32x4 v;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = o[ct][dt][4 * i4 + i];
+          *reinterpret_cast<f32x4*>(a.part_o + pr * d + dim) = v;
+        }
+      }
+    if (half == 0) {
+      if (a.splits == 1) {
+        if (a.lse)
+          a.lse[orow] = z > 0.0f ? (mx[ct] + log2_fast(z)) * kLn2 : (z == 0.0f ? -INFINITY : z);
+      } else {
+        a.part_ml[pr * 2] = mx[ct];
+        a.part_ml[pr * 2 + 1] = z;
+      }
+    }
+  }
+}
+
 // Joins the partial results of the key ranges, in their order: a wave a row.
 template <typename T, bool SEL>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
@@ -1009,7 +1353,8 @@ int check_heads(const gmm_kv_cache* c, int32_t hq) {
 
 // Row tiles and key ranges of an attention call.
 struct Plan {
-  int rt;                  // k_attend_few: 16 rt rows a tile
+  int rt;                  // k_attend_few: 16 rt rows a tile, 0 if it is k_attend_tile
+  int ct;                  // k_attend_tile: 128 ct rows a tile
   int64_t items;           // row tiles of a head
   int tiles_token;
   int chunk, splits;
@@ -1018,28 +1363,39 @@ struct Plan {
 // Workgroups wanted: 256 CUs hold 2 each; four rounds of them even out ragged lengths.
 constexpr int64_t kWantGroups = 2048;
 constexpr int kMaxSplits = 1024;
+constexpr int kCUs = 256;
 
-// 64 rows keep 64 registers of queries, results and keys each above 128 dimensions: too many
+// rows of a tile above 64 are shared through LDS (k_attend_tile)
 int few_rows(int64_t rows, int d) { return rows <= 16 ? 1 : rows <= 32 || d > 128 ? 2 : 4; }
 
 Plan plan_dense(int heads, int page, int d, int64_t tokens, int32_t batch, int group,
                 int32_t max_pages) {
-  Plan p;
-  p.rt = few_rows(cdiv(tokens, batch) * group, d);
-  p.items = tokens * group / (16 * p.rt) + batch;
-  p.tiles_token = 0;
+  Plan p{};
   const int64_t keys = (int64_t)max_pages * page;
-  int64_t want = cdiv(kWantGroups, p.items * heads);
+  const int64_t rows = cdiv(tokens, batch) * group;
+  int64_t want, unit;
+  if (rows > 64) {
+    p.ct = rows > 128 && d <= 128 ? 2 : 1;
+    const int64_t tiles = tokens * group / (128 * p.ct);
+    p.items = tiles + batch;
+    // one workgroup a CU; keys are split where there are fewer row tiles than that
+    want = cdiv(kCUs, (tiles > 0 ? tiles : 1) * heads);
+    unit = 512;
+  } else {
+    p.rt = few_rows(rows, d);
+    p.items = tokens * group / (16 * p.rt) + batch;
+    want = cdiv(kWantGroups, p.items * heads);
+    unit = 128;                      // a step of 32 keys for every wave
+  }
   if (want > kMaxSplits) want = kMaxSplits;
-  // at least 128 keys: a step of 32 for every wave
-  int64_t chunk = cdiv(cdiv(keys, want), 128) * 128;
+  const int64_t chunk = cdiv(cdiv(keys, want), unit) * unit;
   p.chunk = (int)chunk;
   p.splits = (int)cdiv(keys, chunk);
   return p;
 }
 
 Plan plan_sel(int heads, int page, int d, int64_t tokens, int group, int32_t m) {
-  Plan p;
+  Plan p{};
   p.rt = few_rows(group, d);
   p.tiles_token = (int)cdiv(group, 16 * p.rt);
   p.items = tokens * p.tiles_token;
@@ -1101,9 +1457,27 @@ void launch_few_rt(const AttendArgs& a, const Plan& p, hipStream_t st) {
   else if constexpr (NS <= 4) launch_few<T, NS, 4>(a, p, st);
 }
 
+template <typename T, int ND>
+void launch_tile(const AttendArgs& a, const Plan& p, hipStream_t st) {
+  const dim3 grid((unsigned)(p.items * a.heads), (unsigned)p.splits);
+  if constexpr (ND <= 4) {
+    if (p.ct == 2) {
+      hipLaunchKernelGGL((k_attend_tile<T, ND, 2>), grid, dim3(256), 0, st, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((k_attend_tile<T, ND, 1>), grid, dim3(256), 0, st, a);
+}
+
 template <typename T>
 void launch_attend(const AttendArgs& a, const Plan& p, hipStream_t st) {
-  if (a.d <= 64) launch_few_rt<T, 2>(a, p, st);
+  if (p.ct > 0) {
+    if (a.d <= 64) launch_tile<T, 2>(a, p, st);
+    else if (a.d <= 96) launch_tile<T, 3>(a, p, st);
+    else if (a.d <= 128) launch_tile<T, 4>(a, p, st);
+    else if (a.d <= 192) launch_tile<T, 6>(a, p, st);
+    else launch_tile<T, 8>(a, p, st);
+  } else if (a.d <= 64) launch_few_rt<T, 2>(a, p, st);
   else if (a.d <= 128) launch_few_rt<T, 4>(a, p, st);
   else if (a.d <= 192) launch_few_rt<T, 6>(a, p, st);
   else launch_few_rt<T, 8>(a, p, st);
