@@ -89,10 +89,14 @@ __device__ __forceinline__ typename Vec8<T>::type load_row8(const T* p, int vec)
 __host__ __device__ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // ---------------------------------------------------------------- sequences
+// The tables are read in the constant address space: nothing writes them while a kernel runs,
+// and loads at wave-uniform addresses go through the scalar cache.
+typedef const __attribute__((address_space(4))) int32_t* Table;
+
 struct Seqs {
-  const int32_t* cu;
-  const int32_t* total;
-  const int32_t* pages;
+  Table cu;
+  Table total;
+  Table pages;
   int64_t stride;
   int batch, max_pages;
   int page_shift;   // log2 of the page size
@@ -945,15 +949,16 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
 //
 // Rows of the score tile are keys in the order that makes its accumulator the B operand of the
 // second product: row r is key r with bits 2 and 3 exchanged.
-template <typename T, int ND, int CT>
-__global__ __launch_bounds__(256) void k_attend_tile(AttendArgs a) {
+template <typename T, int ND, int CT, int NW>
+__global__ __launch_bounds__(64 * NW, ND * CT <= 4 ? 2 : 1) void k_attend_tile(AttendArgs a) {
   typedef typename Vec8<T>::type V8;
   constexpr int CD = 4 * ND;                      // 16-byte chunks of a key's row
   constexpr int CK = (CD + 7) / 8 * 8;            // and the LDS row's
   constexpr int NS = 2 * ND;                      // 16-dimension steps of the scores
   constexpr int KCH = 32 * CD;                    // chunks of a step's keys, and of its values
-  constexpr int PER = (KCH + 255) / 256;
-  constexpr int R = 128 * CT;
+  constexpr int NT = 64 * NW;
+  constexpr int PER = (KCH + NT - 1) / NT;
+  constexpr int R = 32 * CT * NW;
   __shared__ V8 ks[2][32 * CK];
   __shared__ V8 vs[2][KCH];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -1023,7 +1028,7 @@ __global__ __launch_bounds__(256) void k_attend_tile(AttendArgs a) {
   int kg[PER], kl[PER], vg[PER], vl[PER], vkey[PER];
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
-    const int i = min(tid + 256 * j, KCH - 1);
+    const int i = min(tid + NT * j, KCH - 1);
     const int key = i / CD, c = i - key * CD;
     const int row = (key & 0x13) | ((key & 4) << 1) | ((key & 8) >> 1);
     kg[j] = key * d + min(8 * c, d - 8);
@@ -1056,7 +1061,7 @@ __global__ __launch_bounds__(256) void k_attend_tile(AttendArgs a) {
   const auto store_k = [&](int slot) {
 #pragma unroll
     for (int j = 0; j < PER; ++j)
-      if (KCH % 256 == 0 || tid + 256 * j < KCH) ks[slot][kl[j]] = kreg[j];
+      if (KCH % NT == 0 || tid + NT * j < KCH) ks[slot][kl[j]] = kreg[j];
   };
   // `live` keys of the step exist; the others' slots may hold anything and become 0
   const auto store_v = [&](int slot, int live) {
@@ -1068,7 +1073,7 @@ __global__ __launch_bounds__(256) void k_attend_tile(AttendArgs a) {
     }
 #pragma unroll
     for (int j = 0; j < PER; ++j)
-      if (KCH % 256 == 0 || tid + 256 * j < KCH) vs[slot][vl[j]] = vreg[j];
+      if (KCH % NT == 0 || tid + NT * j < KCH) vs[slot][vl[j]] = vreg[j];
   };
   const auto live_keys = [&](int p, int phys) {
     const int64_t key = (int64_t)(p0 + p) << 5;
@@ -1083,11 +1088,13 @@ __global__ __launch_bounds__(256) void k_attend_tile(AttendArgs a) {
 
   f32x16 o[CT][ND], sa[CT], sb[CT];
   V8 pw[CT][2];
-  float mx[CT], sum[CT];
+  float mx[CT], sum[CT], f[CT];
+  bool moved = false;
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
     mx[ct] = -INFINITY;
     sum[ct] = 0.0f;
+    f[ct] = 1.0f;
     pw[ct][0] = pw[ct][1] = V8((T)0.0f);
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) o[ct][dt] = f32x16(0.0f);
@@ -1103,7 +1110,7 @@ __global__ __launch_bounds__(256) void k_attend_tile(AttendArgs a) {
     // the values of "step -1" are read before any are written: zeros
 #pragma unroll
     for (int j = 0; j < PER; ++j)
-      if (KCH % 256 == 0 || tid + 256 * j < KCH) vs[1][vl[j]] = V8((T)0.0f);
+      if (KCH % NT == 0 || tid + NT * j < KCH) vs[1][vl[j]] = V8((T)0.0f);
     load_k(2, ph2);
     __syncthreads();
 #pragma unroll
@@ -1151,25 +1158,21 @@ __global__ __launch_bounds__(256) void k_attend_tile(AttendArgs a) {
         top[ct] = m * sc2;
         grow |= top[ct] > mx[ct] + 8.0f;
       }
-      if (__ballot(grow) != 0) {
-        // the products still open are at the old maximum: close them, then move it
+      // a maximum moved in turn p - 1: by now the products with the weights before it are in
+      if (moved) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-          for (int dt = 0; dt < ND; ++dt) {
-            const V8 vf = frag_v(nxt, dt, u);
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) o[ct][dt] = mfma32(vf, pw[ct][u], o[ct][dt]);
-          }
+          for (int dt = 0; dt < ND; ++dt) o[ct][dt] *= f[ct];
+      }
+      moved = __ballot(grow) != 0;
+      if (moved) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
           const float m = fmaxf(mx[ct], fmaxf(top[ct], __shfl_xor(top[ct], 32)));
-          const float f = m == -INFINITY ? 1.0f : exp2_fast(mx[ct] - m);
+          f[ct] = m == -INFINITY ? 1.0f : exp2_fast(mx[ct] - m);
           mx[ct] = m;
-          sum[ct] *= f;
-          pw[ct][0] = pw[ct][1] = V8((T)0.0f);
-#pragma unroll
-          for (int dt = 0; dt < ND; ++dt) o[ct][dt] *= f;
+          sum[ct] *= f[ct];
         }
       }
 
@@ -1207,12 +1210,21 @@ __global__ __launch_bounds__(256) void k_attend_tile(AttendArgs a) {
         pw[ct][0] = pn[ct][0];
         pw[ct][1] = pn[ct][1];
       }
+      // the weights are formed here, between the products, and not where they are next used
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) asm volatile("" : "+v"(pw[ct][0]), "+v"(pw[ct][1]));
       __syncthreads();
     };
     // an odd count ends in a step without keys
     for (int p = 0; p < steps; p += 2) {
       turn(p, std::integral_constant<int, 0>{}, sa, sb);
       turn(p + 1, std::integral_constant<int, 1>{}, sb, sa);
+    }
+    if (moved) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) o[ct][dt] *= f[ct];
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -1340,7 +1352,8 @@ int check_seqs(const gmm_kv_cache* c, const gmm_kv_batch* s, int64_t tokens, Seq
   // slots are 32-bit; rows (tokens x heads) too
   if ((int64_t)s->max_pages * c->page > INT32_MAX || tokens > (1 << 24) || s->batch > (1 << 20))
     return GMM_ERR_UNSUPPORTED;
-  *o = Seqs{s->cu, s->total, s->pages, s->pages_stride, s->batch, s->max_pages, log2i(c->page),
+  *o = Seqs{(Table)(uintptr_t)s->cu, (Table)(uintptr_t)s->total, (Table)(uintptr_t)s->pages,
+            s->pages_stride, s->batch, s->max_pages, log2i(c->page),
             c->pages};
   return GMM_OK;
 }
@@ -1354,7 +1367,7 @@ int check_heads(const gmm_kv_cache* c, int32_t hq) {
 // Row tiles and key ranges of an attention call.
 struct Plan {
   int rt;                  // k_attend_few: 16 rt rows a tile, 0 if it is k_attend_tile
-  int ct;                  // k_attend_tile: 128 ct rows a tile
+  int rows;                // k_attend_tile: rows of a tile
   int64_t items;           // row tiles of a head
   int tiles_token;
   int chunk, splits;
@@ -1375,8 +1388,9 @@ Plan plan_dense(int heads, int page, int d, int64_t tokens, int32_t batch, int g
   const int64_t rows = cdiv(tokens, batch) * group;
   int64_t want, unit;
   if (rows > 64) {
-    p.ct = rows > 128 && d <= 128 ? 2 : 1;
-    const int64_t tiles = tokens * group / (128 * p.ct);
+    const int least = d <= 64 ? 256 : 128;
+    p.rows = rows > least && d <= 128 ? 2 * least : least;
+    const int64_t tiles = tokens * group / p.rows;
     p.items = tiles + batch;
     // one workgroup a CU; keys are split where there are fewer row tiles than that
     want = cdiv(kCUs, (tiles > 0 ? tiles : 1) * heads);
@@ -1459,19 +1473,20 @@ void launch_few_rt(const AttendArgs& a, const Plan& p, hipStream_t st) {
 
 template <typename T, int ND>
 void launch_tile(const AttendArgs& a, const Plan& p, hipStream_t st) {
+  constexpr int CT = ND <= 2 ? 2 : 1;
   const dim3 grid((unsigned)(p.items * a.heads), (unsigned)p.splits);
   if constexpr (ND <= 4) {
-    if (p.ct == 2) {
-      hipLaunchKernelGGL((k_attend_tile<T, ND, 2>), grid, dim3(256), 0, st, a);
+    if (p.rows == 256 * CT) {
+      hipLaunchKernelGGL((k_attend_tile<T, ND, CT, 8>), grid, dim3(512), 0, st, a);
       return;
     }
   }
-  hipLaunchKernelGGL((k_attend_tile<T, ND, 1>), grid, dim3(256), 0, st, a);
+  hipLaunchKernelGGL((k_attend_tile<T, ND, CT, 4>), grid, dim3(256), 0, st, a);
 }
 
 template <typename T>
 void launch_attend(const AttendArgs& a, const Plan& p, hipStream_t st) {
-  if (p.ct > 0) {
+  if (p.rows > 0) {
     if (a.d <= 64) launch_tile<T, 2>(a, p, st);
     else if (a.d <= 96) launch_tile<T, 3>(a, p, st);
     else if (a.d <= 128) launch_tile<T, 4>(a, p, st);
