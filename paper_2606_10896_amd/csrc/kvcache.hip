@@ -934,33 +934,41 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
   }
 }
 
-// Many query rows (4 waves x 32 CT) against a range of keys.  The steps of 32 keys pass through
-// LDS, where the four waves share them; a wave holds its queries (B operands) and results in
-// registers, so that one operand read from LDS serves CT matrix instructions.
+// Many query rows (NW waves x 32) against a range of keys.  Steps of 64 keys (32 with four waves)
+// pass through LDS, where the waves share them; a wave holds its queries (B operands) and results
+// in registers.
 //
-// A step's three parts, scores S^T = K Q^T, weights, and O^T += V^T P^T, are those of three
-// successive steps in one turn of the loop: the scores of step p + 1 and the products of step
-// p - 1 occupy the matrix unit while the vector unit forms the weights of step p.  Keys are
-// therefore needed two turns before values; each has two LDS slots, filled from registers that
-// were loaded a turn earlier.
+// A turn of the loop has a matrix part, the products of step p - 1 and the scores of step p, and
+// a vector part, the weights of a step; between them the operands of the step after are passed
+// on.  Eight waves are two on every SIMD, one of either half of the workgroup: the first half
+// runs matrix(p), vector(p), the second half vector(p - 1), matrix(p), so that one wave's matrix
+// part meets the other's vector part.  (Four waves leave that to chance: two workgroups share a
+// CU.)
+//
+// Keys and values have two LDS slots each, filled from registers that were loaded a turn
+// earlier: every wave reads keys p and values p - 1 in turn p and writes keys p + 1 and
+// values p, and a barrier ends the turn.
 //
 // The running maximum is only moved (and the results rescaled) when a score exceeds it by 2^8:
 // a common factor cancels in the end, and weights up to 2^8 are as exact as those up to 1.
 //
 // Rows of the score tile are keys in the order that makes its accumulator the B operand of the
 // second product: row r is key r with bits 2 and 3 exchanged.
-template <typename T, int ND, int CT, int NW>
-__global__ __launch_bounds__(64 * NW, ND * CT <= 4 ? 2 : 1) void k_attend_tile(AttendArgs a) {
+template <typename T, int ND, int NW>
+__global__ __launch_bounds__(64 * NW, ND <= 2 ? 4 : ND <= 4 ? 2 : 1) void k_attend_tile(AttendArgs a) {
   typedef typename Vec8<T>::type V8;
-  constexpr int CD = 4 * ND;                      // 16-byte chunks of a key's row
-  constexpr int CK = (CD + 7) / 8 * 8;            // and the LDS row's
-  constexpr int NS = 2 * ND;                      // 16-dimension steps of the scores
-  constexpr int KCH = 32 * CD;                    // chunks of a step's keys, and of its values
   constexpr int NT = 64 * NW;
+  constexpr int HV = NW == 8 ? 2 : 1;             // 32-key blocks of a step
+  constexpr int KEYS = 32 * HV;
+  constexpr int CD = 4 * ND;                      // 16-byte chunks of a key's row
+  constexpr int CK = CD <= 8 ? 8 : (CD + 15) / 16 * 16;   // and the LDS row's
+  constexpr int KX = CK <= 8 ? 7 : 15;            // chunk c of row r is kept at c ^ (r & KX)
+  constexpr int NS = 2 * ND;                      // 16-dimension steps of the scores
+  constexpr int KCH = 32 * CD;                    // chunks of a block's keys, and of its values
   constexpr int PER = (KCH + NT - 1) / NT;
-  constexpr int R = 32 * CT * NW;
-  __shared__ V8 ks[2][32 * CK];
-  __shared__ V8 vs[2][KCH];
+  constexpr int R = 32 * NW;
+  __shared__ V8 ks[2][HV][32 * CK];
+  __shared__ V8 vs[2][HV][KCH];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c32 = lane & 31, half = lane >> 5;
@@ -976,30 +984,30 @@ __global__ __launch_bounds__(64 * NW, ND * CT <= 4 ? 2 : 1) void k_attend_tile(A
   if (rr0 >= (int64_t)n * G) return;
   const int r0 = (int)rr0;
   const int rows = (int)min((int64_t)R, (int64_t)n * G - rr0);
-  const int64_t held = min((int64_t)total, (int64_t)a.s.max_pages << a.s.page_shift);
-  const int64_t khi = min(held, (int64_t)total - n + (r0 + rows - 1) / G + 1);
+  const int held = (int)min((int64_t)total, (int64_t)a.s.max_pages << a.s.page_shift);
+  const int64_t khi64 = min((int64_t)held, (int64_t)total - n + (r0 + rows - 1) / G + 1);
   const int64_t klo = a.window > 0 ? max((int64_t)0, (int64_t)total - n + r0 / G - a.window + 1) : 0;
   const int64_t k0 = (int64_t)split * a.chunk, k1 = k0 + a.chunk;
-  int p0 = 0, steps = 0;                          // steps of 32 keys from key 32 p0
-  if (k0 < khi && k1 > klo) {
-    p0 = (int)(max(k0, klo) >> 5);
-    steps = (int)((min(k1, khi) + 31) >> 5) - p0;
-  } else if (a.splits > 1 || khi > klo) {
+  int kbeg = 0, steps = 0;                        // steps of KEYS keys from key kbeg
+  if (k0 < khi64 && k1 > klo) {
+    kbeg = (int)(max(k0, klo) / KEYS) * KEYS;
+    steps = (int)cdiv(min(k1, khi64) - kbeg, KEYS);
+  } else if (a.splits > 1 || khi64 > klo) {
     return;
   }
+  const int kend = (int)min(k1, khi64);           // first key that is not this workgroup's
 
   // queries, slots of this wave's rows
-  V8 qf[CT][NS];
-  int lim[CT], low[CT];
-  const int wr0 = wave * 32 * CT;
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    const int r = wr0 + ct * 32 + c32;
+  V8 qf[NS];
+  int lim, low;
+  const int wr0 = wave * 32;
+  {
+    const int r = wr0 + c32;
     const bool live = r < rows;
     const int rr = r0 + (live ? r : 0), ti = rr / G, hh = rr - ti * G;
     const int64_t slot = (int64_t)total - n + ti;
-    lim[ct] = live ? (int)max((int64_t)-1, min(slot, held - 1)) : -1;
-    low[ct] = a.window > 0 && live ? (int)max((int64_t)0, slot - a.window + 1) : 0;
+    lim = live ? (int)max((int64_t)-1, min(slot, (int64_t)kend - 1)) : -1;
+    low = a.window > 0 && live ? (int)max((int64_t)0, slot - a.window + 1) : 0;
     const T* qr = (const T*)a.q + (int64_t)(row0 + ti) * a.qt + (int64_t)(head * G + hh) * a.qh;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
@@ -1007,270 +1015,292 @@ __global__ __launch_bounds__(64 * NW, ND * CT <= 4 ? 2 : 1) void k_attend_tile(A
       V8 v = load_row8(qr + min(dim, d - 8), a.q_vec);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = dim < d ? (a.scale2 < 0.0f ? -v[e] : v[e]) : (T)0.0f;
-      qf[ct][s] = v;
+      qf[s] = v;
     }
   }
   const float sc2 = fabsf(a.scale2);
-  // steps in which every row of the wave sees every key need no mask
-  int wlim, wlow;
-  {
-    const int first = min(wr0, rows - 1), last = min(wr0 + 32 * CT, rows) - 1;
-    const int64_t s_first = (int64_t)total - n + (r0 + first) / G;
-    const int64_t s_last = (int64_t)total - n + (r0 + max(last, 0)) / G;
-    wlim = (int)max((int64_t)-1, min(s_first, held - 1));
+  // keys wlow .. wlim are seen by every row of the wave: steps among them need no mask
+  int wlim = -1, wlow = 0;
+  if (wr0 < rows) {
+    const int last = min(wr0 + 32, rows) - 1;
+    const int64_t s_first = (int64_t)total - n + (r0 + wr0) / G;
+    const int64_t s_last = (int64_t)total - n + (r0 + last) / G;
+    wlim = (int)max((int64_t)-1, min(s_first, (int64_t)kend - 1));
     wlow = a.window > 0 ? (int)max((int64_t)0, s_last - a.window + 1) : 0;
-    if (last < wr0) wlim = -1;
   }
 
-  // where this thread's chunks of a step's keys and values come from and go to
-  const T* kc = (const T*)a.k;
-  const T* vc = (const T*)a.v;
-  int kg[PER], kl[PER], vg[PER], vl[PER], vkey[PER];
+  // where this thread's chunks of a block's keys and values come from (bytes) and go to
+  uint32_t kg[PER], vg[PER];
+  int kl[PER], vl[PER], vkey[PER];
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const int i = min(tid + NT * j, KCH - 1);
     const int key = i / CD, c = i - key * CD;
     const int row = (key & 0x13) | ((key & 4) << 1) | ((key & 8) >> 1);
-    kg[j] = key * d + min(8 * c, d - 8);
-    kl[j] = row * CK + (c ^ (row & 7));
+    kg[j] = (key * d + min(8 * c, d - 8)) * 2;
+    kl[j] = row * CK + (c ^ (row & KX));
     const int dim = i >> 2, cv = i & 3;
-    vg[j] = min(dim, d - 1) * P + 8 * cv;
-    vl[j] = dim * 4 + (cv ^ ((dim >> 1) & 3));
+    vg[j] = (min(dim, d - 1) * P + 8 * cv) * 2;
+    vl[j] = dim * 4 + (cv ^ ((dim >> 2) & 3));
     vkey[j] = 8 * cv;
   }
-  V8 kreg[PER], vreg[PER];
-  const auto page_of = [&](int p) {
-    const int key = (p0 + min(p, steps - 1)) << 5;
-    return phys_page(a.s, b, key >> a.s.page_shift);
+  const auto mine = [&](int j) { return KCH % NT == 0 || tid + NT * j < KCH; };
+
+  // A block (32 keys): its page, raw as long as nothing waits for the load; then the byte
+  // offset of its record and how many of its keys exist
+  struct Block {
+    int64_t rec;       // of the page's keys and values
+    int off;           // first key's slot
+    int live;
   };
-  const auto base_of = [&](int p, int phys) {     // element of the step's first key slot
-    const int key = (p0 + min(p, steps - 1)) << 5;
-    return ((int64_t)max(phys, 0) * a.heads + head) * P * d + (int64_t)(key & (P - 1));
+  const Table prow = a.s.pages + (int64_t)b * a.s.stride;
+  const int kcap = steps > 0 ? kend - 1 : 0;
+  const auto raw_page = [&](int step, int hv) {
+    return prow[min(kbeg + step * KEYS + 32 * hv, kcap) >> a.s.page_shift];
   };
-  const auto load_k = [&](int p, int phys) {
-    const int off = ((p0 + min(p, steps - 1)) << 5) & (P - 1);
-    const T* kp = kc + ((int64_t)max(phys, 0) * a.heads + head) * P * d + (int64_t)off * d;
+  const int64_t page_bytes = (int64_t)a.heads * P * d * 2;
+  const auto block_of = [&](int step, int hv, int raw) {
+    Block k;
+    const int key = kbeg + step * KEYS + 32 * hv;
+    const bool ok = (unsigned)raw < (unsigned)a.s.cache_pages;
+    k.rec = (ok ? raw : 0) * page_bytes;
+    k.off = key & (P - 1);
+    k.live = ok ? kend - key : 0;
+    return k;
+  };
+  const char* kc = (const char*)a.k + (int64_t)head * P * d * 2;
+  const char* vc = (const char*)a.v + (int64_t)head * P * d * 2;
+  V8 kreg[HV][PER], vreg[HV][PER];
+  const auto load_k = [&](const Block* k) {
 #pragma unroll
-    for (int j = 0; j < PER; ++j) kreg[j] = load16<V8>(kp + kg[j]);
-  };
-  const auto load_v = [&](int p, int phys) {
-    const T* vp = vc + base_of(p, phys);
+    for (int hv = 0; hv < HV; ++hv)
 #pragma unroll
-    for (int j = 0; j < PER; ++j) vreg[j] = load16<V8>(vp + vg[j]);
+      for (int j = 0; j < PER; ++j)
+        kreg[hv][j] = load16<V8>(kc + k[hv].rec + k[hv].off * d * 2 + kg[j]);
+  };
+  const auto load_v = [&](const Block* k) {
+#pragma unroll
+    for (int hv = 0; hv < HV; ++hv)
+#pragma unroll
+      for (int j = 0; j < PER; ++j)
+        vreg[hv][j] = load16<V8>(vc + k[hv].rec + k[hv].off * 2 + vg[j]);
   };
   const auto store_k = [&](int slot) {
 #pragma unroll
-    for (int j = 0; j < PER; ++j)
-      if (KCH % NT == 0 || tid + NT * j < KCH) ks[slot][kl[j]] = kreg[j];
-  };
-  // `live` keys of the step exist; the others' slots may hold anything and become 0
-  const auto store_v = [&](int slot, int live) {
-    if (live < 32) {
+    for (int hv = 0; hv < HV; ++hv)
 #pragma unroll
       for (int j = 0; j < PER; ++j)
+        if (mine(j)) ks[slot][hv][kl[j]] = kreg[hv][j];
+  };
+  // slots past the last key may hold anything: they become 0, for 0 x NaN must not reach a sum
+  const auto store_v = [&](int slot, const Block* k) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vreg[j][e] = vkey[j] + e < live ? vreg[j][e] : (T)0.0f;
+    for (int hv = 0; hv < HV; ++hv) {
+      if (k[hv].live < 32) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            vreg[hv][j][e] = vkey[j] + e < k[hv].live ? vreg[hv][j][e] : (T)0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < PER; ++j)
+        if (mine(j)) vs[slot][hv][vl[j]] = vreg[hv][j];
     }
-#pragma unroll
-    for (int j = 0; j < PER; ++j)
-      if (KCH % NT == 0 || tid + NT * j < KCH) vs[slot][vl[j]] = vreg[j];
-  };
-  const auto live_keys = [&](int p, int phys) {
-    const int64_t key = (int64_t)(p0 + p) << 5;
-    return phys < 0 || p >= steps ? 0 : (int)min((int64_t)32, khi - key);
-  };
-  const auto frag_k = [&](int slot, int s) {
-    return ks[slot][c32 * CK + ((2 * s + half) ^ (c32 & 7))];
-  };
-  const auto frag_v = [&](int slot, int dt, int u) {
-    return vs[slot][(32 * dt + c32) * 4 + ((2 * u + half) ^ ((c32 >> 1) & 3))];
   };
 
-  f32x16 o[CT][ND], sa[CT], sb[CT];
-  V8 pw[CT][2];
-  float mx[CT], sum[CT], f[CT];
-  bool moved = false;
+  f32x16 o[ND], sc[HV];
+  V8 pw[HV][2];
+  float mx = -INFINITY, sum = 0.0f;
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    mx[ct] = -INFINITY;
-    sum[ct] = 0.0f;
-    f[ct] = 1.0f;
-    pw[ct][0] = pw[ct][1] = V8((T)0.0f);
+  for (int hv = 0; hv < HV; ++hv) pw[hv][0] = pw[hv][1] = V8((T)0.0f);
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt) o[ct][dt] = f32x16(0.0f);
-  }
-
-  if (steps > 0) {
-    int ph0 = page_of(0), ph1 = page_of(1), ph2 = page_of(2), ph3 = page_of(3);
-    load_k(0, ph0);
-    load_v(0, ph0);
-    store_k(0);
-    load_k(1, ph1);
-    store_k(1);
-    // the values of "step -1" are read before any are written: zeros
+  for (int dt = 0; dt < ND; ++dt) o[dt] = f32x16(0.0f);
+  const auto products = [&](int slot) {
 #pragma unroll
-    for (int j = 0; j < PER; ++j)
-      if (KCH % NT == 0 || tid + NT * j < KCH) vs[1][vl[j]] = V8((T)0.0f);
-    load_k(2, ph2);
-    __syncthreads();
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) sa[ct] = f32x16(0.0f);
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const V8 kf = frag_k(0, s);
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) sa[ct] = mfma32(kf, qf[ct][s], sa[ct]);
-    }
-    __syncthreads();
-
-    // one turn: sc the scores of step p, sn those of step p + 1, cur = p % 2
-    const auto turn = [&](int p, auto slot, f32x16(&sc)[CT], f32x16(&sn)[CT]) {
-      constexpr int cur = decltype(slot)::value, nxt = cur ^ 1;
-      // slot cur: keys of step p (used) become those of p + 2, values of p - 2 those of p
-      store_k(cur);
-      const int live = live_keys(p, ph0);
-      store_v(cur, live);
-      load_k(p + 3, ph3);
-      load_v(p + 1, ph1);
-      ph0 = ph1;
-      ph1 = ph2;
-      ph2 = ph3;
-      ph3 = page_of(p + 4);
-
-      const int key0 = (p0 + p) << 5;
-      if (live < 32 || key0 + 31 > wlim || key0 < wlow) {
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int kk = 16 * (i >> 3) + 8 * half + (i & 7);
-            const bool see = kk < live && key0 + kk <= lim[ct] && key0 + kk >= low[ct];
-            sc[ct][i] = see ? sc[ct][i] : -INFINITY;
-          }
-      }
-      float top[CT];
-      bool grow = false;
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        float m = sc[ct][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) m = fmaxf(m, sc[ct][i]);
-        top[ct] = m * sc2;
-        grow |= top[ct] > mx[ct] + 8.0f;
-      }
-      // a maximum moved in turn p - 1: by now the products with the weights before it are in
-      if (moved) {
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int dt = 0; dt < ND; ++dt) o[ct][dt] *= f[ct];
-      }
-      moved = __ballot(grow) != 0;
-      if (moved) {
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          const float m = fmaxf(mx[ct], fmaxf(top[ct], __shfl_xor(top[ct], 32)));
-          f[ct] = m == -INFINITY ? 1.0f : exp2_fast(mx[ct] - m);
-          mx[ct] = m;
-          sum[ct] *= f[ct];
-        }
-      }
-
-      V8 pn[CT][2];
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) sn[ct] = f32x16(0.0f);
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        const V8 kf = frag_k(nxt, s);
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) sn[ct] = mfma32(kf, qf[ct][s], sn[ct]);
-      }
+    for (int hv = 0; hv < HV; ++hv)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
-          const V8 vf = frag_v(nxt, dt, u);
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) o[ct][dt] = mfma32(vf, pw[ct][u], o[ct][dt]);
+          const V8 vf = vs[slot][hv][(32 * dt + c32) * 4 + ((2 * u + half) ^ ((c32 >> 2) & 3))];
+          o[dt] = mfma32(vf, pw[hv][u], o[dt]);
         }
+  };
+
+  const auto matrix = [&](auto parity) {
+    constexpr int cur = decltype(parity)::value;
+    products(cur ^ 1);
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        const float base = mx[ct] == -INFINITY ? 0.0f : mx[ct];
-        float z = 0.0f;
+    for (int hv = 0; hv < HV; ++hv) sc[hv] = f32x16(0.0f);
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int hv = 0; hv < HV; ++hv) {
+        const V8 kf = ks[cur][hv][c32 * CK + ((2 * s + half) ^ (c32 & KX))];
+        sc[hv] = mfma32(kf, qf[s], sc[hv]);
+      }
+    // operands are read a few products ahead
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int i = 0; i < HV * 4 * ND; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // blocks of the steps p, p + 1, p + 2, raw pages of step p + 3
+  Block b0[HV], b1[HV], b2[HV];
+  int raw[HV];
+  const auto pass_on = [&](int p, auto parity) {
+    constexpr int cur = decltype(parity)::value;
+    store_k(cur ^ 1);
+    store_v(cur, b0);
+    load_k(b2);
+    load_v(b1);
+#pragma unroll
+    for (int hv = 0; hv < HV; ++hv) {
+      b0[hv] = b1[hv];
+      b1[hv] = b2[hv];
+      b2[hv] = block_of(p + 3, hv, raw[hv]);
+      raw[hv] = raw_page(p + 4, hv);
+    }
+  };
+  const auto vector = [&](int p, const int* live) {
+    const int key0 = kbeg + p * KEYS;
+    bool edge = key0 + KEYS - 1 > wlim || key0 < wlow;
+#pragma unroll
+    for (int hv = 0; hv < HV; ++hv) edge |= live[hv] < 32;
+    if (edge) {
+#pragma unroll
+      for (int hv = 0; hv < HV; ++hv)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float e = exp2_fast(__fmaf_rn(sc[ct][i], sc2, -base));
-          z += e;
-          pn[ct][i >> 3][i & 7] = (T)e;      // rounded for the matrix product
+          const int kk = 16 * (i >> 3) + 8 * half + (i & 7), key = key0 + 32 * hv + kk;
+          const bool see = kk < live[hv] && key <= lim && key >= low;
+          sc[hv][i] = see ? sc[hv][i] : -INFINITY;
         }
-        sum[ct] += z;
-      }
+    }
+    float top = sc[0][0];
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        pw[ct][0] = pn[ct][0];
-        pw[ct][1] = pn[ct][1];
-      }
-      // the weights are formed here, between the products, and not where they are next used
+    for (int hv = 0; hv < HV; ++hv)
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) asm volatile("" : "+v"(pw[ct][0]), "+v"(pw[ct][1]));
-      __syncthreads();
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[hv][i]);
+    top *= sc2;
+    if (__ballot(top > mx + 8.0f) != 0) {
+      const float m = fmaxf(mx, fmaxf(top, __shfl_xor(top, 32)));
+      const float f = m == -INFINITY ? 1.0f : exp2_fast(mx - m);
+      mx = m;
+      sum *= f;
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) o[dt] *= f;
+    }
+    const float base = mx == -INFINITY ? 0.0f : mx;
+    float z = 0.0f;
+#pragma unroll
+    for (int hv = 0; hv < HV; ++hv)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = exp2_fast(__fmaf_rn(sc[hv][i], sc2, -base));
+        z += e;
+        pw[hv][i >> 3][i & 7] = (T)e;          // rounded for the matrix product
+      }
+    sum += z;
+    // the weights are formed in this part, and not where they are next used
+#pragma unroll
+    for (int hv = 0; hv < HV; ++hv) asm volatile("" : "+v"(pw[hv][0]), "+v"(pw[hv][1]));
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  if (steps > 0) {
+#pragma unroll
+    for (int hv = 0; hv < HV; ++hv) {
+      b0[hv] = block_of(0, hv, raw_page(0, hv));
+      b1[hv] = block_of(1, hv, raw_page(1, hv));
+      b2[hv] = block_of(2, hv, raw_page(2, hv));
+      raw[hv] = raw_page(3, hv);
+    }
+    load_k(b0);
+    load_v(b0);
+    store_k(0);
+    // the values of "step -1" are read before any are written: zeros
+#pragma unroll
+    for (int hv = 0; hv < HV; ++hv)
+#pragma unroll
+      for (int j = 0; j < PER; ++j)
+        if (mine(j)) vs[1][hv][vl[j]] = V8((T)0.0f);
+    load_k(b1);
+    __syncthreads();
+    constexpr std::integral_constant<int, 0> even{};
+    constexpr std::integral_constant<int, 1> odd{};
+    int live[HV];
+    const auto keep_live = [&] {
+#pragma unroll
+      for (int hv = 0; hv < HV; ++hv) live[hv] = b0[hv].live;
     };
-    // an odd count ends in a step without keys
-    for (int p = 0; p < steps; p += 2) {
-      turn(p, std::integral_constant<int, 0>{}, sa, sb);
-      turn(p + 1, std::integral_constant<int, 1>{}, sb, sa);
-    }
-    if (moved) {
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt) o[ct][dt] *= f[ct];
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int dt = 0; dt < ND; ++dt) {
-        const V8 vf = frag_v(1, dt, u);
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) o[ct][dt] = mfma32(vf, pw[ct][u], o[ct][dt]);
+    // an odd count of steps ends in one without keys
+    if (NW == 4 || wave < NW / 2) {
+      for (int p = 0; p < steps; p += 2) {
+        matrix(even);
+        keep_live();
+        pass_on(p, even);
+        vector(p, live);
+        __syncthreads();
+        matrix(odd);
+        keep_live();
+        pass_on(p + 1, odd);
+        vector(p + 1, live);
+        __syncthreads();
       }
+    } else {
+      for (int p = 0; p < steps; p += 2) {
+        if (p > 0) vector(p - 1, live);
+        keep_live();
+        pass_on(p, even);
+        matrix(even);
+        __syncthreads();
+        vector(p, live);
+        keep_live();
+        pass_on(p + 1, odd);
+        matrix(odd);
+        __syncthreads();
+      }
+      vector((steps + 1) / 2 * 2 - 1, live);
+    }
+    products(1);
   }
 
+  const float z = sum + __shfl_xor(sum, 32);
+  const int r = wr0 + c32;
+  if (r >= rows) return;
+  const int rr = r0 + r, ti = rr / G, hh = rr - ti * G;
+  const int64_t orow = (int64_t)(row0 + ti) * a.hq + head * G + hh;
+  const int64_t pr = (int64_t)split * a.tokens * a.hq + orow;
+  const float inv = z > 0.0f ? 1.0f / z : 0.0f;
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
-    const float z = sum[ct] + __shfl_xor(sum[ct], 32);
-    const int r = wr0 + ct * 32 + c32;
-    if (r >= rows) continue;
-    const int rr = r0 + r, ti = rr / G, hh = rr - ti * G;
-    const int64_t orow = (int64_t)(row0 + ti) * a.hq + head * G + hh;
-    const int64_t pr = (int64_t)split * a.tokens * a.hq + orow;
-    const float inv = z > 0.0f ? 1.0f / z : 0.0f;
+  for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) {
-        const int dim = 32 * dt + 8 * i4 + 4 * half;
-        if (dim >= d) continue;
-        if (a.splits == 1) {
-          alignas(8) T w[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = (T)(z > 0.0f ? o[ct][dt][4 * i4 + i] * inv : z);
-          *reinterpret_cast<uint2*>((T*)a.out + orow * d + dim) = *reinterpret_cast<uint2*>(w);
-        } else {
-          f32x4 v;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = o[ct][dt][4 * i4 + i];
-          *reinterpret_cast<f32x4*>(a.part_o + pr * d + dim) = v;
-        }
-      }
-    if (half == 0) {
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const int dim = 32 * dt + 8 * i4 + 4 * half;
+      if (dim >= d) continue;
       if (a.splits == 1) {
-        if (a.lse)
-          a.lse[orow] = z > 0.0f ? (mx[ct] + log2_fast(z)) * kLn2 : (z == 0.0f ? -INFINITY : z);
+        alignas(8) T w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (T)(z > 0.0f ? o[dt][4 * i4 + i] * inv : z);
+        *reinterpret_cast<uint2*>((T*)a.out + orow * d + dim) = *reinterpret_cast<uint2*>(w);
       } else {
-        a.part_ml[pr * 2] = mx[ct];
-        a.part_ml[pr * 2 + 1] = z;
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = o[dt][4 * i4 + i];
+        *reinterpret_cast<f32x4*>(a.part_o + pr * d + dim) = v;
       }
+    }
+  if (half == 0) {
+    if (a.splits == 1) {
+      if (a.lse) a.lse[orow] = z > 0.0f ? (mx + log2_fast(z)) * kLn2 : (z == 0.0f ? -INFINITY : z);
+    } else {
+      a.part_ml[pr * 2] = mx;
+      a.part_ml[pr * 2 + 1] = z;
     }
   }
 }
@@ -1388,8 +1418,9 @@ Plan plan_dense(int heads, int page, int d, int64_t tokens, int32_t batch, int g
   const int64_t rows = cdiv(tokens, batch) * group;
   int64_t want, unit;
   if (rows > 64) {
-    const int least = d <= 64 ? 256 : 128;
-    p.rows = rows > least && d <= 128 ? 2 * least : least;
+    // eight waves share a step's operands up to 128 dimensions; up to 64 the vector part takes
+    // longer than the matrix part, and four workgroups of four waves a CU hide more of it
+    p.rows = rows > 128 && d > 64 && d <= 128 ? 256 : 128;
     const int64_t tiles = tokens * group / p.rows;
     p.items = tiles + batch;
     // one workgroup a CU; keys are split where there are fewer row tiles than that
@@ -1473,15 +1504,14 @@ void launch_few_rt(const AttendArgs& a, const Plan& p, hipStream_t st) {
 
 template <typename T, int ND>
 void launch_tile(const AttendArgs& a, const Plan& p, hipStream_t st) {
-  constexpr int CT = ND <= 2 ? 2 : 1;
   const dim3 grid((unsigned)(p.items * a.heads), (unsigned)p.splits);
-  if constexpr (ND <= 4) {
-    if (p.rows == 256 * CT) {
-      hipLaunchKernelGGL((k_attend_tile<T, ND, CT, 8>), grid, dim3(512), 0, st, a);
+  if constexpr (ND == 3 || ND == 4) {
+    if (p.rows == 256) {
+      hipLaunchKernelGGL((k_attend_tile<T, ND, 8>), grid, dim3(512), 0, st, a);
       return;
     }
   }
-  hipLaunchKernelGGL((k_attend_tile<T, ND, CT, 4>), grid, dim3(256), 0, st, a);
+  hipLaunchKernelGGL((k_attend_tile<T, ND, 4>), grid, dim3(256), 0, st, a);
 }
 
 template <typename T>
