@@ -406,6 +406,7 @@ typedef enum { GMM_F32 = 0, GMM_BF16 = 1, GMM_F16 = 2 } gmm_dtype;
 #define GMM_KV_MAX_HEADS 1024
 #define GMM_KV_MAX_GROUP 64
 #define GMM_KV_MAX_KEEP 4096
+#define GMM_KV_MAX_PAGES 65536
 
 typedef struct {
   void* k;          /* [pages, heads, page, d] */
@@ -506,7 +507,8 @@ size_t gmm_kv_workspace_bytes(const gmm_kv_cache* cache, int64_t tokens, int32_t
  *   q [tokens, hq, d], rows contiguous, strides in elements
  *   idx [tokens, heads, m] int32: indexes into the sequence's page table,
  *   ascending, -1 behind the last where fewer than m pages are visible
- * 1 <= m <= GMM_KV_MAX_KEEP, keep_first >= 0, keep_first + keep_last <= m.
+ * 1 <= m <= GMM_KV_MAX_KEEP, keep_first >= 0, keep_first + keep_last <= m,
+ * max_pages <= GMM_KV_MAX_PAGES.
  */
 int gmm_kv_select(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t tokens,
                   const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t hq,

@@ -243,18 +243,19 @@ __global__ __launch_bounds__(256) void k_rope_table(const double* __restrict__ f
   table[p * 2 * half + half + j] = (float)(scale * s);
 }
 
-// One token a workgroup row (grid.x), 256 units of its heads a workgroup (grid.y); a unit is
-// 16 elements (W = 8: 16-byte accesses) where rot, d, the strides and the addresses allow it,
-// else one pair.  An odd count of dimensions past rot ends in a unit of its own (W = 1).
+// A unit a thread: 16 elements (W = 8: 16-byte accesses) where rot, d, the strides and the
+// addresses allow it, else one pair.  An odd count of dimensions past rot ends in a unit of its
+// own (W = 1).  Bound by the bytes.
 template <typename T, int W, bool INTER>
 __global__ __launch_bounds__(256) void k_rope(const T* x, int64_t xt, int64_t xh, T* out,
-                                              int64_t ot, int64_t oh, int heads, int d,
-                                              const int32_t* __restrict__ pos, RopeShape r) {
-  const int64_t t = blockIdx.x;
-  const int units = (d + 2 * W - 1) / (2 * W);
-  const int i = blockIdx.y * 256 + threadIdx.x;
-  if (i >= heads * units) return;
-  const int h = i / units, u = i - h * units;
+                                              int64_t ot, int64_t oh, uint32_t items, int heads,
+                                              int d, const int32_t* __restrict__ pos,
+                                              RopeShape r) {
+  const uint32_t i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= items) return;
+  const uint32_t units = (d + 2 * W - 1) / (2 * W);
+  const uint32_t row = i / units, t = row / heads;
+  const int u = i - row * units, h = row - t * heads;
   const T* xr = x + t * xt + (int64_t)h * xh;
   T* orow = out + t * ot + (int64_t)h * oh;
   if (W == 1 && 2 * u + 1 >= d && u >= (r.rot >> 1)) {
@@ -284,41 +285,51 @@ struct AppendArgs {
   void* qo;
   int64_t qot, qoh;
   int hq;
+  int per;                   // heads a workgroup takes: 1, 2 or 4
   int64_t page_blocks;       // workgroups of pages; the rest rotate queries
-  int q_blocks;              // workgroups a token's queries take
+  uint32_t q_items;          // units of all queries
 };
 
-// One workgroup a (page touched, head): the page's new keys are rotated and stored, its new
-// values stored transposed, and its box formed from all its keys, the older ones read back
+// One workgroup a (page touched, `per` heads): the page's new keys are rotated and stored, its
+// new values stored transposed, and its box formed from all its keys, the older ones read back
 // (a page of 64 keys of 128 dimensions is 16 KB, so a single new token moves 8 KB on average
 // for a box that saves reading that page in every later step in which it is not selected).
-// The queries' rotation rides along in workgroups of its own: one launch for the step.
+// Small pages share a workgroup, 128 or 64 threads a head.  The queries' rotation rides along in
+// workgroups of its own: one launch for the step.
 template <typename T, int W, bool INTER>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
-  const int tid = threadIdx.x;
+  typedef typename Vec8<T>::type V8;
   if ((int64_t)blockIdx.x >= a.page_blocks) {
-    const int64_t qb = (int64_t)blockIdx.x - a.page_blocks;
-    const int64_t t = qb / a.q_blocks;
-    const int units = a.d / (2 * W);
+    const uint32_t first = (uint32_t)(blockIdx.x - a.page_blocks) * 256;
+    const uint32_t i = first + threadIdx.x;
+    const uint32_t units = a.d / (2 * W), row_units = units * a.hq;
+    if (first >= a.q_items) return;
+    const uint32_t t = min(i, a.q_items - 1) / row_units;
     int p;
     if (a.pos) {
       p = a.pos[t];
     } else {
-      // the sequence of row t is the last with cu[b] <= t that is not empty there
-      const int b = find_seq(a.s, t, 1, 1, 0);
+      // the sequence of the wave's first row, then of this thread's
+      int b = find_seq(a.s, __builtin_amdgcn_readfirstlane(t), 1, 1, 0);
+      while (a.s.cu[b + 1] <= (int)t) ++b;
       p = a.s.total[b] - (a.s.cu[b + 1] - (int)t);
     }
-    const int i = (int)(qb - t * a.q_blocks) * 256 + tid;
-    if (i >= a.hq * units) return;
-    const int h = i / units, u = i - h * units;
+    if (i >= a.q_items) return;
+    const int h = (i - t * row_units) / units, u = i % units;
     rope_unit<T, W, INTER>((const T*)a.q + t * a.qt + (int64_t)h * a.qh,
-                    (T*)a.qo + t * a.qot + (int64_t)h * a.qoh, u, p, a.rope);
+                           (T*)a.qo + t * a.qot + (int64_t)h * a.qoh, u, p, a.rope);
     return;
   }
+  constexpr int kBatch = W == 1 ? 8 : 2;             // rows in flight a thread
   __shared__ T red[256 * 2 * W * 2];
   __shared__ float wmax[4];
-  const int head = blockIdx.x % a.heads;
-  const int64_t item = blockIdx.x / a.heads;
+  __shared__ int wbad[4];
+  const int threads = 256 / a.per;                   // of a head: whole waves
+  const int hsub = threadIdx.x / threads, tid = threadIdx.x - hsub * threads;
+  const int head_blocks = (a.heads + a.per - 1) / a.per;
+  const int head = (int)(blockIdx.x % head_blocks) * a.per + hsub;
+  const bool live = head < a.heads;
+  const int64_t item = blockIdx.x / head_blocks;
   const int P = a.page, d = a.d;
   const int b = find_seq(a.s, item, 1, P, 2);
   const int row0 = a.s.cu[b], n = a.s.cu[b + 1] - row0, total = a.s.total[b];
@@ -333,68 +344,29 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
   const int first = lp << a.s.page_shift;                // first slot of the page
   const int filled = min(P, total - first);
   const int begin = max(0, s0 - first);                  // new keys: begin .. filled - 1
-  const int64_t ph = (int64_t)phys * a.heads + head;
+  const int64_t ph = (int64_t)phys * a.heads + (live ? head : 0);
   const int64_t in0 = row0 + ((int64_t)first - s0l);     // input row of the page's slot 0
 
-  // keys
-  T* ckp = (T*)a.ck + ph * P * d;
-  const int units = d / (2 * W), groups = 256 / units;
-  const int u = tid % units, g = tid / units;
-  const Unit<W> un(u, a.rope.rot, INTER);
-  UnitV<float, W> hi = -INFINITY, lo = INFINITY;
-  bool bad = false;
-  const int from = a.box ? 0 : begin;
-  if (g < groups) {
-    for (int s = from + g; s < filled; s += groups) {
-      UnitV<T, W> v;
-      if (s < begin) {
-        load_run<T, W>(ckp + (int64_t)s * d + un.o0, v, 0);
-        load_run<T, W>(ckp + (int64_t)s * d + un.o1, v, W);
-      } else {
-        const int64_t r = in0 + s;
-        const T* kr = (const T*)a.k + r * a.kt + (int64_t)head * a.kh;
-        load_run<T, W>(kr + un.o0, v, 0);
-        load_run<T, W>(kr + un.o1, v, W);
-        if (a.rope.table) rotate_unit<T, W, INTER>(v, un.pair, a.pos ? a.pos[r] : first + s, a.rope);
-        store_run<T, W>(ckp + (int64_t)s * d + un.o0, v, 0);
-        store_run<T, W>(ckp + (int64_t)s * d + un.o1, v, W);
-      }
-      if (a.box) {
-#pragma unroll
-        for (int e = 0; e < 2 * W; ++e) {
-          const float f = (float)v[e];
-          bad |= !(fabsf(f) <= FLT_MAX);
-          hi[e] = fmaxf(hi[e], f);
-          lo[e] = fminf(lo[e], f);
-        }
-      }
-    }
-  }
-
-  // values: 8 slots x 8 dimensions a thread, slots fastest over the lanes, so that a
-  // dimension's run of slots is written in whole lines
+  // values first, their stores need not be waited for: 8 slots x 8 dimensions a thread, slots
+  // fastest over the lanes, so that a dimension's run of slots is written in whole lines
   {
     T* cvp = (T*)a.cv + ph * d * P;
+    const T* vin = (const T*)a.v + (int64_t)(live ? head : 0) * a.vh;
     const int g0 = begin >> 3, ng = ((filled + 7) >> 3) - g0, nc = d >> 3;
-    for (int i = tid; i < ng * nc; i += 256) {
+    for (int i = tid; live && i < ng * nc; i += threads) {
       const int c = i / ng, sg = (g0 + i - c * ng) << 3;
-      typename Vec8<T>::type blk[8];
+      V8 blk[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int s = sg + j;
-        if (s >= begin && s < filled) {
-          const T* vr = (const T*)a.v + (in0 + s) * a.vt + (int64_t)head * a.vh + c * 8;
-          blk[j] = load_row8(vr, a.v_vec);
-        } else {
-          blk[j] = typename Vec8<T>::type((T)0.0f);
-        }
+        const int s = min(max(sg + j, begin), filled - 1);      // rows outside are not stored
+        blk[j] = load_row8(vin + (in0 + s) * a.vt + c * 8, a.v_vec);
       }
       const bool whole = sg >= begin && sg + 8 <= filled;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         T* dst = cvp + (int64_t)(c * 8 + e) * P + sg;
         if (whole) {
-          typename Vec8<T>::type col;
+          V8 col;
 #pragma unroll
           for (int j = 0; j < 8; ++j) col[j] = blk[j][e];
           *reinterpret_cast<uint4*>(dst) = __builtin_bit_cast(uint4, col);
@@ -406,42 +378,93 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
       }
     }
   }
+
+  // keys
+  T* ckp = (T*)a.ck + ph * P * d;
+  const T* kin = (const T*)a.k + (int64_t)(live ? head : 0) * a.kh;
+  const int units = d / (2 * W), groups = threads / units;
+  const int u = tid % units, g = tid / units;
+  const Unit<W> un(u, a.rope.rot, INTER);
+  UnitV<float, W> hi = -INFINITY, lo = INFINITY;
+  bool bad = false;
+  const int from = a.box ? 0 : begin;
+  if (live && g < groups) {
+    for (int sb = from + g; sb < filled; sb += kBatch * groups) {
+      UnitV<T, W> v[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int s = min(sb + j * groups, filled - 1);
+        const T* kr = s < begin ? ckp + (int64_t)s * d : kin + (in0 + s) * a.kt;
+        load_run<T, W>(kr + un.o0, v[j], 0);
+        load_run<T, W>(kr + un.o1, v[j], W);
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int s = sb + j * groups;
+        if (s >= filled) break;
+        if (s >= begin) {
+          if (a.rope.table)
+            rotate_unit<T, W, INTER>(v[j], un.pair, a.pos ? a.pos[in0 + s] : first + s, a.rope);
+          store_run<T, W>(ckp + (int64_t)s * d + un.o0, v[j], 0);
+          store_run<T, W>(ckp + (int64_t)s * d + un.o1, v[j], W);
+        }
+#pragma unroll
+        for (int e = 0; e < 2 * W; ++e) {
+          const float f = (float)v[j][e];
+          bad |= !(fabsf(f) <= FLT_MAX);
+          hi[e] = fmaxf(hi[e], f);
+          lo[e] = fminf(lo[e], f);
+        }
+      }
+    }
+  }
   if (!a.box) return;
 
-  // box: the keys are of type T, so their bounds are kept in T without rounding
-  T* rhi = red;
-  T* rlo = red + 256 * 2 * W;
-  if (g < groups) {
+  // box: the keys are of type T, so their bounds are kept in T without rounding; a row of 2 d
+  // entries (upper, then lower bounds) for every group
+  T* hred = red + hsub * threads * 4 * W;
+  if (live && g < groups) {
 #pragma unroll
     for (int e = 0; e < 2 * W; ++e) {
       const int dim = (e < W ? un.o0 : un.o1 - W) + e;
-      rhi[g * d + dim] = (T)hi[e];
-      rlo[g * d + dim] = (T)lo[e];
+      hred[g * 2 * d + dim] = (T)hi[e];
+      hred[g * 2 * d + d + dim] = (T)lo[e];
     }
   }
-  const int any_bad = __syncthreads_or(bad);
-  float h = -INFINITY, l = INFINITY, m = 0.0f;
-  if (tid < d) {
-    for (int j = 0; j < groups; ++j) {
-      h = fmaxf(h, (float)rhi[j * d + tid]);
-      l = fminf(l, (float)rlo[j * d + tid]);
-    }
-    m = fmaxf(fabsf(h), fabsf(l));
+  // this head's waves agree on its largest magnitude; up to 512 / 64 bounds a thread
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t any = __ballot(bad);
+  if (lane == 0) wbad[wave] = any != 0;
+  __syncthreads();
+  const int rounds = (2 * d + threads - 1) / threads;
+  float m = 0.0f;
+  for (int r = 0; r < rounds; ++r) {
+    const int t = tid + r * threads;
+    if (!live || t >= 2 * d) continue;
+    const float sign = t < d ? 1.0f : -1.0f;
+    float x = -INFINITY;
+    for (int j = 0; j < groups; ++j) x = fmaxf(x, sign * (float)hred[j * 2 * d + t]);
+    m = fmaxf(m, fabsf(x));
+    hred[t] = (T)(sign * x);             // row 0 becomes the page's (its entry is read)
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  if ((tid & 63) == 0) wmax[tid >> 6] = m;
+  if (lane == 0) wmax[wave] = m;
   __syncthreads();
-  m = fmaxf(fmaxf(wmax[0], wmax[1]), fmaxf(wmax[2], wmax[3]));
+  const int w0 = hsub * (threads >> 6);
+  int any_bad = 0;
+  for (int w = w0; w < w0 + (threads >> 6); ++w) {
+    m = fmaxf(m, wmax[w]);
+    any_bad |= wbad[w];
+  }
+  if (!live) return;
   const float unit = any_bad ? INFINITY : m * kInv127;
-  if (tid < d) {
-    float bh = 0.0f, bl = 0.0f;
-    if (!any_bad && unit > 0.0f) {
-      bh = fminf(127.0f, ceilf(__fdiv_rn(h, unit)));
-      bl = fmaxf(-127.0f, floorf(__fdiv_rn(l, unit)));
-    }
-    a.box[ph * 2 * d + tid] = (int8_t)(int)fmaxf(-127.0f, bh);
-    a.box[ph * 2 * d + d + tid] = (int8_t)(int)fminf(127.0f, bl);
+  for (int t = tid; t < 2 * d; t += threads) {
+    const float x = (float)hred[t];
+    float q = 0.0f;
+    if (!any_bad && unit > 0.0f)
+      q = t < d ? ceilf(__fdiv_rn(x, unit)) : floorf(__fdiv_rn(x, unit));
+    a.box[ph * 2 * d + t] = (int8_t)(int)fminf(127.0f, fmaxf(-127.0f, q));
   }
   if (tid == 0) a.box_scale[ph] = unit;
 }
@@ -459,8 +482,7 @@ struct SelectArgs {
   int col_tiles;             // 16-column tiles a token takes (1 unless group > 16)
   float* score;              // [tokens * heads][row]
   int64_t row;
-  int chunk_tiles;           // 16-page tiles a wave scores
-  int parts;                 // workgroups a row of tiles takes
+  int parts;                 // workgroups (256 pages each) a row of tiles takes
 };
 
 __device__ __forceinline__ float score_of(float query_unit, float page_unit, int dot) {
@@ -470,10 +492,14 @@ __device__ __forceinline__ float score_of(float query_unit, float page_unit, int
 
 // Scores: [pages x 2 d] . [2 d x (token, query head)] in 8-bit integers on 16x16x64 MFMA, the
 // boxes (upper | lower bounds) straight from memory in operand order, the queries (positive |
-// negative parts) from LDS.  Bound by the boxes' bytes: 2 d + 4 a (page, head).
-template <typename T>
+// negative parts) through LDS.  A wave takes 64 pages: their numbers are one load, their boxes
+// (16 KB at d = 128) are in flight together while the queries are rounded to 8 bits.  S: 64-byte
+// steps of a box.  Bound by the boxes' bytes: 2 d + 4 a (page, head).
+template <typename T, int S>
 __global__ __launch_bounds__(256) void k_select_score(SelectArgs a) {
-  extern __shared__ int8_t q8[];            // [col_tiles][16][2 d], then the units [.][16]
+  typedef typename Vec8<T>::type V8;
+  constexpr int TB = S <= 4 ? 4 : 2;        // 16-page tiles in flight
+  extern __shared__ int8_t q8[];            // [col_tiles * 16][2 d + 16], then the units [.]
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = 16 >> a.col_shift;        // tokens a tile holds
   const int part_no = blockIdx.x % a.parts;
@@ -487,108 +513,160 @@ __global__ __launch_bounds__(256) void k_select_score(SelectArgs a) {
   const int64_t total = min((int64_t)a.s.total[b], (int64_t)a.s.max_pages << a.s.page_shift);
   const int64_t last = min(total - 1, (int64_t)a.s.total[b] - n + tok0 + toks - 1);
   const int visible = last < 0 ? 0 : (int)(last >> a.s.page_shift) + 1;
-  const int tile0 = (part_no * 4 + wave) * a.chunk_tiles;
-  if (part_no * 4 * a.chunk_tiles * 16 >= visible) return;
+  if (part_no * 256 >= visible) return;
 
-  // queries in 8 bits: 16 threads a column, 16 columns at a time
-  const int d = a.d, cols = a.col_tiles * 16;
-  float* unit = reinterpret_cast<float*>(q8 + (size_t)cols * 2 * d);
-  for (int c0 = 0; c0 < cols; c0 += 16) {
-    const int c = c0 + (tid >> 4), part = tid & 15;
-    const int tt = (c & 15) >> a.col_shift, hh = c0 + (c & ((1 << a.col_shift) - 1));
-    const bool live = tt < toks && hh < a.group;
-    const T* qr = (const T*)a.q + (int64_t)(row0 + tok0 + (live ? tt : 0)) * a.qt +
-                  (int64_t)(head * a.group + (live ? hh : 0)) * a.qh;
-    float m = 0.0f;
-    bool bad = false;
-    for (int e = part; e < d; e += 16) {
-      const float f = live ? fabsf((float)qr[e]) : 0.0f;
-      bad |= !(f <= FLT_MAX);
-      m = fmaxf(m, f);
+  // queries: 16 threads a column, runs of 8 dimensions part, part + 16
+  const int d = a.d, cols = a.col_tiles * 16, stride = 2 * d + 16;
+  float* unit = reinterpret_cast<float*>(q8 + (size_t)cols * stride);
+  const int part = tid & 15;
+  V8 qv[2];
+  const auto head_of = [&](int c) { return (c & ~15) + (c & ((1 << a.col_shift) - 1)); };
+  const auto live_col = [&](int c) {
+    return ((c & 15) >> a.col_shift) < toks && head_of(c) < a.group;
+  };
+  const auto load_column = [&](int c) {
+    const bool live = live_col(c);
+    const T* qr = (const T*)a.q +
+                  (int64_t)(row0 + tok0 + (live ? (c & 15) >> a.col_shift : 0)) * a.qt +
+                  (int64_t)(head * a.group + (live ? head_of(c) : 0)) * a.qh;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int at = 8 * (part + 16 * j);
+      V8 v = load_row8(qr + min(at, d - 8), a.q_vec);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = live && at < d ? v[e] : (T)0.0f;
+      qv[j] = v;
     }
-    int ib = bad;
+  };
+  const auto round_column = [&](int c) {
+    float m = 0.0f;
+    int bad = 0;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float f = fabsf((float)qv[j][e]);
+        bad |= !(f <= FLT_MAX);
+        m = fmaxf(m, f);
+      }
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) {
       m = fmaxf(m, __shfl_xor(m, o));
-      ib |= __shfl_xor(ib, o);
+      bad |= __shfl_xor(bad, o);
     }
-    const float un = ib ? INFINITY : m * kInv127;
-    const bool zero = ib || !(un > 0.0f);
-    for (int e = part; e < d; e += 16) {
-      const float f = live && !zero ? rintf(__fdiv_rn((float)qr[e], un)) : 0.0f;
-      q8[(size_t)c * 2 * d + e] = (int8_t)(int)fmaxf(f, 0.0f);
-      q8[(size_t)c * 2 * d + d + e] = (int8_t)(int)fminf(f, 0.0f);
+    const float un = bad ? INFINITY : m * kInv127;
+    const bool zero = bad || !(un > 0.0f);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int at = 8 * (part + 16 * j);
+      if (at >= d) continue;
+      uint64_t up = 0, dn = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float f = zero ? 0.0f : rintf(__fdiv_rn((float)qv[j][e], un));
+        up |= (uint64_t)(uint8_t)(int8_t)(int)fmaxf(f, 0.0f) << (8 * e);
+        dn |= (uint64_t)(uint8_t)(int8_t)(int)fminf(f, 0.0f) << (8 * e);
+      }
+      *reinterpret_cast<uint64_t*>(q8 + (size_t)c * stride + at) = up;
+      *reinterpret_cast<uint64_t*>(q8 + (size_t)c * stride + d + at) = dn;
     }
-    if (part == 0) unit[c] = live ? un : -1.0f;          // -1: no query in this column
+    if (part == 0) unit[c] = live_col(c) ? un : -1.0f;       // -1: no query in this column
+  };
+  load_column(tid >> 4);
+
+  // this wave's pages, one a lane
+  const int p0 = (part_no * 4 + wave) * 64;
+  const int lp = p0 + lane;
+  const int phys = lp < visible ? phys_page(a.s, b, lp) : -1;
+  const float sp = a.box_scale[(int64_t)max(phys, 0) * a.heads + head];
+  const int n16 = lane & 15, g = lane >> 4;
+  i32x4 bx[TB][S];
+  const auto load_boxes = [&](int t0) {
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+      const int64_t rec = (int64_t)max(__shfl(phys, 16 * (t0 + t) + n16), 0) * a.heads + head;
+#pragma unroll
+      for (int st = 0; st < S; ++st)               // past the end: times 0 below
+        bx[t][st] = load16<i32x4>(a.box + rec * 2 * d + min(64 * st + 16 * g, 2 * d - 16));
+    }
+  };
+  if (p0 < visible) load_boxes(0);
+  for (int c0 = 0; c0 < cols; c0 += 16) {
+    if (c0 > 0) load_column(c0 + (tid >> 4));
+    round_column(c0 + (tid >> 4));
   }
   __syncthreads();
 
-  const int n16 = lane & 15, g = lane >> 4;
-  const int steps = (2 * d + 63) / 64;
-  for (int t = 0; t < a.chunk_tiles; ++t) {
-    const int p0 = (tile0 + t) * 16;
-    if (p0 >= visible) break;
-    const int lp = p0 + n16;
-    const int phys = lp < visible ? phys_page(a.s, b, lp) : -1;
-    const int64_t rec = (int64_t)max(phys, 0) * a.heads + head;
-    const float sp = a.box_scale[rec];
-    i32x4 bx[8];
+  for (int t0 = 0; t0 < 4; t0 += TB) {
+    if (p0 + 16 * t0 >= visible) break;
+    if (t0 > 0) load_boxes(t0);
+    float best[TB][4];
 #pragma unroll
-    for (int st = 0; st < 8; ++st) {
-      if (st >= steps) break;
-      const int off = min(64 * st + 16 * g, 2 * d - 16);  // past the end: times 0 below
-      bx[st] = load16<i32x4>(a.box + rec * 2 * d + off);
-    }
-    float best[4];
+    for (int t = 0; t < TB; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) best[i] = -INFINITY;
+      for (int i = 0; i < 4; ++i) best[t][i] = -INFINITY;
     for (int ct = 0; ct < a.col_tiles; ++ct) {
-      i32x4 acc = {0, 0, 0, 0};
-      const int8_t* qc = q8 + (size_t)(ct * 16 + n16) * 2 * d;
+      const int8_t* qc = q8 + (size_t)(ct * 16 + n16) * stride;
+      i32x4 qf[S];
 #pragma unroll
-      for (int st = 0; st < 8; ++st) {
-        if (st >= steps) break;
+      for (int st = 0; st < S; ++st) {
         const int off = 64 * st + 16 * g;
-        i32x4 qv = {0, 0, 0, 0};
-        if (off < 2 * d) qv = *reinterpret_cast<const i32x4*>(qc + off);
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(bx[st], qv, acc, 0, 0, 0);
+        qf[st] = i32x4{0, 0, 0, 0};
+        if (off < 2 * d) qf[st] = *reinterpret_cast<const i32x4*>(qc + off);
       }
       const float un = unit[ct * 16 + n16];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float spi = __shfl(sp, 4 * g + i);
-        float v = score_of(un, spi, acc[i]);
-        v = v != v ? INFINITY : v;         // a page or query that has no bound comes first
-        best[i] = un < 0.0f ? best[i] : fmaxf(best[i], v);
+      for (int t = 0; t < TB; ++t) {
+        i32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int st = 0; st < S; ++st)
+          acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(bx[t][st], qf[st], acc, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float v = score_of(un, __shfl(sp, 16 * (t0 + t) + 4 * g + i), acc[i]);
+          v = v != v ? INFINITY : v;       // a page or query that has no bound comes first
+          best[t][i] = un < 0.0f ? best[t][i] : fmaxf(best[t][i], v);
+        }
       }
     }
     for (int o = 1; o < (1 << a.col_shift); o <<= 1)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) best[i] = fmaxf(best[i], __shfl_xor(best[i], o));
+      for (int t = 0; t < TB; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) best[t][i] = fmaxf(best[t][i], __shfl_xor(best[t][i], o));
     const int tt = n16 >> a.col_shift;
-    if ((n16 & ((1 << a.col_shift) - 1)) == 0 && tt < toks && p0 + 4 * g < a.row) {
-      const int64_t r = (int64_t)(row0 + tok0 + tt) * a.heads + head;
-      *reinterpret_cast<float4*>(a.score + r * a.row + p0 + 4 * g) =
-          make_float4(best[0], best[1], best[2], best[3]);
+    if ((n16 & ((1 << a.col_shift) - 1)) == 0 && tt < toks) {
+      float* out = a.score + ((int64_t)(row0 + tok0 + tt) * a.heads + head) * a.row;
+#pragma unroll
+      for (int t = 0; t < TB; ++t) {
+        const int at = p0 + 16 * (t0 + t) + 4 * g;
+        if (at < a.row)
+          *reinterpret_cast<float4*>(out + at) =
+              make_float4(best[t][0], best[t][1], best[t][2], best[t][3]);
+      }
     }
   }
 }
 
-// order-preserving integer of a score
+// order-preserving integer of a score, above 0
 __device__ __forceinline__ uint32_t score_key(float v) {
   const uint32_t u = __float_as_uint(v);
   return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-// The m best pages of a row, one workgroup a row: the m-th largest key by four 8-bit digit
-// counts from the top, then the pages above it and the lowest ones equal to it in page order.
-__global__ __launch_bounds__(256) void k_select_top(Seqs s, const float* __restrict__ score,
-                                                    int64_t row, int heads, int m, int keep_first,
-                                                    int keep_last, int32_t* __restrict__ idx) {
-  __shared__ int hist[256];
-  __shared__ int wsum[4][2];
-  __shared__ uint32_t sh_prefix;
-  __shared__ int sh_left;
+// The m best pages of a row, one workgroup a row, PT pages a thread in registers.  The m-th
+// largest key is bracketed by counting the keys at or above three values between the bounds
+// (ballots, no atomics) until a count is m or the bounds meet; then the pages above it and the
+// lowest ones equal to it are written in page order.  Bound by the rounds' latency: about ten,
+// a barrier each.
+template <int NT, int PT>
+__global__ __launch_bounds__(NT) void k_select_top(Seqs s, const float* __restrict__ score,
+                                                   int64_t row, int heads, int m, int keep_first,
+                                                   int keep_last, int32_t* __restrict__ idx) {
+  constexpr int NW = NT / 64;
+  __shared__ int cnt[2][NW][3];
+  __shared__ uint32_t ext[NW][2];
+  __shared__ int scan[NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t r = blockIdx.x, t = r / heads;
   const int b = find_seq(s, t, 1, 1, 0);
@@ -597,67 +675,154 @@ __global__ __launch_bounds__(256) void k_select_top(Seqs s, const float* __restr
   const int nv = (int)min(nv64, (int64_t)s.max_pages);
   int32_t* out = idx + r * m;
   if (nv <= m) {
-    for (int i = tid; i < m; i += 256) out[i] = i < nv ? i : -1;
+    for (int i = tid; i < m; i += NT) out[i] = i < nv ? i : -1;
     return;
   }
   const float* sc = score + r * row;
-  const auto key = [&](int p) {
-    return p < keep_first || p >= nv - keep_last ? 0xFFFFFFFFu : score_key(sc[p]);
-  };
-  uint32_t prefix = 0;
-  int left = m;                       // rank of the wanted key among those with the prefix
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    hist[tid] = 0;
-    __syncthreads();
-    for (int p = tid; p < nv; p += 256) {
-      const uint32_t k = key(p);
-      if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1);
+  const int first = tid * PT;
+  uint32_t key[PT];                       // 0: no page; kept pages have the largest one
+  uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
+#pragma unroll
+  for (int i = 0; i < PT; i += 4) {
+    float4 v = make_float4(0, 0, 0, 0);
+    if (first + i < nv) v = *reinterpret_cast<const float4*>(sc + first + i);
+    const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int p = first + i + j;
+      const bool keep = p < keep_first || p >= nv - keep_last;
+      const uint32_t k = score_key(f[j]);
+      key[i + j] = p >= nv ? 0 : keep ? 0xFFFFFFFFu : k;
+      if (p < nv && !keep) {
+        kmin = min(kmin, k);
+        kmax = max(kmax, k);
+      }
     }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    kmin = min(kmin, (uint32_t)__shfl_xor((int)kmin, o));
+    kmax = max(kmax, (uint32_t)__shfl_xor((int)kmax, o));
+  }
+  if (lane == 0) {
+    ext[wave][0] = kmin;
+    ext[wave][1] = kmax;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    kmin = min(kmin, ext[w][0]);
+    kmax = max(kmax, ext[w][1]);
+  }
+  // counts of keys >= c0, c1, c2 over the workgroup
+  int buf = 0;
+  const auto count = [&](uint32_t c0, uint32_t c1, uint32_t c2, int* n) {
+    n[0] = n[1] = n[2] = 0;
+    if constexpr (PT <= 16) {
+#pragma unroll
+      for (int i = 0; i < PT; ++i) {
+        n[0] += __popcll(__ballot(key[i] >= c0));
+        n[1] += __popcll(__ballot(key[i] >= c1));
+        n[2] += __popcll(__ballot(key[i] >= c2));
+      }
+    } else {                              // one reduction over the lanes for many keys
+#pragma unroll
+      for (int i = 0; i < PT; ++i) {
+        n[0] += key[i] >= c0;
+        n[1] += key[i] >= c1;
+        n[2] += key[i] >= c2;
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+        for (int j = 0; j < 3; ++j) n[j] += __shfl_xor(n[j], o);
+    }
+    if (lane == 0)
+#pragma unroll
+      for (int j = 0; j < 3; ++j) cnt[buf][wave][j] = n[j];
     __syncthreads();
-    // counts of the digits above this thread's
-    const int digit = 255 - tid;
-    const int c = hist[digit];
-    int incl = c;
+    n[0] = n[1] = n[2] = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+#pragma unroll
+      for (int j = 0; j < 3; ++j) n[j] += cnt[buf][w][j];
+    buf ^= 1;
+  };
+  // more than m keys are >= lo, less than m are >= hi (nv > m; the kept ones are at most m)
+  uint32_t lo = kmin, hi = kmax + 1, above = 0;       // above: take every key > above
+  int ties = 0, n[3];
+  bool exact = false;
+  count(hi, hi, hi, n);
+  int n_hi = n[0];
+  if (n_hi == m) {
+    above = hi - 1;
+    exact = true;
+  }
+  while (!exact && hi - lo > 1) {
+    const uint32_t q = max((hi - lo) >> 2, 1u);
+    const uint32_t c0 = lo + q, c1 = min(lo + 2 * q, hi), c2 = min(lo + 3 * q, hi);
+    count(c0, c1, c2, n);
+    exact = true;
+    if (n[0] == m) above = c0 - 1;
+    else if (n[1] == m) above = c1 - 1;
+    else if (n[2] == m) above = c2 - 1;
+    else exact = false;
+    if (n[0] < m) {
+      hi = c0;
+      n_hi = n[0];
+    } else if (n[1] < m) {
+      lo = c0;
+      hi = c1;
+      n_hi = n[1];
+    } else if (n[2] < m) {
+      lo = c1;
+      hi = c2;
+      n_hi = n[2];
+    } else {
+      lo = c2;
+    }
+  }
+  if (!exact) {                           // the m-th key is lo: some of those equal to it go in
+    above = lo;
+    ties = m - n_hi;
+  }
+  // ranks in page order: a thread's pages are consecutive
+  const auto before = [&](int mine) {
+    int incl = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int v = __shfl_up(incl, o);
       if (lane >= o) incl += v;
     }
-    if (lane == 63) wsum[wave][0] = incl;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) incl += wsum[w][0];
-    if (incl >= left && incl - c < left) {
-      sh_prefix = (prefix << 8) | digit;
-      sh_left = left - (incl - c);
-    }
+    if (lane == 63) scan[wave] = incl;
     __syncthreads();
-    prefix = sh_prefix;
-    left = sh_left;
+    int base = incl - mine;
+    for (int w = 0; w < wave; ++w) base += scan[w];
+    return base;
+  };
+  int eq = 0, left = 0;
+  if (ties > 0) {
+#pragma unroll
+    for (int i = 0; i < PT; ++i) eq += key[i] == above;
+    left = ties - before(eq);
   }
-  // `left` pages with exactly this key are taken, the lowest ones
-  int done = 0, eq_done = 0;
-  for (int p0 = 0; p0 < nv; p0 += 256) {
-    const int p = p0 + tid;
-    const uint32_t k = p < nv ? key(p) : 0;
-    const bool gt = p < nv && k > prefix, eq = p < nv && k == prefix;
-    const uint64_t meq = __ballot(eq), below = ((uint64_t)1 << lane) - 1;
-    __syncthreads();
-    if (lane == 0) wsum[wave][0] = __popcll(meq);
-    __syncthreads();
-    int eq_rank = eq_done + __popcll(meq & below);
-    for (int w = 0; w < wave; ++w) eq_rank += wsum[w][0];
-    const bool take = gt || (eq && eq_rank < left);
-    const uint64_t mt = __ballot(take);
-    if (lane == 0) wsum[wave][1] = __popcll(mt);
-    __syncthreads();
-    int at = done + __popcll(mt & below);
-    for (int w = 0; w < wave; ++w) at += wsum[w][1];
-    if (take && at < m) out[at] = p;
-    for (int w = 0; w < 4; ++w) {
-      eq_done += wsum[w][0];
-      done += wsum[w][1];
+  uint32_t take[(PT + 31) / 32] = {};
+  int taken = 0;
+#pragma unroll
+  for (int i = 0; i < PT; ++i) {
+    bool in = key[i] > above;
+    if (key[i] == above && left > 0 && ties > 0) {
+      in = true;
+      --left;
     }
+    take[i >> 5] |= (uint32_t)in << (i & 31);
+    taken += in;
   }
+  int at = before(taken);
+#pragma unroll
+  for (int i = 0; i < PT; ++i)
+    if ((take[i >> 5] >> (i & 31) & 1) && at < m) out[at++] = first + i;
 }
 
 // ---------------------------------------------------------------- attention
@@ -683,6 +848,16 @@ struct AttendArgs {
   float* part_ml;            // [splits][tokens * hq][2]: maximum (base 2), sum
   int tiles_token;           // selection: row tiles a (token, head) takes
 };
+
+// a row's share of a key range in which it sees no key; r: row of the (sequence, head)
+__device__ __forceinline__ void mark_empty(const AttendArgs& a, int split, int row0, int r,
+                                           int head) {
+  const int ti = r / a.group, hh = r - ti * a.group;
+  const int64_t orow = (int64_t)(row0 + ti) * a.hq + head * a.group + hh;
+  float* ml = a.part_ml + ((int64_t)split * a.tokens * a.hq + orow) * 2;
+  ml[0] = -INFINITY;
+  ml[1] = 0.0f;
+}
 
 // A few query rows (16 RT: tokens x heads of a group) against a range of keys; 4 waves take
 // every fourth step of 32 keys each, straight from memory into matrix operands, and are
@@ -758,7 +933,10 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
   } else {
     const int64_t c0 = (int64_t)split * a.chunk, c1 = c0 + a.chunk;
     if (c0 >= khi || c1 <= klo) {
-      if (a.splits > 1 || khi > klo) return;
+      if (a.splits > 1) {
+        if (tid < rows) mark_empty(a, split, row0, r0 + tid, head);
+        return;
+      }
       st0 = st1 = 0;                        // rows that see no key: zeros
     } else {
       st0 = max(c0, klo) >> 5;
@@ -992,7 +1170,8 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 4 : ND <= 4 ? 2 : 1) void k_atte
   if (k0 < khi64 && k1 > klo) {
     kbeg = (int)(max(k0, klo) / KEYS) * KEYS;
     steps = (int)cdiv(min(k1, khi64) - kbeg, KEYS);
-  } else if (a.splits > 1 || khi64 > klo) {
+  } else if (a.splits > 1) {
+    if (tid < rows) mark_empty(a, split, row0, r0 + tid, head);
     return;
   }
   const int kend = (int)min(k1, khi64);           // first key that is not this workgroup's
@@ -1305,39 +1484,46 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 4 : ND <= 4 ? 2 : 1) void k_atte
   }
 }
 
-// Joins the partial results of the key ranges, in their order: a wave a row.
-template <typename T, bool SEL>
+// Joins the partial results of the key ranges, in their order: a wave a row, 4 dimensions a
+// lane.  Ranges without a key of the row have a sum of 0 and are skipped.
+template <typename T>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t orow = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int64_t nrows = a.tokens * a.hq;
   if (orow >= nrows) return;
-  const int64_t t = orow / a.hq;
-  const int b = find_seq(a.s, t, 1, 1, 0);
-  const int64_t total = a.s.total[b];
-  const int64_t held = min(total, (int64_t)a.s.max_pages << a.s.page_shift);
-  const int64_t slot = total - (a.s.cu[b + 1] - t);
-  const int64_t hi = min(slot, held - 1);
-  const int64_t lo = a.window > 0 ? max((int64_t)0, slot - a.window + 1) : 0;
-  int c0 = 0, c1 = a.splits;
-  if constexpr (!SEL) {
-    c0 = (int)(lo / a.chunk);
-    c1 = hi < lo ? c0 : (int)(hi / a.chunk) + 1;
-  }
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + orow;
   float mm = -INFINITY;
-  for (int c = c0 + lane; c < c1; c += 64)
-    mm = fmaxf(mm, a.part_ml[((int64_t)c * nrows + orow) * 2]);
+  for (int c = lane; c < a.splits; c += 64) mm = fmaxf(mm, ml[c * nrows].x);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o));
   const float base = mm == -INFINITY ? 0.0f : mm;
   float z = 0.0f;
   f32x4 acc = {0, 0, 0, 0};
-  for (int c = c0; c < c1; ++c) {
-    const int64_t pr = (int64_t)c * nrows + orow;
-    const float f = exp2_fast(a.part_ml[pr * 2] - base);
-    z += a.part_ml[pr * 2 + 1] * f;
-    if (lane * 4 < a.d) acc += f * *reinterpret_cast<const f32x4*>(a.part_o + pr * a.d + lane * 4);
+  const int at = min(lane * 4, a.d - 4);
+  for (int c0 = 0; c0 < a.splits; c0 += 64) {
+    const float2 v = c0 + lane < a.splits ? ml[(c0 + lane) * nrows] : make_float2(-INFINITY, 0.0f);
+    const float f = exp2_fast(v.x - base);
+    uint64_t mask = __ballot(v.y != 0.0f);
+    const int some = mask != 0 ? __ffsll((unsigned long long)mask) - 1 : 0;
+    z += mask >> lane & 1 ? v.y * f : 0.0f;
+    while (mask != 0) {                     // four at a time: their loads are in flight together
+      f32x4 o[4];
+      float w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool has = mask != 0;         // past the last: one of them again, times 0
+        const int i = has ? __ffsll((unsigned long long)mask) - 1 : some;
+        mask &= mask - 1;
+        w[j] = has ? __shfl(f, i) : 0.0f;
+        o[j] = *reinterpret_cast<const f32x4*>(a.part_o + ((int64_t)(c0 + i) * nrows + orow) * a.d + at);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc += w[j] * o[j];
+    }
   }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o);
   if (lane * 4 < a.d) {
     alignas(8) T w[4];
     const float inv = 1.0f / z;
@@ -1528,10 +1714,7 @@ void launch_attend(const AttendArgs& a, const Plan& p, hipStream_t st) {
   else launch_few_rt<T, 8>(a, p, st);
   if (a.splits > 1) {
     const dim3 grid((unsigned)cdiv(a.tokens * a.hq, 4));
-    if (a.sel)
-      hipLaunchKernelGGL((k_attend_join<T, true>), grid, dim3(256), 0, st, a);
-    else
-      hipLaunchKernelGGL((k_attend_join<T, false>), grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_attend_join<T>), grid, dim3(256), 0, st, a);
   }
 }
 
@@ -1542,12 +1725,11 @@ int launch_rope(const void* x, int64_t xt, int64_t xh, void* out, int64_t ot, in
   const bool vec = r.rot % 16 == 0 && d % 16 == 0 && aligned16(x) && aligned16(out) &&
                    aligned16(r.table) && (xt | xh | ot | oh) % 8 == 0;
   const int w = vec ? 8 : 1;
-  const int64_t per = cdiv((int64_t)heads * cdiv(d, 2 * w), 256);
-  if (per > 65535 || tokens * per > kMaxBlocks) return GMM_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)tokens, (unsigned)per);
+  const int64_t items = tokens * heads * cdiv(d, 2 * w), blocks = cdiv(items, 256);
+  if (blocks > kMaxBlocks) return GMM_ERR_UNSUPPORTED;
   const auto run = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, (const T*)x, xt, xh, (T*)out, ot, oh,
-                       heads, d, pos, r);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, (const T*)x, xt, xh,
+                       (T*)out, ot, oh, (uint32_t)items, heads, d, pos, r);
   };
   if (vec && inter) run(k_rope<T, 8, true>);
   else if (vec) run(k_rope<T, 8, false>);
@@ -1645,10 +1827,15 @@ int gmm_kv_append(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
                    (!q || (aligned16(q) && aligned16(q_out) &&
                            (q_token_stride | q_head_stride | qo_token_stride | qo_head_stride) % 8 == 0));
   const int w = vec ? 8 : 1;
-  a.q_blocks = q ? (int)cdiv((int64_t)hq * (d / (2 * w)), 256) : 0;
-  a.page_blocks = (tokens / cache->page + 2 * (int64_t)seqs->batch) * cache->heads;
-  const int64_t blocks = a.page_blocks + tokens * a.q_blocks;
+  const int64_t q_items = q ? tokens * hq * (d / (2 * w)) : 0;
+  // a head's page has page * d / (8 w) units of keys: two for each of its threads
+  const int size = cache->page * d;
+  a.per = size >= 8192 ? 1 : size >= 4096 ? 2 : 4;
+  while (a.per > 1 && 256 / a.per < d / (2 * w)) a.per /= 2;
+  a.page_blocks = (tokens / cache->page + 2 * (int64_t)seqs->batch) * cdiv(cache->heads, a.per);
+  const int64_t blocks = a.page_blocks + cdiv(q_items, 256);
   if (blocks > kMaxBlocks) return GMM_ERR_UNSUPPORTED;
+  a.q_items = (uint32_t)q_items;
   const bool inter = table && interleaved;
   if (cache->dtype == GMM_BF16) launch_append<__bf16>(a, vec, inter, blocks, stream);
   else launch_append<_Float16>(a, vec, inter, blocks, stream);
@@ -1676,7 +1863,7 @@ int gmm_kv_select(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
   rc = check_heads(cache, hq);
   if (rc != GMM_OK) return rc;
   if (!cache->box || m < 1 || keep_first < 0 || keep_last < 1) return GMM_ERR_INVALID_ARG;
-  if (m > GMM_KV_MAX_KEEP) return GMM_ERR_UNSUPPORTED;
+  if (m > GMM_KV_MAX_KEEP || seqs->max_pages > GMM_KV_MAX_PAGES) return GMM_ERR_UNSUPPORTED;
   if ((int64_t)keep_first + keep_last > m) return GMM_ERR_INVALID_ARG;
   if (tokens == 0) return GMM_OK;
   if (!q || !idx) return GMM_ERR_INVALID_ARG;
@@ -1696,19 +1883,25 @@ int gmm_kv_select(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
   a.row = score_row(seqs->max_pages);
   const int per = 16 >> a.col_shift;
   const int64_t items = tokens / per + seqs->batch;
-  const int64_t tiles = cdiv(seqs->max_pages, 16);
-  a.chunk_tiles = 4;
-  a.parts = (int)cdiv(tiles, 4 * a.chunk_tiles);
-  const int64_t blocks = a.parts * items * cache->heads;
-  if (blocks > kMaxBlocks || tokens * cache->heads > kMaxBlocks) return GMM_ERR_UNSUPPORTED;
-  const size_t lds = (size_t)a.col_tiles * 16 * (2 * a.d + 4);
-  const dim3 grid((unsigned)blocks);
-  if (cache->dtype == GMM_BF16)
-    hipLaunchKernelGGL((k_select_score<__bf16>), grid, dim3(256), lds, stream, a);
-  else
-    hipLaunchKernelGGL((k_select_score<_Float16>), grid, dim3(256), lds, stream, a);
-  hipLaunchKernelGGL(k_select_top, dim3((unsigned)(tokens * cache->heads)), dim3(256), 0, stream,
-                     a.s, a.score, a.row, a.heads, m, keep_first, keep_last, idx);
+  a.parts = (int)cdiv(seqs->max_pages, 256);
+  const int64_t blocks = a.parts * items * cache->heads, rows = tokens * cache->heads;
+  // a row's workgroup has up to 1024 threads
+  if (blocks > kMaxBlocks || rows > kMaxBlocks / 4) return GMM_ERR_UNSUPPORTED;
+  const size_t lds = (size_t)a.col_tiles * 16 * (2 * a.d + 16 + 4);
+  const auto run_score = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), lds, stream, a);
+  };
+  const bool bf = cache->dtype == GMM_BF16;
+  if (a.d <= 64) bf ? run_score(k_select_score<__bf16, 2>) : run_score(k_select_score<_Float16, 2>);
+  else if (a.d <= 128) bf ? run_score(k_select_score<__bf16, 4>) : run_score(k_select_score<_Float16, 4>);
+  else bf ? run_score(k_select_score<__bf16, 8>) : run_score(k_select_score<_Float16, 8>);
+  const auto run_top = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(threads), 0, stream, a.s, a.score,
+                       a.row, a.heads, m, keep_first, keep_last, idx);
+  };
+  if (seqs->max_pages <= 2048) run_top(k_select_top<256, 8>, 256);
+  else if (seqs->max_pages <= 16384) run_top(k_select_top<1024, 16>, 1024);
+  else run_top(k_select_top<1024, 64>, 1024);
   return launch_status();
 }
 

@@ -11,6 +11,8 @@ from __future__ import annotations
 import ctypes
 import math
 
+import torch
+
 import paper_2606_10896_amd as _base
 
 GMM_F32 = 0
@@ -58,12 +60,37 @@ def bind(lib):
         fn.restype = ctypes.c_size_t if name == "gmm_kv_workspace_bytes" else ctypes.c_int
 
 
+_CODES = {torch.float32: GMM_F32, torch.bfloat16: GMM_BF16, torch.float16: GMM_F16}
+
+
 def _dtype(t):
-    import torch
-    code = {torch.float32: GMM_F32, torch.bfloat16: GMM_BF16, torch.float16: GMM_F16}.get(t)
+    code = _CODES.get(t)
     if code is None:
         raise TypeError(f"{t} is not a type of these calls")
     return code
+
+
+# A step of a single token is a few microseconds on the GPU: the binding keeps its own share of
+# a call small (addresses as plain integers, one look at a tensor's strides, the stream's handle
+# without a Stream object).
+
+def _stream(stream, t):
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
+
+
+def _flat(t, dtype, numel, name):
+    """Address of a contiguous CUDA tensor of at least numel elements."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous {dtype} CUDA tensor")
+    if t.numel() < numel:
+        raise ValueError(f"{name} holds {t.numel()} elements, {numel} needed")
+    return t.data_ptr()
+
+
+def _ws(ws):
+    return (0, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 class KVCache:
@@ -72,7 +99,6 @@ class KVCache:
     [pages, heads] fp32 for gmm_kv_select, or None for a cache without boxes."""
 
     def __init__(self, k, v, box=None, box_scale=None):
-        import torch
         dev = _base._dev
         pages, heads, page, d = k.shape
         if k.dtype not in (torch.bfloat16, torch.float16):
@@ -91,6 +117,7 @@ class KVCache:
         at = lambda t: None if t is None else t.data_ptr()
         self._c = _CCache(at(k), at(v), at(box), at(box_scale), pages, heads, page, d,
                           _dtype(k.dtype))
+        self._ref = ctypes.byref(self._c)
 
     def box_values(self):
         """The boxes as numbers, fp32 [pages, heads, 2, d]: upper, then lower bounds."""
@@ -99,7 +126,6 @@ class KVCache:
 
 def kv_cache(pages, heads, page, d, dtype=None, boxes=True, device="cuda"):
     """An empty KVCache (bfloat16 unless dtype says otherwise)."""
-    import torch
     dtype = torch.bfloat16 if dtype is None else dtype
     k = torch.zeros(pages, heads, page, d, dtype=dtype, device=device)
     v = torch.zeros(pages, heads, d, page, dtype=dtype, device=device)
@@ -131,56 +157,55 @@ def rope_frequencies(rot, base=10000.0, factor=1.0, trained=None, slow=1.0, fast
 def gmm_rope_table(freq, table, scale=1.0, stream=None):
     """Fills table [positions, rot] fp32 (rot/2 cosines, then rot/2 sines of every position,
     times scale) from the frequencies freq [rot/2] (fp64 CUDA tensor)."""
-    import torch
     positions, rot = table.shape
     if rot % 2:
         raise ValueError("table must hold an even number of columns")
     rc = _base.load_library().gmm_rope_table(
         _base._ptr(_base._dev(freq, torch.float64, "freq", rot // 2)), rot // 2, float(scale),
-        positions, _base._ptr(_base._dev(table, torch.float32, "table")), _base._stream(stream))
+        positions, _base._ptr(_base._dev(table, torch.float32, "table")), _stream(stream, table))
     _base._check("gmm_rope_table", rc)
 
 
-def _rows(t, dtype, shape, name):
-    """(pointer, token stride, head stride) of a CUDA tensor [tokens, heads, d] whose rows are
+def _rows(t, dtype, tokens, heads, d, name):
+    """(address, token stride, head stride) of a CUDA tensor [tokens, heads, d] whose rows are
     contiguous."""
-    import torch
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype):
         raise TypeError(f"{name} must be a {dtype} CUDA tensor")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have the shape {list(shape)}, has {list(t.shape)}")
-    if t.stride(2) != 1 and t.numel():
+    if t.shape != (tokens, heads, d):
+        raise ValueError(f"{name} must have the shape {[tokens, heads, d]}, has {list(t.shape)}")
+    st = t.stride()
+    if st[2] != 1 and t.numel():
         raise TypeError(f"{name} must have contiguous rows")
-    return ctypes.c_void_p(t.data_ptr()), t.stride(0), t.stride(1)
+    return t.data_ptr(), st[0], st[1]
 
 
 def gmm_rope(x, pos, table, out, interleaved=False, inverse=False, stream=None):
     """Rotates x [tokens, heads, d] by the positions pos [tokens] int32 into out (which may be x):
     the first rot = table.shape[1] dimensions in pairs (i, i + rot/2), or (2i, 2i + 1) if
     interleaved.  inverse applies the transposed rotation: the gradient."""
-    import torch
     tokens, heads, d = x.shape
-    xs = _rows(x, x.dtype, x.shape, "x")
+    dt = x.dtype
     rc = _base.load_library().gmm_rope(
-        *xs, *_rows(out, x.dtype, x.shape, "out"), tokens, heads, d, _dtype(x.dtype),
-        _base._ptr(_base._dev(pos, torch.int32, "pos", tokens)),
-        _base._ptr(_base._dev(table, torch.float32, "table")), table.shape[0], table.shape[1],
-        int(interleaved), int(inverse), _base._stream(stream))
-    _base._check("gmm_rope", rc)
+        *_rows(x, dt, tokens, heads, d, "x"), *_rows(out, dt, tokens, heads, d, "out"), tokens,
+        heads, d, _dtype(dt), _flat(pos, torch.int32, tokens, "pos"),
+        _flat(table, torch.float32, 0, "table"), table.shape[0], table.shape[1],
+        1 if interleaved else 0, 1 if inverse else 0, _stream(stream, x))
+    if rc:
+        raise _base.GMMError("gmm_rope", rc)
 
 
 def _batch(cu, total, pages):
-    import torch
     batch = total.numel()
-    _base._dev(cu, torch.int32, "cu", batch + 1)
-    _base._dev(total, torch.int32, "total")
-    if not (isinstance(pages, torch.Tensor) and pages.is_cuda and pages.dtype == torch.int32 and
+    if not (isinstance(pages, torch.Tensor) and pages.is_cuda and pages.dtype is torch.int32 and
             pages.dim() == 2 and (pages.stride(1) == 1 or pages.shape[1] == 1)):
         raise TypeError("pages must be an int32 CUDA tensor [batch, max_pages] with contiguous rows")
-    if pages.shape[0] != batch:
-        raise ValueError(f"pages has {pages.shape[0]} rows for {batch} sequences")
-    stride = max(pages.stride(0), pages.shape[1]) if batch == 1 else pages.stride(0)
-    return _CBatch(cu.data_ptr(), total.data_ptr(), pages.data_ptr(), batch, pages.shape[1], stride)
+    rows, width = pages.shape
+    if rows != batch:
+        raise ValueError(f"pages has {rows} rows for {batch} sequences")
+    stride = max(pages.stride(0), width) if batch == 1 else pages.stride(0)
+    return ctypes.byref(_CBatch(_flat(cu, torch.int32, batch + 1, "cu"),
+                                _flat(total, torch.int32, batch, "total"), pages.data_ptr(), batch,
+                                width, stride))
 
 
 def gmm_kv_append(cache, k, v, cu, total, pages, pos=None, table=None, q=None, q_out=None,
@@ -188,39 +213,34 @@ def gmm_kv_append(cache, k, v, cu, total, pages, pos=None, table=None, q=None, q
     """Stores the new tokens' keys (rotated if a table is given) and values [tokens, heads, d] in
     the cache and renews the boxes of their pages; rotates q [tokens, hq, d] into q_out.  pos
     [tokens] int32: rotation positions, a token's slot in its sequence if None."""
-    import torch
     tokens = k.shape[0]
-    dt, shape = cache.k.dtype, (tokens, cache.heads, cache.d)
-    ks, vs = _rows(k, dt, shape, "k"), _rows(v, dt, shape, "v")
-    none = (None, 0, 0)
-    qs = qo = none
+    dt, heads, d = cache.k.dtype, cache.heads, cache.d
+    qs = qo = (0, 0, 0)
     hq = 0
     if q is not None:
         hq = q.shape[1]
-        qs = _rows(q, dt, (tokens, hq, cache.d), "q")
-        qo = _rows(q_out, dt, (tokens, hq, cache.d), "q_out")
-    if pos is not None:
-        _base._dev(pos, torch.int32, "pos", tokens)
+        qs = _rows(q, dt, tokens, hq, d, "q")
+        qo = _rows(q_out, dt, tokens, hq, d, "q_out")
+    tb = (0, 0, 0)
     if table is not None:
-        _base._dev(table, torch.float32, "table")
-    b = _batch(cu, total, pages)
+        tb = _flat(table, torch.float32, 0, "table"), table.shape[0], table.shape[1]
     rc = _base.load_library().gmm_kv_append(
-        ctypes.byref(cache._c), ctypes.byref(b), tokens, *ks, *vs, _base._ptr(pos),
-        _base._ptr(table), 0 if table is None else table.shape[0],
-        0 if table is None else table.shape[1], int(interleaved), *qs, *qo, hq,
-        _base._stream(stream))
-    _base._check("gmm_kv_append", rc)
+        cache._ref, _batch(cu, total, pages), tokens, *_rows(k, dt, tokens, heads, d, "k"),
+        *_rows(v, dt, tokens, heads, d, "v"),
+        0 if pos is None else _flat(pos, torch.int32, tokens, "pos"), *tb,
+        1 if interleaved else 0, *qs, *qo, hq, _stream(stream, k))
+    if rc:
+        raise _base.GMMError("gmm_kv_append", rc)
 
 
 def kv_workspace_bytes(cache, tokens, hq, batch, max_pages):
     """Workspace size of gmm_kv_select and gmm_kv_attend."""
     return int(_base.load_library().gmm_kv_workspace_bytes(
-        ctypes.byref(cache._c), int(tokens), int(hq), int(batch), int(max_pages)))
+        cache._ref, int(tokens), int(hq), int(batch), int(max_pages)))
 
 
 def kv_workspace(cache, tokens, hq, batch, max_pages):
     """A workspace tensor (uint8) for calls with up to these sizes."""
-    import torch
     nb = kv_workspace_bytes(cache, tokens, hq, batch, max_pages)
     if nb == 0:
         raise _base.GMMError("gmm_kv_workspace_bytes", _base.GMM_ERR_UNSUPPORTED)
@@ -230,18 +250,15 @@ def kv_workspace(cache, tokens, hq, batch, max_pages):
 def gmm_kv_select(cache, q, cu, total, pages, idx, ws, keep_first=1, keep_last=1, stream=None):
     """The m = idx.shape[2] best pages of every new token and cache head into idx
     [tokens, heads, m] int32 (indexes into the page table, ascending, -1 at the end)."""
-    import torch
     tokens, hq = q.shape[:2]
-    qs = _rows(q, cache.k.dtype, (tokens, hq, cache.d), "q")
-    _base._dev(idx, torch.int32, "idx")
-    if idx.dim() != 3 or tuple(idx.shape[:2]) != (tokens, cache.heads):
+    if idx.dim() != 3 or idx.shape[0] != tokens or idx.shape[1] != cache.heads:
         raise ValueError(f"idx must be [{tokens}, {cache.heads}, m]")
-    b = _batch(cu, total, pages)
     rc = _base.load_library().gmm_kv_select(
-        ctypes.byref(cache._c), ctypes.byref(b), tokens, *qs, hq, idx.shape[2], int(keep_first),
-        int(keep_last), _base._ptr(idx), _base._ptr(ws), ws.numel() if ws is not None else 0,
-        _base._stream(stream))
-    _base._check("gmm_kv_select", rc)
+        cache._ref, _batch(cu, total, pages), tokens, *_rows(q, cache.k.dtype, tokens, hq, cache.d, "q"),
+        hq, idx.shape[2], keep_first, keep_last, _flat(idx, torch.int32, 0, "idx"), *_ws(ws),
+        _stream(stream, q))
+    if rc:
+        raise _base.GMMError("gmm_kv_select", rc)
 
 
 def gmm_kv_attend(cache, q, cu, total, pages, out, ws, lse=None, scale=None, window=0, sel=None,
@@ -249,23 +266,18 @@ def gmm_kv_attend(cache, q, cu, total, pages, out, ws, lse=None, scale=None, win
     """Attention of the new tokens' queries q [tokens, hq, d] over their sequences' keys (causal;
     the last `window` keys if window > 0; the pages listed in sel [tokens, heads, m] if given)
     into out [tokens, hq, d] and lse [tokens, hq] fp32.  scale is 1/sqrt(d) if None."""
-    import torch
     tokens, hq = q.shape[:2]
-    shape = (tokens, hq, cache.d)
-    qs = _rows(q, cache.k.dtype, shape, "q")
-    _base._dev(out, cache.k.dtype, "out", tokens * hq * cache.d)
-    if lse is not None:
-        _base._dev(lse, torch.float32, "lse", tokens * hq)
-    m = 0
+    dt, d = cache.k.dtype, cache.d
+    sp, m = 0, 0
     if sel is not None:
-        _base._dev(sel, torch.int32, "sel")
-        if sel.dim() != 3 or tuple(sel.shape[:2]) != (tokens, cache.heads):
+        sp, m = _flat(sel, torch.int32, 0, "sel"), sel.shape[-1]
+        if sel.dim() != 3 or sel.shape[0] != tokens or sel.shape[1] != cache.heads:
             raise ValueError(f"sel must be [{tokens}, {cache.heads}, m]")
-        m = sel.shape[2]
-    b = _batch(cu, total, pages)
     rc = _base.load_library().gmm_kv_attend(
-        ctypes.byref(cache._c), ctypes.byref(b), tokens, *qs, hq,
-        1.0 / math.sqrt(cache.d) if scale is None else float(scale), int(window), _base._ptr(sel),
-        m, _base._ptr(out), _base._ptr(lse), _base._ptr(ws), ws.numel() if ws is not None else 0,
-        _base._stream(stream))
-    _base._check("gmm_kv_attend", rc)
+        cache._ref, _batch(cu, total, pages), tokens, *_rows(q, dt, tokens, hq, d, "q"), hq,
+        1.0 / math.sqrt(d) if scale is None else scale, window, sp, m,
+        _flat(out, dt, tokens * hq * d, "out"),
+        0 if lse is None else _flat(lse, torch.float32, tokens * hq, "lse"), *_ws(ws),
+        _stream(stream, q))
+    if rc:
+        raise _base.GMMError("gmm_kv_attend", rc)
