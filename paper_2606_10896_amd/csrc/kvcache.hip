@@ -88,6 +88,13 @@ __device__ __forceinline__ typename Vec8<T>::type load_row8(const T* p, int vec)
 
 __host__ __device__ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Barrier for what goes through LDS: unlike __syncthreads it does not wait for global stores.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // ---------------------------------------------------------------- sequences
 // The tables are read in the constant address space: nothing writes them while a kernel runs,
 // and loads at wave-uniform addresses go through the scalar cache.
@@ -105,15 +112,23 @@ struct Seqs {
 
 // Work items are numbered over all sequences without a table made beforehand: sequence b's
 // items start at first(b) = floor(cu[b] mul / div) + slack b, which leaves room for
-// ceil(n mul / div) items (slack 1), or one more (slack 2), for its n tokens.  The sequence of
-// an item is the last b with first(b) <= item: a search by the whole wave, 64 sequences a step.
-__device__ __forceinline__ int64_t first_item(const Seqs& s, int b, int mul, int div, int slack) {
-  return (int64_t)s.cu[b] * mul / div + (int64_t)slack * b;
+// ceil(n mul / div) items (slack 1), or one more (slack 2), for its n tokens; with slack 2 at
+// min(first(b), cu[b]), as a token makes at most one item.  The sequence of an item is the last b
+// with first(b) <= item: a search by the whole wave, 64 sequences a step.
+__device__ __forceinline__ int64_t first_of(int64_t row0, int b, int mul, int div, int slack) {
+  const int64_t f = row0 * mul / div + (int64_t)slack * b;
+  return slack == 2 ? min(f, row0) : f;
 }
-__device__ __forceinline__ int find_seq(const Seqs& s, int64_t item, int mul, int div, int slack) {
+__device__ __forceinline__ int64_t first_item(const Seqs& s, int b, int mul, int div, int slack) {
+  return first_of(s.cu[b], b, mul, div, slack);
+}
+struct Seq {
+  int b, row0, n, total;     // index, first row, new tokens, keys with them
+};
+__device__ __forceinline__ Seq find_seq(const Seqs& s, int64_t item, int mul, int div, int slack) {
   int lo = 0, hi = s.batch;            // the answer is in [lo, hi)
   const int lane = threadIdx.x & 63;
-  while (hi - lo > 1) {
+  while (hi - lo > 64) {
     const int step = (hi - lo + 63) / 64;
     const int b = lo + lane * step;
     const bool in = b < hi && first_item(s, b, mul, div, slack) <= item;
@@ -121,7 +136,23 @@ __device__ __forceinline__ int find_seq(const Seqs& s, int64_t item, int mul, in
     lo += (cnt > 0 ? cnt - 1 : 0) * step;
     hi = min(hi, lo + step);
   }
-  return __builtin_amdgcn_readfirstlane(lo);
+  Seq q;
+  if (hi - lo == 1) {
+    q.b = __builtin_amdgcn_readfirstlane(lo);
+    q.row0 = s.cu[q.b];
+    q.n = s.cu[q.b + 1] - q.row0;
+    q.total = s.total[q.b];
+  } else {                             // a sequence a lane: its numbers come along
+    const int b = min(lo + lane, hi - 1);
+    const int row0 = s.cu[b], next = s.cu[b + 1], total = s.total[b];
+    const bool in = lo + lane < hi && first_of(row0, b, mul, div, slack) <= item;
+    const int i = max(__popcll(__ballot(in)) - 1, 0);
+    q.b = __builtin_amdgcn_readfirstlane(lo) + i;
+    q.row0 = __builtin_amdgcn_readlane(row0, i);
+    q.n = __builtin_amdgcn_readlane(next, i) - q.row0;
+    q.total = __builtin_amdgcn_readlane(total, i);
+  }
+  return q;
 }
 
 // physical page of a sequence's logical page, -1 if there is none
@@ -201,13 +232,11 @@ template <typename T, int W, bool INTER>
 __device__ __forceinline__ void rotate_unit(UnitV<T, W>& v, int pair, int pos, const RopeShape& r) {
 #pragma clang fp contract(off)
   if (pair < 0 || pos < 0) return;
-  UnitV<float, W> cs;                       // cosines, then sines
+  UnitV<float, W> cs = UnitV<float, W>(__builtin_nanf(""));      // cosines, then sines
   if (pos < r.positions) {
     const float* row = r.table + (int64_t)pos * r.rot + pair;
     load_run<float, W>(row, cs, 0);
     load_run<float, W>(row + (r.rot >> 1), cs, W);
-  } else {
-    cs = UnitV<float, W>(__builtin_nanf(""));
   }
 #pragma unroll
   for (int i = 0; i < W; ++i) {
@@ -310,7 +339,7 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
       p = a.pos[t];
     } else {
       // the sequence of the wave's first row, then of this thread's
-      int b = find_seq(a.s, __builtin_amdgcn_readfirstlane(t), 1, 1, 0);
+      int b = find_seq(a.s, __builtin_amdgcn_readfirstlane(t), 1, 1, 0).b;
       while (a.s.cu[b + 1] <= (int)t) ++b;
       p = a.s.total[b] - (a.s.cu[b + 1] - (int)t);
     }
@@ -331,12 +360,12 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
   const bool live = head < a.heads;
   const int64_t item = blockIdx.x / head_blocks;
   const int P = a.page, d = a.d;
-  const int b = find_seq(a.s, item, 1, P, 2);
-  const int row0 = a.s.cu[b], n = a.s.cu[b + 1] - row0, total = a.s.total[b];
+  const Seq sq = find_seq(a.s, item, 1, P, 2);
+  const int b = sq.b, row0 = sq.row0, n = sq.n, total = sq.total;
   if (n <= 0) return;
   const int64_t s0l = (int64_t)total - n;
   const int s0 = s0l < 0 ? 0 : (int)s0l;                 // first new slot that exists
-  const int64_t lp64 = (s0 >> a.s.page_shift) + (item - first_item(a.s, b, 1, P, 2));
+  const int64_t lp64 = (s0 >> a.s.page_shift) + (item - first_of(row0, b, 1, P, 2));
   if ((lp64 << a.s.page_shift) >= total) return;
   const int lp = (int)lp64;
   const int phys = phys_page(a.s, b, lp);
@@ -346,38 +375,6 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
   const int begin = max(0, s0 - first);                  // new keys: begin .. filled - 1
   const int64_t ph = (int64_t)phys * a.heads + (live ? head : 0);
   const int64_t in0 = row0 + ((int64_t)first - s0l);     // input row of the page's slot 0
-
-  // values first, their stores need not be waited for: 8 slots x 8 dimensions a thread, slots
-  // fastest over the lanes, so that a dimension's run of slots is written in whole lines
-  {
-    T* cvp = (T*)a.cv + ph * d * P;
-    const T* vin = (const T*)a.v + (int64_t)(live ? head : 0) * a.vh;
-    const int g0 = begin >> 3, ng = ((filled + 7) >> 3) - g0, nc = d >> 3;
-    for (int i = tid; live && i < ng * nc; i += threads) {
-      const int c = i / ng, sg = (g0 + i - c * ng) << 3;
-      V8 blk[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int s = min(max(sg + j, begin), filled - 1);      // rows outside are not stored
-        blk[j] = load_row8(vin + (in0 + s) * a.vt + c * 8, a.v_vec);
-      }
-      const bool whole = sg >= begin && sg + 8 <= filled;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        T* dst = cvp + (int64_t)(c * 8 + e) * P + sg;
-        if (whole) {
-          V8 col;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) col[j] = blk[j][e];
-          *reinterpret_cast<uint4*>(dst) = __builtin_bit_cast(uint4, col);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (sg + j >= begin && sg + j < filled) dst[j] = blk[j][e];
-        }
-      }
-    }
-  }
 
   // keys
   T* ckp = (T*)a.ck + ph * P * d;
@@ -418,6 +415,39 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
       }
     }
   }
+
+  // values: 8 slots x 8 dimensions a thread, slots fastest over the lanes, so that a dimension's
+  // run of slots is written in whole lines
+  {
+    T* cvp = (T*)a.cv + ph * d * P;
+    const T* vin = (const T*)a.v + (int64_t)(live ? head : 0) * a.vh;
+    const int g0 = begin >> 3, ng = ((filled + 7) >> 3) - g0, blocks = live ? ng * (d >> 3) : 0;
+    for (int i = tid; i < blocks; i += threads) {
+      const int c = i / ng, sg = (g0 + i - c * ng) << 3;
+      V8 blk[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        blk[j] = V8((T)0.0f);
+        if (sg + j >= begin && sg + j < filled)
+          blk[j] = load_row8(vin + (in0 + sg + j) * a.vt + c * 8, a.v_vec);
+      }
+      const bool whole = sg >= begin && sg + 8 <= filled;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        T* dst = cvp + (int64_t)(c * 8 + e) * P + sg;
+        if (whole) {
+          V8 col;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) col[j] = blk[j][e];
+          *reinterpret_cast<uint4*>(dst) = __builtin_bit_cast(uint4, col);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (sg + j >= begin && sg + j < filled) dst[j] = blk[j][e];
+        }
+      }
+    }
+  }
   if (!a.box) return;
 
   // box: the keys are of type T, so their bounds are kept in T without rounding; a row of 2 d
@@ -435,7 +465,7 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint64_t any = __ballot(bad);
   if (lane == 0) wbad[wave] = any != 0;
-  __syncthreads();
+  lds_barrier();
   const int rounds = (2 * d + threads - 1) / threads;
   float m = 0.0f;
   for (int r = 0; r < rounds; ++r) {
@@ -450,7 +480,7 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
   if (lane == 0) wmax[wave] = m;
-  __syncthreads();
+  lds_barrier();
   const int w0 = hsub * (threads >> 6);
   int any_bad = 0;
   for (int w = w0; w < w0 + (threads >> 6); ++w) {
@@ -482,7 +512,8 @@ struct SelectArgs {
   int col_tiles;             // 16-column tiles a token takes (1 unless group > 16)
   float* score;              // [tokens * heads][row]
   int64_t row;
-  int parts;                 // workgroups (256 pages each) a row of tiles takes
+  int parts;                 // workgroups a row of tiles takes
+  int rounds;                // of 256 pages each
 };
 
 __device__ __forceinline__ float score_of(float query_unit, float page_unit, int dot) {
@@ -505,15 +536,15 @@ __global__ __launch_bounds__(256) void k_select_score(SelectArgs a) {
   const int part_no = blockIdx.x % a.parts;
   const int head = blockIdx.x / a.parts % a.heads;
   const int64_t item = blockIdx.x / a.parts / a.heads;
-  const int b = find_seq(a.s, item, 1, per, 1);
-  const int row0 = a.s.cu[b], n = a.s.cu[b + 1] - row0;
-  const int tok0 = (int)(item - first_item(a.s, b, 1, per, 1)) * per;
+  const Seq sq = find_seq(a.s, item, 1, per, 1);
+  const int b = sq.b, row0 = sq.row0, n = sq.n;
+  const int tok0 = (int)(item - first_of(row0, b, 1, per, 1)) * per;
   if (tok0 >= n) return;
   const int toks = min(per, n - tok0);
-  const int64_t total = min((int64_t)a.s.total[b], (int64_t)a.s.max_pages << a.s.page_shift);
-  const int64_t last = min(total - 1, (int64_t)a.s.total[b] - n + tok0 + toks - 1);
+  const int64_t total = min((int64_t)sq.total, (int64_t)a.s.max_pages << a.s.page_shift);
+  const int64_t last = min(total - 1, (int64_t)sq.total - n + tok0 + toks - 1);
   const int visible = last < 0 ? 0 : (int)(last >> a.s.page_shift) + 1;
-  if (part_no * 256 >= visible) return;
+  if (part_no * a.rounds * 256 >= visible) return;
 
   // queries: 16 threads a column, runs of 8 dimensions part, part + 16
   const int d = a.d, cols = a.col_tiles * 16, stride = 2 * d + 16;
@@ -575,10 +606,13 @@ __global__ __launch_bounds__(256) void k_select_score(SelectArgs a) {
   load_column(tid >> 4);
 
   // this wave's pages, one a lane
-  const int p0 = (part_no * 4 + wave) * 64;
-  const int lp = p0 + lane;
-  const int phys = lp < visible ? phys_page(a.s, b, lp) : -1;
-  const float sp = a.box_scale[(int64_t)max(phys, 0) * a.heads + head];
+  int p0 = 0, phys = -1;
+  float sp = 0.0f;
+  const auto take_pages = [&](int round) {
+    p0 = ((part_no * a.rounds + round) * 4 + wave) * 64;
+    phys = p0 + lane < visible ? phys_page(a.s, b, p0 + lane) : -1;
+    sp = a.box_scale[(int64_t)max(phys, 0) * a.heads + head];
+  };
   const int n16 = lane & 15, g = lane >> 4;
   i32x4 bx[TB][S];
   const auto load_boxes = [&](int t0) {
@@ -590,6 +624,7 @@ __global__ __launch_bounds__(256) void k_select_score(SelectArgs a) {
         bx[t][st] = load16<i32x4>(a.box + rec * 2 * d + min(64 * st + 16 * g, 2 * d - 16));
     }
   };
+  take_pages(0);
   if (p0 < visible) load_boxes(0);
   for (int c0 = 0; c0 < cols; c0 += 16) {
     if (c0 > 0) load_column(c0 + (tid >> 4));
@@ -597,52 +632,56 @@ __global__ __launch_bounds__(256) void k_select_score(SelectArgs a) {
   }
   __syncthreads();
 
-  for (int t0 = 0; t0 < 4; t0 += TB) {
-    if (p0 + 16 * t0 >= visible) break;
-    if (t0 > 0) load_boxes(t0);
-    float best[TB][4];
-#pragma unroll
-    for (int t = 0; t < TB; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) best[t][i] = -INFINITY;
-    for (int ct = 0; ct < a.col_tiles; ++ct) {
-      const int8_t* qc = q8 + (size_t)(ct * 16 + n16) * stride;
-      i32x4 qf[S];
-#pragma unroll
-      for (int st = 0; st < S; ++st) {
-        const int off = 64 * st + 16 * g;
-        qf[st] = i32x4{0, 0, 0, 0};
-        if (off < 2 * d) qf[st] = *reinterpret_cast<const i32x4*>(qc + off);
-      }
-      const float un = unit[ct * 16 + n16];
-#pragma unroll
-      for (int t = 0; t < TB; ++t) {
-        i32x4 acc = {0, 0, 0, 0};
-#pragma unroll
-        for (int st = 0; st < S; ++st)
-          acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(bx[t][st], qf[st], acc, 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float v = score_of(un, __shfl(sp, 16 * (t0 + t) + 4 * g + i), acc[i]);
-          v = v != v ? INFINITY : v;       // a page or query that has no bound comes first
-          best[t][i] = un < 0.0f ? best[t][i] : fmaxf(best[t][i], v);
-        }
-      }
-    }
-    for (int o = 1; o < (1 << a.col_shift); o <<= 1)
+  for (int round = 0; round < a.rounds; ++round) {
+    if (round > 0) take_pages(round);
+    if (p0 >= visible) break;
+    for (int t0 = 0; t0 < 4; t0 += TB) {
+      if (p0 + 16 * t0 >= visible) break;
+      if (t0 > 0 || round > 0) load_boxes(t0);
+      float best[TB][4];
 #pragma unroll
       for (int t = 0; t < TB; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) best[t][i] = fmaxf(best[t][i], __shfl_xor(best[t][i], o));
-    const int tt = n16 >> a.col_shift;
-    if ((n16 & ((1 << a.col_shift) - 1)) == 0 && tt < toks) {
-      float* out = a.score + ((int64_t)(row0 + tok0 + tt) * a.heads + head) * a.row;
+        for (int i = 0; i < 4; ++i) best[t][i] = -INFINITY;
+      for (int ct = 0; ct < a.col_tiles; ++ct) {
+        const int8_t* qc = q8 + (size_t)(ct * 16 + n16) * stride;
+        i32x4 qf[S];
 #pragma unroll
-      for (int t = 0; t < TB; ++t) {
-        const int at = p0 + 16 * (t0 + t) + 4 * g;
-        if (at < a.row)
-          *reinterpret_cast<float4*>(out + at) =
-              make_float4(best[t][0], best[t][1], best[t][2], best[t][3]);
+        for (int st = 0; st < S; ++st) {
+          const int off = 64 * st + 16 * g;
+          qf[st] = i32x4{0, 0, 0, 0};
+          if (off < 2 * d) qf[st] = *reinterpret_cast<const i32x4*>(qc + off);
+        }
+        const float un = unit[ct * 16 + n16];
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+          i32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+          for (int st = 0; st < S; ++st)
+            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(bx[t][st], qf[st], acc, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float v = score_of(un, __shfl(sp, 16 * (t0 + t) + 4 * g + i), acc[i]);
+            v = v != v ? INFINITY : v;       // a page or query that has no bound comes first
+            best[t][i] = un < 0.0f ? best[t][i] : fmaxf(best[t][i], v);
+          }
+        }
+      }
+      for (int o = 1; o < (1 << a.col_shift); o <<= 1)
+#pragma unroll
+        for (int t = 0; t < TB; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) best[t][i] = fmaxf(best[t][i], __shfl_xor(best[t][i], o));
+      const int tt = n16 >> a.col_shift;
+      if ((n16 & ((1 << a.col_shift) - 1)) == 0 && tt < toks) {
+        float* out = a.score + ((int64_t)(row0 + tok0 + tt) * a.heads + head) * a.row;
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+          const int at = p0 + 16 * (t0 + t) + 4 * g;
+          if (at < a.row)
+            *reinterpret_cast<float4*>(out + at) =
+                make_float4(best[t][0], best[t][1], best[t][2], best[t][3]);
+        }
       }
     }
   }
@@ -669,8 +708,8 @@ __global__ __launch_bounds__(NT) void k_select_top(Seqs s, const float* __restri
   __shared__ int scan[NW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t r = blockIdx.x, t = r / heads;
-  const int b = find_seq(s, t, 1, 1, 0);
-  const int64_t slot = (int64_t)s.total[b] - (s.cu[b + 1] - t);
+  const Seq sq = find_seq(s, t, 1, 1, 0);
+  const int64_t slot = (int64_t)sq.total - (sq.row0 + sq.n - t);
   const int64_t nv64 = slot < 0 ? 0 : (slot >> s.page_shift) + 1;
   const int nv = (int)min(nv64, (int64_t)s.max_pages);
   int32_t* out = idx + r * m;
@@ -859,18 +898,20 @@ __device__ __forceinline__ void mark_empty(const AttendArgs& a, int split, int r
   ml[1] = 0.0f;
 }
 
-// A few query rows (16 RT: tokens x heads of a group) against a range of keys; 4 waves take
-// every fourth step of 32 keys each, straight from memory into matrix operands, and are
-// joined at the end.  Every byte of the cache is read by one wave once, so LDS would only add
-// a trip; the next step's 16 KB (d = 128) are in flight while one is computed.  Bound by the
-// cache's bytes.
-template <typename T, int NS, int RT, bool SEL>
-__global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
+// A few query rows (16 RT: tokens x heads of a group) against a range of keys; the NW waves take
+// every NW-th step of 32 keys each, straight from memory into matrix operands, and are joined at
+// the end.  Every byte of the cache is read by one wave once, so LDS would only add a trip.  The
+// page numbers of 64 steps are one load, a lane a step; while a step is computed the next one's
+// operands are in flight (16 KB at d = 128) where registers allow it.  Bound by the cache's bytes,
+// for short contexts by the chain of loads: sequence, page numbers, keys.
+template <typename T, int NS, int RT, bool SEL, int NW>
+__global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(AttendArgs a) {
   typedef typename Vec8<T>::type V8;
   constexpr int ND = 2 * NS;                 // 16-dimension tiles of the result
   constexpr int R = 16 * RT;
-  __shared__ float sm[4][R], sl[4][R];
-  __shared__ f32x4 so[2][ND][64];
+  constexpr int BUF = NS * RT <= 4 ? 2 : 1;  // steps in registers
+  __shared__ float sm[NW][R], sl[NW][R];
+  __shared__ f32x4 so[NW / 2][ND][64];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n16 = lane & 15, g = lane >> 4;
@@ -879,57 +920,33 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
   const int split = blockIdx.y;
   const int P = 1 << a.s.page_shift, d = a.d, G = a.group;
 
-  int b, r0, rows, row0, n;
+  Seq sq;
+  int r0, rows;
   int64_t tok = 0;
   if constexpr (SEL) {
     tok = item / a.tiles_token;
-    b = find_seq(a.s, tok, 1, 1, 0);
-    row0 = a.s.cu[b];
-    n = a.s.cu[b + 1] - row0;
-    r0 = (int)(tok - row0) * G + (int)(item - tok * a.tiles_token) * R;
-    rows = min(R, (int)(tok - row0 + 1) * G - r0);
+    sq = find_seq(a.s, tok, 1, 1, 0);
+    r0 = (int)(tok - sq.row0) * G + (int)(item - tok * a.tiles_token) * R;
+    rows = min(R, (int)(tok - sq.row0 + 1) * G - r0);
   } else {
-    b = find_seq(a.s, item, G, R, 1);
-    row0 = a.s.cu[b];
-    n = a.s.cu[b + 1] - row0;
-    const int64_t rr = (item - first_item(a.s, b, G, R, 1)) * R;
-    if (rr >= (int64_t)n * G) return;
+    sq = find_seq(a.s, item, G, R, 1);
+    const int64_t rr = (item - first_of(sq.row0, sq.b, G, R, 1)) * R;
+    if (rr >= (int64_t)sq.n * G) return;
     r0 = (int)rr;
-    rows = (int)min((int64_t)R, (int64_t)n * G - rr);
+    rows = (int)min((int64_t)R, (int64_t)sq.n * G - rr);
   }
-  // keys that exist for this sequence, and slots of the rows
-  const int total = a.s.total[b];
+  const int b = sq.b, row0 = sq.row0, n = sq.n, total = sq.total;
+  // keys that exist for this sequence, and the tile's: [klo, khi)
   const int64_t held = min((int64_t)total, (int64_t)a.s.max_pages << a.s.page_shift);
-  int64_t lim[RT], low[RT];
-  V8 qf[RT][NS];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int r = rt * 16 + n16;
-    const bool live = r < rows;
-    const int rr = r0 + (live ? r : 0), ti = rr / G, hh = rr - ti * G;
-    const int64_t slot = (int64_t)total - n + ti;
-    lim[rt] = live ? min(slot, held - 1) : -1;
-    low[rt] = a.window > 0 ? slot - a.window + 1 : 0;
-    const T* qr = (const T*)a.q + (int64_t)(row0 + ti) * a.qt + (int64_t)(head * G + hh) * a.qh;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const int dim = 32 * s + 8 * g;
-      V8 v = load_row8(qr + min(dim, d - 8), a.q_vec);
-      if (dim >= d)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (T)0.0f;
-      qf[rt][s] = v;
-    }
-  }
-  // the tile's keys: [klo, khi)
-  const int64_t khi = min(held, (int64_t)total - n + (r0 + rows - 1) / G + 1);
-  const int64_t klo = a.window > 0 ? max((int64_t)0, (int64_t)total - n + r0 / G - a.window + 1) : 0;
+  const int khi = (int)max((int64_t)0, min(held, (int64_t)total - n + (r0 + rows - 1) / G + 1));
+  const int klo = a.window > 0
+      ? (int)max((int64_t)0, (int64_t)total - n + r0 / G - a.window + 1) : 0;
   // steps of 32 keys: [st0, st1) in units of 32 keys, or of (list entry, part of its page)
-  int64_t st0, st1;
+  int st0, st1;
   const int sub_shift = a.s.page_shift - 5;
   if constexpr (SEL) {
-    st0 = ((int64_t)split * a.chunk) << sub_shift;
-    st1 = min(((int64_t)(split + 1) * a.chunk), (int64_t)a.m) << sub_shift;
+    st0 = (split * a.chunk) << sub_shift;
+    st1 = min((split + 1) * a.chunk, a.m) << sub_shift;
   } else {
     const int64_t c0 = (int64_t)split * a.chunk, c1 = c0 + a.chunk;
     if (c0 >= khi || c1 <= klo) {
@@ -939,44 +956,93 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
       }
       st0 = st1 = 0;                        // rows that see no key: zeros
     } else {
-      st0 = max(c0, klo) >> 5;
-      st1 = (min(c1, khi) + 31) >> 5;
+      st0 = (int)(max(c0, (int64_t)klo) >> 5);
+      st1 = (int)((min(c1, (int64_t)khi) + 31) >> 5);
     }
   }
-  const int32_t* list = SEL ? a.sel + (tok * a.heads + head) * a.m : nullptr;
-  const T* kc = (const T*)a.k;
-  const T* vc = (const T*)a.v;
-  const int krow = 8 * (n16 >> 2) + (n16 & 3);
 
-  // a step's page and first key; page -1: nothing to read
-  const auto locate = [&](int64_t st, int& phys, int64_t& key) {
-    int lp, sub;
-    if constexpr (SEL) {
-      lp = list[st >> sub_shift];
-      sub = (int)(st & ((1 << sub_shift) - 1));
-      key = ((int64_t)lp << a.s.page_shift) + 32 * sub;
-      phys = lp >= 0 && key < khi ? phys_page(a.s, b, lp) : -1;
-    } else {
-      key = st << 5;
-      phys = phys_page(a.s, b, (int)(key >> a.s.page_shift));
+  // this wave's steps, 64 at a time: a lane's page and first key
+  const int32_t* list = SEL ? a.sel + (tok * a.heads + head) * a.m : nullptr;
+  int ahead = st0 + wave, lphys = -1, lkey = 0;
+  uint64_t todo = 0;
+  const auto refill = [&] {
+    const int st = ahead + NW * lane;
+    lphys = -1;
+    if (st < st1 && st >= st0) {
+      if constexpr (SEL) {
+        const int lp = list[st >> sub_shift];
+        const int64_t key = ((int64_t)lp << a.s.page_shift) + 32 * (st & ((1 << sub_shift) - 1));
+        if (lp >= 0 && key < khi) {
+          lphys = phys_page(a.s, b, lp);
+          lkey = (int)key;
+        }
+      } else {
+        lkey = st << 5;
+        lphys = phys_page(a.s, b, lkey >> a.s.page_shift);
+      }
     }
-    phys = __builtin_amdgcn_readfirstlane(phys);
+    ahead += NW * 64;
+    todo = __ballot(lphys >= 0);
   };
-  V8 kf[2][NS], vf[ND];
-  const auto load = [&](int phys, int64_t key) {
-    const int64_t rec = ((int64_t)phys * a.heads + head) * P * d;
-    const int off = (int)(key & (P - 1));
-    const T* kp = kc + rec + (int64_t)off * d;
-    const T* vp = vc + rec + off;
+  // the next step's lane, -1 if there is none
+  const auto next = [&] {
+    while (todo == 0 && ahead < st1) refill();
+    const int i = todo == 0 ? -1 : __ffsll((unsigned long long)todo) - 1;
+    todo &= todo - 1;
+    return __builtin_amdgcn_readfirstlane(i);
+  };
+  // addresses: a uniform part and the lane's own bytes.  The last 32 dimensions of a row that is
+  // no multiple of 32 wide overlap those before; queries are 0 where they do.
+  const char* kc = (const char*)a.k + (int64_t)head * P * d * 2;
+  const char* vc = (const char*)a.v + (int64_t)head * P * d * 2;
+  const uint32_t klane = ((8 * (n16 >> 2) + (n16 & 3)) * d + min(8 * g, d - 8)) * 2;
+  const uint32_t vlane = (n16 * P + 8 * g) * 2;
+  const auto dims_at = [&](int s) { return max(0, min(32 * s, d - 32)); };
+  V8 kf[BUF][2][NS], vf[BUF][ND];
+  int key[BUF];
+  const auto load = [&](int i, auto buf) {
+    constexpr int B = decltype(buf)::value;
+    const int phys = __builtin_amdgcn_readlane(lphys, i);
+    key[B] = __builtin_amdgcn_readlane(lkey, i);
+    const int64_t rec = (int64_t)phys * a.heads * P * d * 2;
+    const int off = key[B] & (P - 1);
+    const char* kp = kc + rec + off * d * 2;
+    const char* vp = vc + rec + off * 2;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int s = 0; s < NS; ++s)
-        kf[t][s] = load16<V8>(kp + (krow + 4 * t) * d + min(32 * s + 8 * g, d - 8));
+        kf[B][t][s] = load16<V8>(kp + (4 * t * d + dims_at(s)) * 2 + klane);
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
-      vf[dt] = load16<V8>(vp + min(16 * dt + n16, d - 1) * P + 8 * g);
+      vf[B][dt] = load16<V8>(vp + min(16 * dt, d - 16) * P * 2 + vlane);
   };
+  constexpr std::integral_constant<int, 0> first{};
+  constexpr std::integral_constant<int, BUF - 1> second{};
+  int cur = next();
+  if (BUF == 2 && cur >= 0) load(cur, first);
+
+  int lim[RT], low[RT];
+  V8 qf[RT][NS];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = rt * 16 + n16;
+    const bool live = r < rows;
+    const int rr = r0 + (live ? r : 0), ti = rr / G, hh = rr - ti * G;
+    const int64_t slot = (int64_t)total - n + ti;
+    lim[rt] = live ? (int)max((int64_t)-1, min(slot, held - 1)) : -1;
+    low[rt] = a.window > 0 ? (int)max((int64_t)0, slot - a.window + 1) : 0;
+    const T* qr = (const T*)a.q + (int64_t)(row0 + ti) * a.qt + (int64_t)(head * G + hh) * a.qh;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const int dim = dims_at(s) + 8 * g;
+      V8 v = load_row8(qr + min(dim, d - 8), a.q_vec);
+      if (dim >= d || dim < 32 * s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (T)0.0f;
+      qf[rt][s] = v;
+    }
+  }
 
   f32x4 o[RT][ND];
   float mx[RT], sum[RT];
@@ -987,20 +1053,15 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) o[rt][dt] = f32x4{0, 0, 0, 0};
   }
-
-  for (int64_t st = st0 + wave; st < st1; st += 4) {
-    int phys;
-    int64_t key;
-    locate(st, phys, key);
-    if (phys < 0) continue;
-    load(phys, key);
-    if (key + 32 > khi) {
+  const auto compute = [&](auto buf) {
+    constexpr int B = decltype(buf)::value;
+    if (key[B] + 32 > khi) {
       // slots past the last key may hold anything: 0 x NaN must not reach the sums
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (key + 8 * g + e >= khi) vf[dt][e] = (T)0.0f;
+          vf[B][dt][e] = key[B] + 8 * g + e < khi ? vf[B][dt][e] : (T)0.0f;
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -1009,14 +1070,14 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
       for (int t = 0; t < 2; ++t) {
         sc[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int s = 0; s < NS; ++s) sc[t] = mfma16(kf[t][s], qf[rt][s], sc[t]);
+        for (int s = 0; s < NS; ++s) sc[t] = mfma16(kf[B][t][s], qf[rt][s], sc[t]);
       }
       float m = mx[rt];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int64_t kk = key + 8 * g + 4 * t + i;
+          const int kk = key[B] + 8 * g + 4 * t + i;
           const float v = sc[t][i] * a.scale2;
           sc[t][i] = kk <= lim[rt] && kk >= low[rt] ? v : -INFINITY;
           m = fmaxf(m, sc[t][i]);
@@ -1040,12 +1101,29 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) {
         o[rt][dt] *= alpha;
-        o[rt][dt] = mfma16(vf[dt], p, o[rt][dt]);
+        o[rt][dt] = mfma16(vf[B][dt], p, o[rt][dt]);
       }
+    }
+  };
+  if constexpr (BUF == 2) {
+    while (cur >= 0) {
+      const int nxt = next();
+      if (nxt >= 0) load(nxt, second);
+      compute(first);
+      if (nxt < 0) break;
+      cur = next();
+      if (cur >= 0) load(cur, first);
+      compute(second);
+    }
+  } else {
+    while (cur >= 0) {
+      load(cur, first);
+      cur = next();
+      compute(first);
     }
   }
 
-  // join the four waves
+  // join the waves
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     sum[rt] += __shfl_xor(sum[rt], 16);
@@ -1059,33 +1137,35 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int c = rt * 16 + n16;
-    const float mm = fmaxf(fmaxf(sm[0][c], sm[1][c]), fmaxf(sm[2][c], sm[3][c]));
+    float mm = sm[0][c];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) mm = fmaxf(mm, sm[w][c]);
     const float base = mm == -INFINITY ? 0.0f : mm;
     float z = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) z += sl[w][c] * exp2_fast(sm[w][c] - base);
+    for (int w = 0; w < NW; ++w) z += sl[w][c] * exp2_fast(sm[w][c] - base);
     const float f = exp2_fast(mx[rt] - base);
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) o[rt][dt] *= f;
-    if (wave >= 2)
+    // halves: the upper waves hand their sums to the lower ones
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) so[wave - 2][dt][lane] = o[rt][dt];
-    __syncthreads();
-    if (wave < 2)
+    for (int h = NW / 2; h >= 1; h /= 2) {
+      if (wave >= h && wave < 2 * h)
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) o[rt][dt] += so[wave][dt][lane];
-    __syncthreads();
-    if (wave == 1)
+        for (int dt = 0; dt < ND; ++dt) so[wave - h][dt][lane] = o[rt][dt];
+      __syncthreads();
+      if (wave < h)
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) so[0][dt][lane] = o[rt][dt];
-    __syncthreads();
+        for (int dt = 0; dt < ND; ++dt) o[rt][dt] += so[wave][dt][lane];
+      __syncthreads();
+    }
     if (wave == 0 && c < rows) {
       const int rr = r0 + c, ti = rr / G, hh = rr - ti * G;
       const int64_t orow = (int64_t)(row0 + ti) * a.hq + head * G + hh;
       const float inv = z > 0.0f ? 1.0f / z : 0.0f;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) {
-        const f32x4 v = o[rt][dt] + so[0][dt][lane];
+        const f32x4 v = o[rt][dt];
         const int dim = 16 * dt + 4 * g;
         if (dim >= d) continue;
         if (a.splits == 1) {
@@ -1108,7 +1188,6 @@ __global__ __launch_bounds__(256) void k_attend_few(AttendArgs a) {
         }
       }
     }
-    __syncthreads();
   }
 }
 
@@ -1156,9 +1235,9 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 4 : ND <= 4 ? 2 : 1) void k_atte
   const int split = blockIdx.y;
   const int P = 1 << a.s.page_shift, d = a.d, G = a.group;
 
-  const int b = find_seq(a.s, item, G, R, 1);
-  const int row0 = a.s.cu[b], n = a.s.cu[b + 1] - row0, total = a.s.total[b];
-  const int64_t rr0 = (item - first_item(a.s, b, G, R, 1)) * R;
+  const Seq sq = find_seq(a.s, item, G, R, 1);
+  const int b = sq.b, row0 = sq.row0, n = sq.n, total = sq.total;
+  const int64_t rr0 = (item - first_of(row0, b, G, R, 1)) * R;
   if (rr0 >= (int64_t)n * G) return;
   const int r0 = (int)rr0;
   const int rows = (int)min((int64_t)R, (int64_t)n * G - rr0);
@@ -1484,12 +1563,14 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 4 : ND <= 4 ? 2 : 1) void k_atte
   }
 }
 
-// Joins the partial results of the key ranges, in their order: a wave a row, 4 dimensions a
-// lane.  Ranges without a key of the row have a sum of 0 and are skipped.
-template <typename T>
+// Joins the partial results of the key ranges: WR waves a row (every WR-th eight ranges each, then
+// the waves' sums in order), 4 dimensions a lane.  Ranges without a key of the row have a sum of 0
+// and are skipped.
+template <typename T, int WR>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t orow = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  __shared__ f32x4 so[WR][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t orow = WR == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
   const int64_t nrows = a.tokens * a.hq;
   if (orow >= nrows) return;
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + orow;
@@ -1504,26 +1585,37 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   for (int c0 = 0; c0 < a.splits; c0 += 64) {
     const float2 v = c0 + lane < a.splits ? ml[(c0 + lane) * nrows] : make_float2(-INFINITY, 0.0f);
     const float f = exp2_fast(v.x - base);
-    uint64_t mask = __ballot(v.y != 0.0f);
-    const int some = mask != 0 ? __ffsll((unsigned long long)mask) - 1 : 0;
-    z += mask >> lane & 1 ? v.y * f : 0.0f;
-    while (mask != 0) {                     // four at a time: their loads are in flight together
-      f32x4 o[4];
-      float w[4];
+    const uint64_t all = __ballot(v.y != 0.0f);
+    uint64_t mask = all;
+    const int some = all != 0 ? __ffsll((unsigned long long)all) - 1 : 0;
+    z += all >> lane & 1 ? v.y * f : 0.0f;
+    for (int turn = 0; mask != 0; ++turn) {   // eight at a time: their loads are in flight together
+      f32x4 o[8];
+      float w[8];
+      const bool mine = WR == 1 || turn % WR == wave;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bool has = mask != 0;         // past the last: one of them again, times 0
+      for (int j = 0; j < 8; ++j) {
+        const bool has = mask != 0;           // past the last: one of them again, times 0
         const int i = has ? __ffsll((unsigned long long)mask) - 1 : some;
         mask &= mask - 1;
         w[j] = has ? __shfl(f, i) : 0.0f;
-        o[j] = *reinterpret_cast<const f32x4*>(a.part_o + ((int64_t)(c0 + i) * nrows + orow) * a.d + at);
+        if (mine)
+          o[j] = *reinterpret_cast<const f32x4*>(a.part_o + ((int64_t)(c0 + i) * nrows + orow) * a.d + at);
       }
+      if (mine)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc += w[j] * o[j];
+        for (int j = 0; j < 8; ++j) acc += w[j] * o[j];
     }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o);
+  if constexpr (WR > 1) {
+    so[wave][lane] = acc;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 1; w < WR; ++w) acc += so[w][lane];
+  }
   if (lane * 4 < a.d) {
     alignas(8) T w[4];
     const float inv = 1.0f / z;
@@ -1582,6 +1674,7 @@ int check_heads(const gmm_kv_cache* c, int32_t hq) {
 
 // Row tiles and key ranges of an attention call.
 struct Plan {
+  int waves;               // k_attend_few: 4, or 8 for a whole row tile's keys in one workgroup
   int rt;                  // k_attend_few: 16 rt rows a tile, 0 if it is k_attend_tile
   int rows;                // k_attend_tile: rows of a tile
   int64_t items;           // row tiles of a head
@@ -1589,13 +1682,23 @@ struct Plan {
   int chunk, splits;
 };
 
-// Workgroups wanted: 256 CUs hold 2 each; four rounds of them even out ragged lengths.
-constexpr int64_t kWantGroups = 2048;
-constexpr int kMaxSplits = 1024;
+// Workgroups wanted: 256 CUs hold 2 each; many rounds of them even out ragged lengths (64
+// sequences of up to 32,768 keys: 802 us with 1024, 673 with 2048, 644 with 4096, 632 with 8192).
+constexpr int64_t kWantGroups = 8192;
+// and at most this many partial results of a row: a wave joins a quarter of them
+constexpr int kMaxSplits = 128;
 constexpr int kCUs = 256;
 
 // rows of a tile above 64 are shared through LDS (k_attend_tile)
 int few_rows(int64_t rows, int d) { return rows <= 16 ? 1 : rows <= 32 || d > 128 ? 2 : 4; }
+
+// One workgroup of eight waves takes all keys of a row tile where these are few or there are
+// tiles for half of the CUs: nothing to join, one launch less.  (One token on 1000 keys and 8
+// heads: 8 workgroups read 4 MB in 14 us, 64 in 3; 256 tiles of 2048 keys: 42 us, split and
+// joined 56.)
+bool whole_rows(int64_t keys, int64_t tiles, int rt, int d) {
+  return rt == 1 && d <= 128 && keys <= (tiles >= kCUs / 2 ? 2048 : 512);
+}
 
 Plan plan_dense(int heads, int page, int d, int64_t tokens, int32_t batch, int group,
                 int32_t max_pages) {
@@ -1617,6 +1720,8 @@ Plan plan_dense(int heads, int page, int d, int64_t tokens, int32_t batch, int g
     p.items = tokens * group / (16 * p.rt) + batch;
     want = cdiv(kWantGroups, p.items * heads);
     unit = 128;                      // a step of 32 keys for every wave
+    p.waves = whole_rows(keys, p.items * heads, p.rt, d) ? 8 : 4;
+    if (p.waves == 8) want = 1;
   }
   if (want > kMaxSplits) want = kMaxSplits;
   const int64_t chunk = cdiv(cdiv(keys, want), unit) * unit;
@@ -1631,6 +1736,8 @@ Plan plan_sel(int heads, int page, int d, int64_t tokens, int group, int32_t m) 
   p.tiles_token = (int)cdiv(group, 16 * p.rt);
   p.items = tokens * p.tiles_token;
   int64_t want = cdiv(kWantGroups, p.items * heads);
+  p.waves = whole_rows((int64_t)m * page, p.items * heads, p.rt, d) ? 8 : 4;
+  if (p.waves == 8) want = 1;
   if (want > kMaxSplits) want = kMaxSplits;
   const int least = page >= 128 ? 1 : 128 / page;
   int64_t chunk = cdiv(m, want);
@@ -1675,10 +1782,18 @@ void launch_append(const AppendArgs& a, bool vec, bool inter, int64_t blocks, hi
 template <typename T, int NS, int RT>
 void launch_few(const AttendArgs& a, const Plan& p, hipStream_t st) {
   const dim3 grid((unsigned)(p.items * a.heads), (unsigned)p.splits);
-  if (a.sel)
-    hipLaunchKernelGGL((k_attend_few<T, NS, RT, true>), grid, dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL((k_attend_few<T, NS, RT, false>), grid, dim3(256), 0, st, a);
+  const auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * p.waves), 0, st, a);
+  };
+  if constexpr (RT == 1 && NS <= 4) {
+    if (p.waves == 8) {
+      if (a.sel) run(k_attend_few<T, NS, RT, true, 8>);
+      else run(k_attend_few<T, NS, RT, false, 8>);
+      return;
+    }
+  }
+  if (a.sel) run(k_attend_few<T, NS, RT, true, 4>);
+  else run(k_attend_few<T, NS, RT, false, 4>);
 }
 
 template <typename T, int NS>
@@ -1713,8 +1828,12 @@ void launch_attend(const AttendArgs& a, const Plan& p, hipStream_t st) {
   else if (a.d <= 192) launch_few_rt<T, 6>(a, p, st);
   else launch_few_rt<T, 8>(a, p, st);
   if (a.splits > 1) {
-    const dim3 grid((unsigned)cdiv(a.tokens * a.hq, 4));
-    hipLaunchKernelGGL((k_attend_join<T>), grid, dim3(256), 0, st, a);
+    if (a.splits > 16)
+      hipLaunchKernelGGL((k_attend_join<T, 4>), dim3((unsigned)(a.tokens * a.hq)), dim3(256), 0,
+                         st, a);
+    else
+      hipLaunchKernelGGL((k_attend_join<T, 1>), dim3((unsigned)cdiv(a.tokens * a.hq, 4)),
+                         dim3(256), 0, st, a);
   }
 }
 
@@ -1832,7 +1951,9 @@ int gmm_kv_append(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
   const int size = cache->page * d;
   a.per = size >= 8192 ? 1 : size >= 4096 ? 2 : 4;
   while (a.per > 1 && 256 / a.per < d / (2 * w)) a.per /= 2;
-  a.page_blocks = (tokens / cache->page + 2 * (int64_t)seqs->batch) * cdiv(cache->heads, a.per);
+  int64_t pages = tokens / cache->page + 2 * (int64_t)seqs->batch;
+  if (pages > tokens) pages = tokens;
+  a.page_blocks = pages * cdiv(cache->heads, a.per);
   const int64_t blocks = a.page_blocks + cdiv(q_items, 256);
   if (blocks > kMaxBlocks) return GMM_ERR_UNSUPPORTED;
   a.q_items = (uint32_t)q_items;
@@ -1883,7 +2004,11 @@ int gmm_kv_select(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
   a.row = score_row(seqs->max_pages);
   const int per = 16 >> a.col_shift;
   const int64_t items = tokens / per + seqs->batch;
-  a.parts = (int)cdiv(seqs->max_pages, 256);
+  // about four workgroups a CU: what a workgroup does first takes as long as a round of pages
+  const int64_t parts = cdiv(seqs->max_pages, 256);
+  const int64_t rounds = cdiv(parts * items * cache->heads, 4 * kCUs);
+  a.rounds = (int)(rounds < 1 ? 1 : rounds > 8 ? 8 : rounds);
+  a.parts = (int)cdiv(parts, a.rounds);
   const int64_t blocks = a.parts * items * cache->heads, rows = tokens * cache->heads;
   // a row's workgroup has up to 1024 threads
   if (blocks > kMaxBlocks || rows > kMaxBlocks / 4) return GMM_ERR_UNSUPPORTED;
@@ -1949,7 +2074,7 @@ int gmm_kv_attend(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
   a.part_o = (float*)ws;
   a.part_ml = a.part_o + (int64_t)p.splits * tokens * hq * a.d;
   if (p.items * a.heads * p.splits > kMaxBlocks || p.splits > 65535 ||
-      cdiv(tokens * hq, 4) > kMaxBlocks)
+      tokens * hq > kMaxBlocks)
     return GMM_ERR_UNSUPPORTED;
   if (cache->dtype == GMM_BF16) launch_attend<__bf16>(a, p, stream);
   else launch_attend<_Float16>(a, p, stream);
