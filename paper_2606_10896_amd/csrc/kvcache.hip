@@ -34,6 +34,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // 1/127 rounded to fp32
 constexpr float kInv127 = 1.0f / 127.0f;
+// partial results of a row at most: 1024 keys each at 131,072 keys
+constexpr int kMaxSplits = 128;
 // a launch has fewer than 2^32 threads
 constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 1;
 
@@ -524,12 +526,12 @@ __device__ __forceinline__ float score_of(float query_unit, float page_unit, int
 // Scores: [pages x 2 d] . [2 d x (token, query head)] in 8-bit integers on 16x16x64 MFMA, the
 // boxes (upper | lower bounds) straight from memory in operand order, the queries (positive |
 // negative parts) through LDS.  A wave takes 64 pages: their numbers are one load, their boxes
-// (16 KB at d = 128) are in flight together while the queries are rounded to 8 bits.  S: 64-byte
+// (8 KB at a time at d = 128) are in flight while the queries are rounded to 8 bits.  S: 64-byte
 // steps of a box.  Bound by the boxes' bytes: 2 d + 4 a (page, head).
 template <typename T, int S>
-__global__ __launch_bounds__(256) void k_select_score(SelectArgs a) {
+__global__ __launch_bounds__(256, S <= 4 ? 4 : 2) void k_select_score(SelectArgs a) {
   typedef typename Vec8<T>::type V8;
-  constexpr int TB = S <= 4 ? 4 : 2;        // 16-page tiles in flight
+  constexpr int TB = S <= 2 ? 4 : 2;        // 16-page tiles in flight
   extern __shared__ int8_t q8[];            // [col_tiles * 16][2 d + 16], then the units [.]
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = 16 >> a.col_shift;        // tokens a tile holds
@@ -606,12 +608,17 @@ __global__ __launch_bounds__(256) void k_select_score(SelectArgs a) {
   load_column(tid >> 4);
 
   // this wave's pages, one a lane
-  int p0 = 0, phys = -1;
+  const auto page_at = [&](int round) {
+    const int p = ((part_no * a.rounds + round) * 4 + wave) * 64 + lane;
+    return p < visible ? phys_page(a.s, b, p) : -1;
+  };
+  int p0 = 0, phys = page_at(0), ahead = -1;        // ahead: the next round's
   float sp = 0.0f;
   const auto take_pages = [&](int round) {
     p0 = ((part_no * a.rounds + round) * 4 + wave) * 64;
-    phys = p0 + lane < visible ? phys_page(a.s, b, p0 + lane) : -1;
+    if (round > 0) phys = ahead;
     sp = a.box_scale[(int64_t)max(phys, 0) * a.heads + head];
+    ahead = round + 1 < a.rounds ? page_at(round + 1) : -1;
   };
   const int n16 = lane & 15, g = lane >> 4;
   i32x4 bx[TB][S];
@@ -1563,68 +1570,104 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 4 : ND <= 4 ? 2 : 1) void k_atte
   }
 }
 
-// Joins the partial results of the key ranges: WR waves a row (every WR-th eight ranges each, then
-// the waves' sums in order), 4 dimensions a lane.  Ranges without a key of the row have a sum of 0
-// and are skipped.
-template <typename T, int WR>
+// Joins the partial results of the key ranges, in their order.  Ranges without a key of the row
+// have a sum of 0 and are skipped: nothing was written for them.
+template <typename T>
+__device__ __forceinline__ void store_row4(const AttendArgs& a, int64_t orow, int dim, f32x4 acc,
+                                           float z) {
+  alignas(8) T w[4];
+  const float inv = 1.0f / z;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = (T)(z > 0.0f ? acc[i] * inv : z);
+  *reinterpret_cast<uint2*>((T*)a.out + orow * a.d + dim) = *reinterpret_cast<uint2*>(w);
+}
+__device__ __forceinline__ void store_lse(const AttendArgs& a, int64_t orow, float mm, float z) {
+  if (a.lse) a.lse[orow] = z > 0.0f ? (mm + log2_fast(z)) * kLn2 : (z == 0.0f ? -INFINITY : z);
+}
+
+// up to 16 ranges: a wave a row, 4 dimensions a lane
+template <typename T>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
-  __shared__ f32x4 so[WR][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t orow = WR == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+  const int lane = threadIdx.x & 63;
+  const int64_t orow = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int64_t nrows = a.tokens * a.hq;
   if (orow >= nrows) return;
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + orow;
-  float mm = -INFINITY;
-  for (int c = lane; c < a.splits; c += 64) mm = fmaxf(mm, ml[c * nrows].x);
+  const float2 v = lane < a.splits ? ml[lane * nrows] : make_float2(-INFINITY, 0.0f);
+  float mm = v.x;
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o));
+  mm = __shfl(mm, 0);
+  const float f = v.y != 0.0f ? exp2_fast(v.x - mm) : 0.0f;   // mm is finite where one is not 0
+  float z = f * v.y;
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) z += __shfl_xor(z, o);
+  z = __shfl(z, 0);
+  f32x4 acc = {0, 0, 0, 0};
+  const float* po = a.part_o + orow * a.d + min(lane * 4, a.d - 4);
+  for (int c0 = 0; c0 < a.splits; c0 += 8) {       // eight loads in flight
+    f32x4 o[8];
+    float w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      w[j] = c0 + j < a.splits ? __shfl(f, c0 + j) : 0.0f;
+      o[j] = f32x4{0, 0, 0, 0};
+      if (w[j] != 0.0f) o[j] = *reinterpret_cast<const f32x4*>(po + (c0 + j) * nrows * a.d);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc += w[j] * o[j];
+  }
+  if (lane * 4 < a.d) store_row4<T>(a, orow, lane * 4, acc, z);
+  if (lane == 0) store_lse(a, orow, mm, z);
+}
+
+// up to kMaxSplits ranges: a workgroup a row, every eighth (d <= 128) or fourth range a group of
+// lanes, the groups' sums in order
+template <typename T>
+__global__ __launch_bounds__(256) void k_attend_join_many(AttendArgs a) {
+  __shared__ float w[kMaxSplits], red[4][2];
+  __shared__ f32x4 so[256];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t orow = blockIdx.x, nrows = a.tokens * a.hq;
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + orow;
+  const float2 v = tid < a.splits ? ml[tid * nrows] : make_float2(-INFINITY, 0.0f);
+  float mm = v.x;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o));
-  const float base = mm == -INFINITY ? 0.0f : mm;
-  float z = 0.0f;
-  f32x4 acc = {0, 0, 0, 0};
-  const int at = min(lane * 4, a.d - 4);
-  for (int c0 = 0; c0 < a.splits; c0 += 64) {
-    const float2 v = c0 + lane < a.splits ? ml[(c0 + lane) * nrows] : make_float2(-INFINITY, 0.0f);
-    const float f = exp2_fast(v.x - base);
-    const uint64_t all = __ballot(v.y != 0.0f);
-    uint64_t mask = all;
-    const int some = all != 0 ? __ffsll((unsigned long long)all) - 1 : 0;
-    z += all >> lane & 1 ? v.y * f : 0.0f;
-    for (int turn = 0; mask != 0; ++turn) {   // eight at a time: their loads are in flight together
-      f32x4 o[8];
-      float w[8];
-      const bool mine = WR == 1 || turn % WR == wave;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool has = mask != 0;           // past the last: one of them again, times 0
-        const int i = has ? __ffsll((unsigned long long)mask) - 1 : some;
-        mask &= mask - 1;
-        w[j] = has ? __shfl(f, i) : 0.0f;
-        if (mine)
-          o[j] = *reinterpret_cast<const f32x4*>(a.part_o + ((int64_t)(c0 + i) * nrows + orow) * a.d + at);
-      }
-      if (mine)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc += w[j] * o[j];
-    }
-  }
+  if (lane == 0) red[wave][0] = mm;
+  __syncthreads();
+  mm = fmaxf(fmaxf(red[0][0], red[1][0]), fmaxf(red[2][0], red[3][0]));
+  const float f = v.y != 0.0f ? exp2_fast(v.x - mm) : 0.0f;
+  if (tid < kMaxSplits) w[tid] = f;
+  float z = f * v.y;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o);
-  if constexpr (WR > 1) {
-    so[wave][lane] = acc;
-    __syncthreads();
-    if (wave > 0) return;
+  if (lane == 0) red[wave][1] = z;
+  __syncthreads();
+  z = red[0][1] + red[1][1] + red[2][1] + red[3][1];
+  const int width = a.d <= 128 ? 32 : 64, groups = 256 / width;
+  const int at = tid % width * 4;
+  const float* po = a.part_o + orow * a.d + min(at, a.d - 4);
+  f32x4 acc = {0, 0, 0, 0};
+  for (int c0 = tid / width; c0 < a.splits; c0 += 8 * groups) {
+    f32x4 o[8];
+    float f8[8];
 #pragma unroll
-    for (int w = 1; w < WR; ++w) acc += so[w][lane];
-  }
-  if (lane * 4 < a.d) {
-    alignas(8) T w[4];
-    const float inv = 1.0f / z;
+    for (int j = 0; j < 8; ++j) {
+      const int c = c0 + j * groups;
+      f8[j] = c < a.splits ? w[c] : 0.0f;
+      o[j] = f32x4{0, 0, 0, 0};
+      if (f8[j] != 0.0f) o[j] = *reinterpret_cast<const f32x4*>(po + c * nrows * a.d);
+    }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = (T)(z > 0.0f ? acc[i] * inv : z);
-    *reinterpret_cast<uint2*>((T*)a.out + orow * a.d + lane * 4) = *reinterpret_cast<uint2*>(w);
+    for (int j = 0; j < 8; ++j) acc += f8[j] * o[j];
   }
-  if (lane == 0 && a.lse)
-    a.lse[orow] = z > 0.0f ? (mm + log2_fast(z)) * kLn2 : (z == 0.0f ? -INFINITY : z);
+  so[tid] = acc;
+  __syncthreads();
+  if (tid >= width) return;
+  for (int g = 1; g < groups; ++g) acc += so[g * width + tid];
+  if (at < a.d) store_row4<T>(a, orow, at, acc, z);
+  if (tid == 0) store_lse(a, orow, mm, z);
 }
 
 // ---------------------------------------------------------------- host
@@ -1685,8 +1728,6 @@ struct Plan {
 // Workgroups wanted: 256 CUs hold 2 each; many rounds of them even out ragged lengths (64
 // sequences of up to 32,768 keys: 802 us with 1024, 673 with 2048, 644 with 4096, 632 with 8192).
 constexpr int64_t kWantGroups = 8192;
-// and at most this many partial results of a row: a wave joins a quarter of them
-constexpr int kMaxSplits = 128;
 constexpr int kCUs = 256;
 
 // rows of a tile above 64 are shared through LDS (k_attend_tile)
@@ -1829,10 +1870,10 @@ void launch_attend(const AttendArgs& a, const Plan& p, hipStream_t st) {
   else launch_few_rt<T, 8>(a, p, st);
   if (a.splits > 1) {
     if (a.splits > 16)
-      hipLaunchKernelGGL((k_attend_join<T, 4>), dim3((unsigned)(a.tokens * a.hq)), dim3(256), 0,
+      hipLaunchKernelGGL((k_attend_join_many<T>), dim3((unsigned)(a.tokens * a.hq)), dim3(256), 0,
                          st, a);
     else
-      hipLaunchKernelGGL((k_attend_join<T, 1>), dim3((unsigned)cdiv(a.tokens * a.hq, 4)),
+      hipLaunchKernelGGL((k_attend_join<T>), dim3((unsigned)cdiv(a.tokens * a.hq, 4)),
                          dim3(256), 0, st, a);
   }
 }
