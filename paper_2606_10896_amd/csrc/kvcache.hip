@@ -1279,11 +1279,13 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 4 : ND <= 4 ? 2 : 1) void k_atte
       const int dim = 16 * s + 8 * half;
       V8 v = load_row8(qr + min(dim, d - 8), a.q_vec);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = dim < d ? (a.scale2 < 0.0f ? -v[e] : v[e]) : (T)0.0f;
+      for (int e = 0; e < 8; ++e)
+        v[e] = dim < d && a.scale2 != 0.0f ? (a.scale2 < 0.0f ? -v[e] : v[e]) : (T)0.0f;
       qf[s] = v;
     }
   }
-  const float sc2 = fabsf(a.scale2);
+  // the scale's sign is in the queries, and so is a scale of 0: a masked score, -inf, stays -inf
+  const float sc2 = a.scale2 != 0.0f ? fabsf(a.scale2) : 1.0f;
   // keys wlow .. wlim are seen by every row of the wave: steps among them need no mask
   int wlim = -1, wlow = 0;
   if (wr0 < rows) {
@@ -1725,10 +1727,20 @@ struct Plan {
   int chunk, splits;
 };
 
-// Workgroups wanted: 256 CUs hold 2 each; many rounds of them even out ragged lengths (64
-// sequences of up to 32,768 keys: 802 us with 1024, 673 with 2048, 644 with 4096, 632 with 8192).
-constexpr int64_t kWantGroups = 8192;
 constexpr int kCUs = 256;
+
+// Key ranges of k_attend_few: enough workgroups for every CU to hold two, whatever a range's
+// length (a workgroup's first loads take as long as some steps: 8 sequences of 4000 keys, 4
+// tokens and 32 rows each: 66 us in ranges of 128 keys, 32 in ranges of 512), and more where ranges stay above
+// 1024 keys, which evens out ragged lengths (64 sequences of up to 32,768 keys: 802 us with 1024
+// workgroups, 673 with 2048, 644 with 4096, 632 with 8192).
+int64_t few_ranges(int64_t tiles, int64_t keys) {
+  const int64_t fill = cdiv(2 * kCUs, tiles), even = cdiv(32 * kCUs, tiles);
+  const int64_t long_ones = keys / 1024;
+  int64_t want = even < long_ones ? even : long_ones;
+  if (want < fill) want = fill;
+  return want > kMaxSplits ? kMaxSplits : want;
+}
 
 // rows of a tile above 64 are shared through LDS (k_attend_tile)
 int few_rows(int64_t rows, int d) { return rows <= 16 ? 1 : rows <= 32 || d > 128 ? 2 : 4; }
@@ -1759,7 +1771,7 @@ Plan plan_dense(int heads, int page, int d, int64_t tokens, int32_t batch, int g
   } else {
     p.rt = few_rows(rows, d);
     p.items = tokens * group / (16 * p.rt) + batch;
-    want = cdiv(kWantGroups, p.items * heads);
+    want = few_ranges(p.items * heads, keys);
     unit = 128;                      // a step of 32 keys for every wave
     p.waves = whole_rows(keys, p.items * heads, p.rt, d) ? 8 : 4;
     if (p.waves == 8) want = 1;
@@ -1776,10 +1788,9 @@ Plan plan_sel(int heads, int page, int d, int64_t tokens, int group, int32_t m) 
   p.rt = few_rows(group, d);
   p.tiles_token = (int)cdiv(group, 16 * p.rt);
   p.items = tokens * p.tiles_token;
-  int64_t want = cdiv(kWantGroups, p.items * heads);
+  int64_t want = few_ranges(p.items * heads, (int64_t)m * page);
   p.waves = whole_rows((int64_t)m * page, p.items * heads, p.rt, d) ? 8 : 4;
   if (p.waves == 8) want = 1;
-  if (want > kMaxSplits) want = kMaxSplits;
   const int least = page >= 128 ? 1 : 128 / page;
   int64_t chunk = cdiv(m, want);
   if (chunk < least) chunk = least;
@@ -2065,7 +2076,8 @@ int gmm_kv_select(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
     hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(threads), 0, stream, a.s, a.score,
                        a.row, a.heads, m, keep_first, keep_last, idx);
   };
-  if (seqs->max_pages <= 2048) run_top(k_select_top<256, 8>, 256);
+  if (seqs->max_pages <= 512) run_top(k_select_top<64, 8>, 64);
+  else if (seqs->max_pages <= 2048) run_top(k_select_top<256, 8>, 256);
   else if (seqs->max_pages <= 16384) run_top(k_select_top<1024, 16>, 1024);
   else run_top(k_select_top<1024, 64>, 1024);
   return launch_status();

@@ -121,7 +121,7 @@ class KVCache:
 
     def box_values(self):
         """The boxes as numbers, fp32 [pages, heads, 2, d]: upper, then lower bounds."""
-        return self.box * self.box_scale[..., None, None]
+        return self.box * self.box_scale.view(self.pages, self.heads, 1, 1)
 
 
 def kv_cache(pages, heads, page, d, dtype=None, boxes=True, device="cuda"):
