@@ -423,7 +423,8 @@ typedef struct {
  * slot t % page of page pages[b * pages_stride + t / page].  A sequence may
  * have no new token.  total[b] <= max_pages * page and every page number of a
  * used entry in [0, cache pages) are the caller's duty; keys beyond the table
- * and pages out of range are left out (never read or written). */
+ * and pages out of range are left out (never read or written).  At most 2^20
+ * sequences, 2^24 new tokens and 2^30 keys a sequence. */
 typedef struct {
   const int32_t* cu;     /* [batch + 1] */
   const int32_t* total;  /* [batch] */
@@ -528,9 +529,10 @@ int gmm_kv_select(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
  *   counts twice
  * A row without a visible key gives zeros and lse = -inf.  Inner products and
  * sums are fp32, the softmax weights are rounded to dtype for the second
- * product.  What slots past a sequence's last key hold does not matter; a NaN
- * or infinite value at a key that one token sees can reach the rows of earlier
- * tokens of the same call.
+ * product.  What slots past a sequence's last key hold does not matter, nor
+ * does a key that a row does not see.  A NaN or infinite value (of v) reaches
+ * every row whose step of 32 or 64 keys it lies in, also rows of the same call
+ * that do not see its key (a weight of 0 times it).
  */
 int gmm_kv_attend(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t tokens,
                   const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t hq,

@@ -1213,13 +1213,14 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
 // earlier: every wave reads keys p and values p - 1 in turn p and writes keys p + 1 and
 // values p, and a barrier ends the turn.
 //
-// The running maximum is only moved (and the results rescaled) when a score exceeds it by 2^8:
-// a common factor cancels in the end, and weights up to 2^8 are as exact as those up to 1.
+// The running maximum is only moved (and the results rescaled) when a step's weights at the old
+// one add up to more than 2^8, or a row sees its first key: a common factor cancels in the end,
+// and weights up to 2^8 are as exact as those up to 1.  So most steps need no maximum at all.
 //
 // Rows of the score tile are keys in the order that makes its accumulator the B operand of the
 // second product: row r is key r with bits 2 and 3 exchanged.
 template <typename T, int ND, int NW>
-__global__ __launch_bounds__(64 * NW, ND <= 2 ? 4 : ND <= 4 ? 2 : 1) void k_attend_tile(AttendArgs a) {
+__global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_attend_tile(AttendArgs a) {
   typedef typename Vec8<T>::type V8;
   constexpr int NT = 64 * NW;
   constexpr int HV = NW == 8 ? 2 : 1;             // 32-key blocks of a step
@@ -1448,30 +1449,40 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 4 : ND <= 4 ? 2 : 1) void k_atte
           sc[hv][i] = see ? sc[hv][i] : -INFINITY;
         }
     }
-    float top = sc[0][0];
+    // weights at the present maximum; their sum says whether it has to move
+    const auto weights = [&] {
+      float z = 0.0f;
+      const float base = mx == -INFINITY ? 0.0f : mx;
 #pragma unroll
-    for (int hv = 0; hv < HV; ++hv)
+      for (int hv = 0; hv < HV; ++hv)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[hv][i]);
-    top *= sc2;
-    if (__ballot(top > mx + 8.0f) != 0) {
-      const float m = fmaxf(mx, fmaxf(top, __shfl_xor(top, 32)));
+        for (int i = 0; i < 16; ++i) {
+          const float e = exp2_fast(__fmaf_rn(sc[hv][i], sc2, -base));
+          z += e;
+          pw[hv][i >> 3][i & 7] = (T)e;        // rounded for the matrix product
+        }
+      return z;
+    };
+    float z = 0.0f;
+    bool move = __ballot(mx == -INFINITY && lim >= key0) != 0;
+    if (!move) {
+      z = weights();
+      move = __ballot(!(z <= 256.0f)) != 0;
+    }
+    if (move) {
+      float top = sc[0][0];
+#pragma unroll
+      for (int hv = 0; hv < HV; ++hv)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[hv][i]);
+      const float m = fmaxf(mx, fmaxf(top, __shfl_xor(top, 32)) * sc2);
       const float f = m == -INFINITY ? 1.0f : exp2_fast(mx - m);
       mx = m;
       sum *= f;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) o[dt] *= f;
+      z = weights();
     }
-    const float base = mx == -INFINITY ? 0.0f : mx;
-    float z = 0.0f;
-#pragma unroll
-    for (int hv = 0; hv < HV; ++hv)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float e = exp2_fast(__fmaf_rn(sc[hv][i], sc2, -base));
-        z += e;
-        pw[hv][i >> 3][i & 7] = (T)e;          // rounded for the matrix product
-      }
     sum += z;
     // the weights are formed in this part, and not where they are next used
 #pragma unroll
@@ -1702,8 +1713,8 @@ int check_seqs(const gmm_kv_cache* c, const gmm_kv_batch* s, int64_t tokens, Seq
   if (!s || !s->cu || !s->total || !s->pages) return GMM_ERR_INVALID_ARG;
   if (s->batch < 1 || s->max_pages < 1 || s->pages_stride < s->max_pages || tokens < 0)
     return GMM_ERR_INVALID_ARG;
-  // slots are 32-bit; rows (tokens x heads) too
-  if ((int64_t)s->max_pages * c->page > INT32_MAX || tokens > (1 << 24) || s->batch > (1 << 20))
+  // slots, and those of steps past the last, are 32-bit; rows (tokens x heads) too
+  if ((int64_t)s->max_pages * c->page > (1 << 30) || tokens > (1 << 24) || s->batch > (1 << 20))
     return GMM_ERR_UNSUPPORTED;
   *o = Seqs{(Table)(uintptr_t)s->cu, (Table)(uintptr_t)s->total, (Table)(uintptr_t)s->pages,
             s->pages_stride, s->batch, s->max_pages, log2i(c->page),
@@ -1760,8 +1771,10 @@ Plan plan_dense(int heads, int page, int d, int64_t tokens, int32_t batch, int g
   const int64_t rows = cdiv(tokens, batch) * group;
   int64_t want, unit;
   if (rows > 64) {
-    // eight waves share a step's operands up to 128 dimensions; up to 64 the vector part takes
-    // longer than the matrix part, and four workgroups of four waves a CU hide more of it
+    // eight waves share a step's operands from 65 to 128 dimensions (2048 tokens on 34,816 keys:
+    // 1.02 ms, 1.15 in workgroups of four waves); up to 64 the vector part takes longer than the
+    // matrix part, and three workgroups of four waves a CU hide more of it (prompts of 4000
+    // tokens with a window: 0.19 ms, 0.23); above 128 there are registers for four waves
     p.rows = rows > 128 && d > 64 && d <= 128 ? 256 : 128;
     const int64_t tiles = tokens * group / p.rows;
     p.items = tiles + batch;
@@ -2019,7 +2032,7 @@ size_t gmm_kv_workspace_bytes(const gmm_kv_cache* cache, int64_t tokens, int32_t
                               int32_t batch, int32_t max_pages) {
   if (check_cache(cache) != GMM_OK || check_heads(cache, hq) != GMM_OK) return 0;
   if (tokens < 0 || tokens > (1 << 24) || batch < 1 || batch > (1 << 20) || max_pages < 1 ||
-      (int64_t)max_pages * cache->page > INT32_MAX)
+      (int64_t)max_pages * cache->page > (1 << 30))
     return 0;
   return (size_t)ws_need(cache, tokens, hq, batch, max_pages);
 }
