@@ -535,9 +535,10 @@ __global__ __launch_bounds__(256, S <= 4 ? 4 : 2) void k_select_score(SelectArgs
   extern __shared__ int8_t q8[];            // [col_tiles * 16][2 d + 16], then the units [.]
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = 16 >> a.col_shift;        // tokens a tile holds
-  const int part_no = blockIdx.x % a.parts;
-  const int head = blockIdx.x / a.parts % a.heads;
-  const int64_t item = blockIdx.x / a.parts / a.heads;
+  // heads fastest: a page's boxes of all heads are neighbours in memory
+  const int head = blockIdx.x % a.heads;
+  const int part_no = blockIdx.x / a.heads % a.parts;
+  const int64_t item = blockIdx.x / a.heads / a.parts;
   const Seq sq = find_seq(a.s, item, 1, per, 1);
   const int b = sq.b, row0 = sq.row0, n = sq.n;
   const int tok0 = (int)(item - first_of(row0, b, 1, per, 1)) * per;
