@@ -77,15 +77,21 @@ __device__ __forceinline__ V load16(const void* p) {
   return __builtin_bit_cast(V, u);
 }
 
-// 8 elements of a caller's row; vec: its rows allow 16-byte loads
-template <typename T>
-__device__ __forceinline__ typename Vec8<T>::type load_row8(const T* p, int vec) {
-  typedef typename Vec8<T>::type V8;
-  if (vec) return load16<V8>(p);
-  V8 v;
+// 8 elements each at at(0) .. at(N - 1) of a caller's rows; vec: these allow 16-byte loads.  The
+// loads are issued before any is waited for.
+template <typename T, int N, typename At>
+__device__ __forceinline__ void load_rows8(typename Vec8<T>::type* v, At at, int vec) {
+  if (vec) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = p[e];
-  return v;
+    for (int i = 0; i < N; ++i) v[i] = load16<typename Vec8<T>::type>(at(i));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const T* p = at(i);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = p[e];
+    }
+  }
 }
 
 __host__ __device__ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -426,14 +432,15 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
     const int g0 = begin >> 3, ng = ((filled + 7) >> 3) - g0, blocks = live ? ng * (d >> 3) : 0;
     for (int i = tid; i < blocks; i += threads) {
       const int c = i / ng, sg = (g0 + i - c * ng) << 3;
+      const bool whole = sg >= begin && sg + 8 <= filled;
       V8 blk[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         blk[j] = V8((T)0.0f);
         if (sg + j >= begin && sg + j < filled)
-          blk[j] = load_row8(vin + (in0 + sg + j) * a.vt + c * 8, a.v_vec);
+          load_rows8<T, 1>(&blk[j], [&](int) { return vin + (in0 + sg + j) * a.vt + c * 8; },
+                           a.v_vec);
       }
-      const bool whole = sg >= begin && sg + 8 <= filled;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         T* dst = cvp + (int64_t)(c * 8 + e) * P + sg;
@@ -563,14 +570,10 @@ __global__ __launch_bounds__(256, S <= 4 ? 4 : 2) void k_select_score(SelectArgs
     const T* qr = (const T*)a.q +
                   (int64_t)(row0 + tok0 + (live ? (c & 15) >> a.col_shift : 0)) * a.qt +
                   (int64_t)(head * a.group + (live ? head_of(c) : 0)) * a.qh;
+    load_rows8<T, 2>(qv, [&](int j) { return qr + min(8 * (part + 16 * j), d - 8); }, a.q_vec);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int at = 8 * (part + 16 * j);
-      V8 v = load_row8(qr + min(at, d - 8), a.q_vec);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = live && at < d ? v[e] : (T)0.0f;
-      qv[j] = v;
-    }
+    for (int j = 0; j < 2; ++j)
+      if (!live || 8 * (part + 16 * j) >= d) qv[j] = V8((T)0.0f);
   };
   const auto round_column = [&](int c) {
     float m = 0.0f;
@@ -1041,14 +1044,11 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
     lim[rt] = live ? (int)max((int64_t)-1, min(slot, held - 1)) : -1;
     low[rt] = a.window > 0 ? (int)max((int64_t)0, slot - a.window + 1) : 0;
     const T* qr = (const T*)a.q + (int64_t)(row0 + ti) * a.qt + (int64_t)(head * G + hh) * a.qh;
+    load_rows8<T, NS>(qf[rt], [&](int s) { return qr + min(dims_at(s) + 8 * g, d - 8); }, a.q_vec);
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       const int dim = dims_at(s) + 8 * g;
-      V8 v = load_row8(qr + min(dim, d - 8), a.q_vec);
-      if (dim >= d || dim < 32 * s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (T)0.0f;
-      qf[rt][s] = v;
+      if (dim >= d || dim < 32 * s) qf[rt][s] = V8((T)0.0f);
     }
   }
 
@@ -1276,14 +1276,13 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
     lim = live ? (int)max((int64_t)-1, min(slot, (int64_t)kend - 1)) : -1;
     low = a.window > 0 && live ? (int)max((int64_t)0, slot - a.window + 1) : 0;
     const T* qr = (const T*)a.q + (int64_t)(row0 + ti) * a.qt + (int64_t)(head * G + hh) * a.qh;
+    load_rows8<T, NS>(qf, [&](int s) { return qr + min(16 * s + 8 * half, d - 8); }, a.q_vec);
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      const int dim = 16 * s + 8 * half;
-      V8 v = load_row8(qr + min(dim, d - 8), a.q_vec);
+      const bool zero = 16 * s + 8 * half >= d || a.scale2 == 0.0f;
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        v[e] = dim < d && a.scale2 != 0.0f ? (a.scale2 < 0.0f ? -v[e] : v[e]) : (T)0.0f;
-      qf[s] = v;
+        qf[s][e] = zero ? (T)0.0f : a.scale2 < 0.0f ? -qf[s][e] : qf[s][e];
     }
   }
   // the scale's sign is in the queries, and so is a scale of 0: a masked score, -inf, stays -inf
