@@ -528,8 +528,12 @@ int gmm_kv_select(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
  *   lists of pages in range; entries < 0 are skipped, a page listed twice
  *   counts twice
  * A row without a visible key gives zeros and lse = -inf.  Inner products and
- * sums are fp32, the softmax weights are rounded to dtype for the second
- * product.  What slots past a sequence's last key hold does not matter, nor
+ * sums are fp32; for the second product the softmax weights are rounded to
+ * dtype, with what the rounding leaves as a second term where a sequence has
+ * up to 64 query rows a cache head in the call's mean (tokens x group), and
+ * without it above (an error of a unit roundoff of dtype per weight, as the
+ * result's own rounding).
+ * What slots past a sequence's last key hold does not matter, nor
  * does a key that a row does not see.  A NaN or infinite value (of v) reaches
  * every row whose step of 32 or 64 keys it lies in, also rows of the same call
  * that do not see its key (a weight of 0 times it).

@@ -1095,7 +1095,9 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
       const float base = m == -INFINITY ? 0.0f : m;
       const float alpha = exp2_fast(mx[rt] - base);
       mx[rt] = m;
-      V8 p;
+      // weights in [0, 1] for the matrix product: rounded to T, and what the rounding leaves (the
+      // matrix unit waits for memory here, a second product costs nothing)
+      V8 p, rest;
       float z = 0.0f;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -1103,12 +1105,14 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
         for (int i = 0; i < 4; ++i) {
           const float e = exp2_fast(sc[t][i] - base);
           z += e;
-          p[4 * t + i] = (T)e;           // weights in [0, 1], rounded for the matrix product
+          p[4 * t + i] = (T)e;
+          rest[4 * t + i] = (T)(e - (float)p[4 * t + i]);
         }
       sum[rt] = sum[rt] * alpha + z;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) {
         o[rt][dt] *= alpha;
+        o[rt][dt] = mfma16(vf[B][dt], rest, o[rt][dt]);
         o[rt][dt] = mfma16(vf[B][dt], p, o[rt][dt]);
       }
     }
