@@ -282,7 +282,8 @@ __global__ __launch_bounds__(256) void k_rope_table(const double* __restrict__ f
 
 // A unit a thread: 16 elements (W = 8: 16-byte accesses) where rot, d, the strides and the
 // addresses allow it, else one pair.  An odd count of dimensions past rot ends in a unit of its
-// own (W = 1).  Bound by the bytes.
+// own (W = 1).  Bound by the bytes: 8192 x 32 x 128 bf16, half rotated, 28.6 us a call, 4.8 TB/s
+// (a 2 GiB copy: 5.0); a single token's 40 heads take 2 us.
 template <typename T, int W, bool INTER>
 __global__ __launch_bounds__(256) void k_rope(const T* x, int64_t xt, int64_t xh, T* out,
                                               int64_t ot, int64_t oh, uint32_t items, int heads,
@@ -332,7 +333,9 @@ struct AppendArgs {
 // (a page of 64 keys of 128 dimensions is 16 KB, so a single new token moves 8 KB on average
 // for a box that saves reading that page in every later step in which it is not selected).
 // Small pages share a workgroup, 128 or 64 threads a head.  The queries' rotation rides along in
-// workgroups of its own: one launch for the step.
+// workgroups of its own: one launch for the step.  Bound by the bytes for prompts (7498 tokens, 16
+// heads of 64: 28 us, about 130 MB), for single tokens by the chain sequence, page, keys, barrier
+// (64 sequences, 8 heads of 128: 9.6 us).
 template <typename T, int W, bool INTER>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
   typedef typename Vec8<T>::type V8;
@@ -534,7 +537,9 @@ __device__ __forceinline__ float score_of(float query_unit, float page_unit, int
 // boxes (upper | lower bounds) straight from memory in operand order, the queries (positive |
 // negative parts) through LDS.  A wave takes 64 pages: their numbers are one load, their boxes
 // (8 KB at a time at d = 128) are in flight while the queries are rounded to 8 bits.  S: 64-byte
-// steps of a box.  Bound by the boxes' bytes: 2 d + 4 a (page, head).
+// steps of a box.  Bound by the boxes' bytes, 2 d + 4 a (page, head), and the loads before them:
+// 32 sequences of up to 2049 pages, 8 heads of 128, 18.8 us, 2.6 TB/s; a few sequences of a few
+// hundred pages 7.4 us.
 template <typename T, int S>
 __global__ __launch_bounds__(256, S <= 4 ? 4 : 2) void k_select_score(SelectArgs a) {
   typedef typename Vec8<T>::type V8;
@@ -708,7 +713,7 @@ __device__ __forceinline__ uint32_t score_key(float v) {
 // largest key is bracketed by counting the keys at or above three values between the bounds
 // (ballots, no atomics) until a count is m or the bounds meet; then the pages above it and the
 // lowest ones equal to it are written in page order.  Bound by the rounds' latency: about ten,
-// a barrier each.
+// a barrier each: 7.4 us at up to 2049 pages, m = 32, 6.1 at a few hundred.
 template <int NT, int PT>
 __global__ __launch_bounds__(NT) void k_select_top(Seqs s, const float* __restrict__ score,
                                                    int64_t row, int heads, int m, int keep_first,
@@ -914,7 +919,10 @@ __device__ __forceinline__ void mark_empty(const AttendArgs& a, int split, int r
 // the end.  Every byte of the cache is read by one wave once, so LDS would only add a trip.  The
 // page numbers of 64 steps are one load, a lane a step; while a step is computed the next one's
 // operands are in flight (16 KB at d = 128) where registers allow it.  Bound by the cache's bytes,
-// for short contexts by the chain of loads: sequence, page numbers, keys.
+// for short contexts by the chain of loads: sequence, page numbers, keys.  64 sequences of up to
+// 32,768 keys, 32 heads on 8 of 128: 647 us, 5.4 TB/s; one token on 1000 keys 7.8 us.  The rest of
+// the weights' rounding as a second product takes 3 % of the former (633 us without) and brings
+// the error from 1.3 times the result's rounding to that rounding.
 template <typename T, int NS, int RT, bool SEL, int NW>
 __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(AttendArgs a) {
   typedef typename Vec8<T>::type V8;
@@ -1224,6 +1232,10 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
 //
 // Rows of the score tile are keys in the order that makes its accumulator the B operand of the
 // second product: row r is key r with bits 2 and 3 exchanged.
+//
+// 2048 tokens on 34,816 keys, 32 heads on 8 of 128: 974 us a call, 1164 TFLOP/s (a product of 8192^3
+// 1274): matrix unit busy 59 % of the cycles, vector unit 44, LDS 37.  Up to 64 dimensions the
+// vector unit bounds it (51 %, matrix unit 30): prompts with a window, 168 us.
 template <typename T, int ND, int NW>
 __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_attend_tile(AttendArgs a) {
   typedef typename Vec8<T>::type V8;
@@ -1746,9 +1758,9 @@ constexpr int kCUs = 256;
 
 // Key ranges of k_attend_few: enough workgroups for every CU to hold two, whatever a range's
 // length (a workgroup's first loads take as long as some steps: 8 sequences of 4000 keys, 4
-// tokens and 32 rows each: 66 us in ranges of 128 keys, 32 in ranges of 512), and more where ranges stay above
-// 1024 keys, which evens out ragged lengths (64 sequences of up to 32,768 keys: 802 us with 1024
-// workgroups, 673 with 2048, 644 with 4096, 632 with 8192).
+// tokens and 32 rows each: 66 us in ranges of 128 keys, 32 in ranges of 512), and more where
+// ranges stay above 1024 keys, which evens out ragged lengths (64 sequences of up to 32,768 keys:
+// 811 us with 1024 workgroups, 686 with 2048, 657 with 4096, 652 with 8192).
 int64_t few_ranges(int64_t tiles, int64_t keys) {
   const int64_t fill = cdiv(2 * kCUs, tiles), even = cdiv(32 * kCUs, tiles);
   const int64_t long_ones = keys / 1024;
@@ -1761,9 +1773,8 @@ int64_t few_ranges(int64_t tiles, int64_t keys) {
 int few_rows(int64_t rows, int d) { return rows <= 16 ? 1 : rows <= 32 || d > 128 ? 2 : 4; }
 
 // One workgroup of eight waves takes all keys of a row tile where these are few or there are
-// tiles for half of the CUs: nothing to join, one launch less.  (One token on 1000 keys and 8
-// heads: 8 workgroups read 4 MB in 14 us, 64 in 3; 256 tiles of 2048 keys: 42 us, split and
-// joined 56.)
+// tiles for half of the CUs: nothing to join, one launch less.  (2048 keys, whole and split with
+// its join: 256 tiles 45 us, 48; 32 tiles 35 us, 18; 8 tiles of 1000 keys 21 us, 13.)
 bool whole_rows(int64_t keys, int64_t tiles, int rt, int d) {
   return rt == 1 && d <= 128 && keys <= (tiles >= kCUs / 2 ? 2048 : 512);
 }
@@ -1776,10 +1787,16 @@ Plan plan_dense(int heads, int page, int d, int64_t tokens, int32_t batch, int g
   int64_t want, unit;
   if (rows > 64) {
     // eight waves share a step's operands from 65 to 128 dimensions (2048 tokens on 34,816 keys:
-    // 1.02 ms, 1.15 in workgroups of four waves); up to 64 the vector part takes longer than the
-    // matrix part, and three workgroups of four waves a CU hide more of it (prompts of 4000
-    // tokens with a window: 0.19 ms, 0.23); above 128 there are registers for four waves
-    p.rows = rows > 128 && d > 64 && d <= 128 ? 256 : 128;
+    // 0.97 ms, 1.12 in workgroups of four waves; 512 on 8512: 90 us, 132), but not for prompts
+    // that are most of their own context, whose few steps a tile of 128 rows ends earlier at the
+    // diagonal (32 heads on 8, eight waves and four: 2 prompts of 700 tokens 48 us, 30; 4: 54, 44;
+    // 16: 153, 132; one of 2000 91, 85; but 4 of 500 31, 33, and 8 of 2000 372, between 367 and
+    // 388).  Up to 64 the vector part
+    // takes longer than the matrix part, and three workgroups of four waves a CU hide more of it
+    // (prompts of 4000 tokens with a window, when it was chosen: 0.21 ms, 0.23); above 128 there
+    // are registers for four waves
+    const bool prompt = keys <= 2048 && keys * batch <= 2 * tokens;
+    p.rows = rows > 128 && d > 64 && d <= 128 && !prompt ? 256 : 128;
     const int64_t tiles = tokens * group / p.rows;
     p.items = tiles + batch;
     // one workgroup a CU; keys are split where there are fewer row tiles than that

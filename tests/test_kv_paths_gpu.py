@@ -86,6 +86,27 @@ def test_tiles_with_rows_before_the_first_key(gmm):
     _check(bt, _attend(gmm, bt), attend64(bt, 1.0 / math.sqrt(128)))
 
 
+def test_tiles_with_rows_before_the_first_key_of_a_long_context(gmm):
+    bt = Batch([(200, 70), (80, 80), (2, 1500)], 2, 1, 128, 32, "bf16")
+    _check(bt, _attend(gmm, bt), attend64(bt, 1.0 / math.sqrt(128)))
+
+
+# prompts that are most of their own context (four waves), and the same with longer contexts
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("seqs,hq,hk,d,page", [
+    ([(300, 300)], 1, 1, 128, 64),
+    ([(500, 640), (0, 0), (411, 411)], 4, 2, 128, 32),
+    ([(129, 129), (257, 258)], 3, 3, 96, 128),
+    ([(300, 601)], 1, 1, 128, 64),
+    ([(500, 640), (0, 0), (411, 1411)], 4, 2, 128, 32),
+    ([(2050, 2050)], 1, 1, 80, 256),
+])
+def test_prompts(gmm, dtype, seqs, hq, hk, d, page):
+    print(f"attend {dtype} {seqs} {hq} {hk} {d} {page}", flush=True)
+    bt = Batch(seqs, hq, hk, d, page, dtype, seed=len(seqs) + d)
+    _check(bt, _attend(gmm, bt), attend64(bt, 1.0 / math.sqrt(d)))
+
+
 def test_tiles_move_their_maximum(gmm):
     """Keys whose scores grow along the sequence: every step moves the running maximum."""
     bt = Batch([(140, 900)], 1, 1, 128, 64, "bf16", seed=9)
