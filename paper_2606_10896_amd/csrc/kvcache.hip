@@ -351,7 +351,7 @@ __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
     } else {
       // the sequence of the wave's first row, then of this thread's
       int b = find_seq(a.s, __builtin_amdgcn_readfirstlane(t), 1, 1, 0).b;
-      while (a.s.cu[b + 1] <= (int)t) ++b;
+      while (b + 1 < a.s.batch && a.s.cu[b + 1] <= (int)t) ++b;
       p = a.s.total[b] - (a.s.cu[b + 1] - (int)t);
     }
     if (i >= a.q_items) return;
