@@ -27,17 +27,16 @@
 #include <type_traits>
 
 #include "flashgmm.h"
+#include "kv_plan.h"
 
 namespace {
+
+using namespace kv;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // 1/127 rounded to fp32
 constexpr float kInv127 = 1.0f / 127.0f;
-// partial results of a row at most: 1024 keys each at 131,072 keys
-constexpr int kMaxSplits = 128;
-// a launch has fewer than 2^32 threads
-constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 1;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -93,8 +92,6 @@ __device__ __forceinline__ void load_rows8(typename Vec8<T>::type* v, At at, int
     }
   }
 }
-
-__host__ __device__ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Barrier for what goes through LDS: unlike __syncthreads it does not wait for global stores.
 __device__ __forceinline__ void lds_barrier() {
@@ -1744,111 +1741,8 @@ int check_heads(const gmm_kv_cache* c, int32_t hq) {
   return GMM_OK;
 }
 
-// Row tiles and key ranges of an attention call.
-struct Plan {
-  int waves;               // k_attend_few: 4, or 8 for a whole row tile's keys in one workgroup
-  int rt;                  // k_attend_few: 16 rt rows a tile, 0 if it is k_attend_tile
-  int rows;                // k_attend_tile: rows of a tile
-  int64_t items;           // row tiles of a head
-  int tiles_token;
-  int chunk, splits;
-};
-
-constexpr int kCUs = 256;
-
-// Key ranges of k_attend_few: enough workgroups for every CU to hold two, whatever a range's
-// length (a workgroup's first loads take as long as some steps: 8 sequences of 4000 keys, 4
-// tokens and 32 rows each: 66 us in ranges of 128 keys, 32 in ranges of 512), and more where
-// ranges stay above 1024 keys, which evens out ragged lengths (64 sequences of up to 32,768 keys:
-// 811 us with 1024 workgroups, 686 with 2048, 657 with 4096, 652 with 8192).
-int64_t few_ranges(int64_t tiles, int64_t keys) {
-  const int64_t fill = cdiv(2 * kCUs, tiles), even = cdiv(32 * kCUs, tiles);
-  const int64_t long_ones = keys / 1024;
-  int64_t want = even < long_ones ? even : long_ones;
-  if (want < fill) want = fill;
-  return want > kMaxSplits ? kMaxSplits : want;
-}
-
-// rows of a tile above 64 are shared through LDS (k_attend_tile)
-int few_rows(int64_t rows, int d) { return rows <= 16 ? 1 : rows <= 32 || d > 128 ? 2 : 4; }
-
-// One workgroup of eight waves takes all keys of a row tile where these are few or there are
-// tiles for half of the CUs: nothing to join, one launch less.  (2048 keys, whole and split with
-// its join: 256 tiles 45 us, 48; 32 tiles 35 us, 18; 8 tiles of 1000 keys 21 us, 13.)
-bool whole_rows(int64_t keys, int64_t tiles, int rt, int d) {
-  return rt == 1 && d <= 128 && keys <= (tiles >= kCUs / 2 ? 2048 : 512);
-}
-
-Plan plan_dense(int heads, int page, int d, int64_t tokens, int32_t batch, int group,
-                int32_t max_pages) {
-  Plan p{};
-  const int64_t keys = (int64_t)max_pages * page;
-  const int64_t rows = cdiv(tokens, batch) * group;
-  int64_t want, unit;
-  if (rows > 64) {
-    // eight waves share a step's operands from 65 to 128 dimensions (2048 tokens on 34,816 keys:
-    // 0.97 ms, 1.12 in workgroups of four waves; 512 on 8512: 90 us, 132), but not for prompts
-    // that are most of their own context, whose few steps a tile of 128 rows ends earlier at the
-    // diagonal (32 heads on 8, eight waves and four: 2 prompts of 700 tokens 48 us, 30; 4: 54, 44;
-    // 16: 153, 132; one of 2000 91, 85; but 4 of 500 31, 33, and 8 of 2000 372, between 367 and
-    // 388).  Up to 64 the vector part
-    // takes longer than the matrix part, and three workgroups of four waves a CU hide more of it
-    // (prompts of 4000 tokens with a window, when it was chosen: 0.21 ms, 0.23); above 128 there
-    // are registers for four waves
-    const bool prompt = keys <= 2048 && keys * batch <= 2 * tokens;
-    p.rows = rows > 128 && d > 64 && d <= 128 && !prompt ? 256 : 128;
-    const int64_t tiles = tokens * group / p.rows;
-    p.items = tiles + batch;
-    // one workgroup a CU; keys are split where there are fewer row tiles than that
-    want = cdiv(kCUs, (tiles > 0 ? tiles : 1) * heads);
-    unit = 512;
-  } else {
-    p.rt = few_rows(rows, d);
-    p.items = tokens * group / (16 * p.rt) + batch;
-    want = few_ranges(p.items * heads, keys);
-    unit = 128;                      // a step of 32 keys for every wave
-    p.waves = whole_rows(keys, p.items * heads, p.rt, d) ? 8 : 4;
-    if (p.waves == 8) want = 1;
-  }
-  if (want > kMaxSplits) want = kMaxSplits;
-  const int64_t chunk = cdiv(cdiv(keys, want), unit) * unit;
-  p.chunk = (int)chunk;
-  p.splits = (int)cdiv(keys, chunk);
-  return p;
-}
-
-Plan plan_sel(int heads, int page, int d, int64_t tokens, int group, int32_t m) {
-  Plan p{};
-  p.rt = few_rows(group, d);
-  p.tiles_token = (int)cdiv(group, 16 * p.rt);
-  p.items = tokens * p.tiles_token;
-  int64_t want = few_ranges(p.items * heads, (int64_t)m * page);
-  p.waves = whole_rows((int64_t)m * page, p.items * heads, p.rt, d) ? 8 : 4;
-  if (p.waves == 8) want = 1;
-  const int least = page >= 128 ? 1 : 128 / page;
-  int64_t chunk = cdiv(m, want);
-  if (chunk < least) chunk = least;
-  p.chunk = (int)chunk;
-  p.splits = (int)cdiv(m, chunk);
-  return p;
-}
-
-int64_t part_bytes(int64_t tokens, int hq, int d, int splits) {
-  return splits <= 1 ? 0 : (int64_t)splits * tokens * hq * (d + 2) * 4;
-}
-
-int64_t score_row(int32_t max_pages) { return cdiv(max_pages, 4) * 4; }
-
 int64_t ws_need(const gmm_kv_cache* c, int64_t tokens, int hq, int32_t batch, int32_t max_pages) {
-  const int group = hq / c->heads;
-  int64_t need = tokens * c->heads * score_row(max_pages) * 4;
-  const Plan pd = plan_dense(c->heads, c->page, c->d, tokens, batch, group, max_pages);
-  const Plan ps = plan_sel(c->heads, c->page, c->d, tokens, group, GMM_KV_MAX_KEEP);
-  const int64_t a = part_bytes(tokens, hq, c->d, pd.splits);
-  const int64_t b = part_bytes(tokens, hq, c->d, ps.splits);
-  if (a > need) need = a;
-  if (b > need) need = b;
-  return cdiv(need + 256, 256) * 256;
+  return kv::ws_need(c->heads, c->page, c->d, tokens, hq, batch, max_pages, GMM_KV_MAX_KEEP);
 }
 
 int check_kv_ws(void* ws, size_t have, int64_t need) {
@@ -2133,12 +2027,20 @@ int gmm_kv_attend(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
   if (m > GMM_KV_MAX_KEEP) return GMM_ERR_UNSUPPORTED;
   if (tokens == 0) return GMM_OK;
   if (!q || !out || ((uintptr_t)out & 7)) return GMM_ERR_INVALID_ARG;
-  rc = check_kv_ws(ws, ws_bytes, ws_need(cache, tokens, hq, seqs->batch, seqs->max_pages));
+  const int group = hq / cache->heads;
+  const Plan p = sel ? plan_sel(cache->heads, cache->page, cache->d, tokens, group, m)
+                     : plan_dense(cache->heads, cache->page, cache->d, tokens, seqs->batch, group,
+                                  seqs->max_pages);
+  // the documented size, and, whatever that is, what this launch writes
+  int64_t need = ws_need(cache, tokens, hq, seqs->batch, seqs->max_pages);
+  const int64_t own = part_bytes(tokens, hq, cache->d, p.splits);
+  if (own > need) need = own;
+  rc = check_kv_ws(ws, ws_bytes, need);
   if (rc != GMM_OK) return rc;
   a.k = cache->k;
   a.v = cache->v;
   a.heads = cache->heads;
-  a.group = hq / cache->heads;
+  a.group = group;
   a.d = cache->d;
   a.q = q;
   a.qt = q_token_stride;
@@ -2152,9 +2054,6 @@ int gmm_kv_attend(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
   a.lse = lse;
   a.hq = hq;
   a.tokens = tokens;
-  const Plan p = sel ? plan_sel(a.heads, cache->page, a.d, tokens, a.group, m)
-                     : plan_dense(a.heads, cache->page, a.d, tokens, seqs->batch, a.group,
-                                  seqs->max_pages);
   a.chunk = p.chunk;
   a.splits = p.splits;
   a.tiles_token = p.tiles_token;
