@@ -31,6 +31,7 @@ struct Plan {
 // ranges stay above 1024 keys, which evens out ragged lengths (64 sequences of up to 32,768 keys:
 // 811 us with 1024 workgroups, 686 with 2048, 657 with 4096, 652 with 8192).
 inline int64_t few_ranges(int64_t tiles, int64_t keys) {
+  if (tiles < 1) tiles = 1;          // the workspace of no tokens is asked for, too
   const int64_t fill = cdiv(2 * kCUs, tiles), even = cdiv(32 * kCUs, tiles);
   const int64_t long_ones = keys / 1024;
   int64_t want = even < long_ones ? even : long_ones;

@@ -1,11 +1,13 @@
 """The launch plans of the paged cache's attention and its workspace, swept on the host: no GPU is
 needed to show that what a call writes fits into what it checks."""
+import ctypes
 import os
 import subprocess
 
 import pytest
 
 import paper_2606_10896_amd as gmm
+from paper_2606_10896_amd.kv import _CCache
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(os.path.dirname(gmm.__file__), "csrc")
@@ -25,3 +27,10 @@ def check(tmp_path_factory):
 
 def test_a_call_fits_into_its_workspace(check):
     check("covers")
+
+
+def test_the_workspace_of_no_tokens(check):
+    """A server's empty step: a size, and not a division by its zero tiles."""
+    cache = _CCache(1 << 20, 1 << 20, None, None, 10, 2, 64, 128, 1)
+    size = gmm.load_library().gmm_kv_workspace_bytes
+    assert 0 < size(ctypes.byref(cache), 0, 4, 3, 4) <= size(ctypes.byref(cache), 1, 4, 3, 4)
