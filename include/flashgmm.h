@@ -488,7 +488,8 @@ int gmm_kv_append(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
  * `batch` sequences with hq query heads and page tables of max_pages entries:
  * the page scores (tokens * heads * max_pages floats), or the partial results
  * of the key ranges that long contexts are split into, whichever is larger.
- * 0 when the shape is unsupported.
+ * It serves every call of up to these sizes on caches of this shape, with lists
+ * of any length.  0 when the shape is unsupported.
  */
 size_t gmm_kv_workspace_bytes(const gmm_kv_cache* cache, int64_t tokens, int32_t hq,
                               int32_t batch, int32_t max_pages);

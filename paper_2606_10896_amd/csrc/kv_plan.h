@@ -109,24 +109,53 @@ inline int64_t part_bytes(int64_t tokens, int hq, int d, int splits) {
 
 inline int64_t score_row(int32_t max_pages) { return cdiv(max_pages, 4) * 4; }
 
-// Partial results of a selection with lists of up to max_keep entries.  A list's ranges are
-// ceil(m / chunk) with chunk = ceil(m / want): never more than want, which grows with m, but not
-// monotone in m themselves (2016 entries may make 126 ranges where 4096 make 125).
-inline int64_t sel_bytes(int heads, int page, int d, int64_t tokens, int hq, int32_t max_keep) {
-  const Plan p = plan_sel(heads, page, d, tokens, hq / heads, max_keep);
-  const int64_t most = few_ranges(p.items * heads, (int64_t)max_keep * page);
-  return part_bytes(tokens, hq, d, (int)most);
+// The workspace is sized for every call of up to its sizes, not for one plan: fewer rows make
+// more ranges (17 tokens of 32 heads on 8 may take no partial results, 16 tokens 128 ranges), and
+// a list of m pages makes ceil(m / ceil(m / want)) of them, which does not grow with m (2016
+// entries may make 126 ranges where 4096 make 125).
+//
+// Each kind of plan makes s > 1 ranges only for tiles * heads <= a / (s - 1), a + 1 being the
+// workgroups it wants: it makes up to ceil((a + 1) / tiles) ranges.  A tile has at most c rows, so a
+// head has at most f(s) = c (a / ((s - 1) heads) + extra) of them.  most_rows returns the largest
+// s min(rows, f(s)) with 2 <= s <= most.  f falls with s, and s f(s) is convex: the largest value is at
+// the last s with f(s) >= rows, at the one after it, or at the end.
+inline int64_t most_rows(int64_t rows, int64_t c, int64_t a, int extra, int heads, int64_t most) {
+  if (most > kMaxSplits) most = kMaxSplits;
+  if (most > a / heads + 1) most = a / heads + 1;       // at least one tile
+  if (most < 2) return 0;
+  const auto all = [&](int64_t s) { return cdiv(s * c * a, (s - 1) * heads) + s * c * extra; };
+  // f(s) >= rows for s - 1 <= c a / (heads (rows - c extra))
+  const int64_t over = heads * (rows - c * extra);
+  int64_t s1 = over > 0 ? c * a / over + 1 : most;
+  if (s1 >= most) return most * rows;
+  int64_t res = s1 >= 2 ? s1 * rows : 0;
+  const int64_t next = all(s1 >= 2 ? s1 + 1 : 2), last = all(most);
+  if (next > res) res = next;
+  return last > res ? last : res;
 }
 
 inline int64_t ws_need(int heads, int page, int d, int64_t tokens, int hq, int32_t batch,
                        int32_t max_pages, int32_t max_keep) {
-  int64_t need = tokens * heads * score_row(max_pages) * 4;
-  const Plan pd = plan_dense(heads, page, d, tokens, batch, hq / heads, max_pages);
-  const int64_t a = part_bytes(tokens, hq, d, pd.splits);
-  const int64_t b = sel_bytes(heads, page, d, tokens, hq, max_keep);
-  if (a > need) need = a;
-  if (b > need) need = b;
-  return cdiv(need + 256, 256) * 256;
+  const int group = hq / heads;
+  const int64_t keys = (int64_t)max_pages * page, rows = tokens * group;
+  // k_attend_few, at most 64 rows a sequence: floor(rows / (16 rt)) + batch tiles, batch at least
+  // rows / 64; ranges have 128 keys, and 1024 beyond the first two workgroups a CU
+  const int64_t few = rows < 64 * (int64_t)batch ? rows : 64 * (int64_t)batch;
+  const int64_t c = d > 128 ? 22 : 32;       // 1 / (1 / (16 rt) + 1 / 64), rounded up
+  const int64_t long_ones = keys / 1024;
+  int64_t part = most_rows(few, c, 2 * kCUs - 1, 1, heads, cdiv(keys, 128));
+  const auto more = [&](int64_t v) { part = v > part ? v : part; };
+  more(most_rows(few, c, 32 * kCUs - 1, 1, heads, long_ones));
+  // k_attend_tile: tiles of up to 256 rows, ranges of 512 keys
+  more(most_rows(rows, 256, kCUs - 1, 1, heads, cdiv(keys, 512)));
+  // selected pages: whole tiles a token
+  const int64_t per = 16 * few_rows(group, d), ct = group < per ? group : per;
+  const int64_t kept = (int64_t)max_keep * page;
+  more(most_rows(rows, ct, 2 * kCUs - 1, 0, heads, kMaxSplits));
+  more(most_rows(rows, ct, 32 * kCUs - 1, 0, heads, kept / 1024));
+  const int64_t scores = tokens * heads * score_row(max_pages) * 4;
+  part *= (int64_t)heads * (d + 2) * 4;
+  return cdiv((part > scores ? part : scores) + 256, 256) * 256;
 }
 
 }  // namespace kv

@@ -1,15 +1,18 @@
 // Sweeps the launch plans of the paged cache's attention on the host.  kv_plan_check RULE prints
 // the first size that breaks the rule and returns 1, or returns 0.
 //   covers   what a call's plan writes fits into the workspace of its sizes
+//   grows    a workspace for larger sizes serves smaller ones
 #include <stdio.h>
 #include <string.h>
+
+#include <initializer_list>
 
 #include "kv_plan.h"
 
 using namespace kv;
 
 static const int kKeep = 4096;       // pages of a selection's lists at most
-static const int kHeads[] = {1, 2, 3, 8}, kGroups[] = {1, 4, 16, 64}, kDims[] = {128, 256};
+static const int kHeads[] = {1, 2, 3, 5, 8, 16}, kGroups[] = {1, 4, 16, 64}, kDims[] = {128, 256};
 static const int kPages[] = {32, 64, 128, 256};
 
 static bool fits(int heads, int group, int d, int page, long tokens, int batch, int max_pages, int m) {
@@ -29,7 +32,7 @@ static int covers() {
     for (int group : kGroups)
       for (int d : kDims)
         for (int page : kPages)
-          for (long tokens = 1; tokens <= 700; tokens += tokens < 140 ? 1 : 37) {
+          for (long tokens = 1; tokens <= 2100; tokens += tokens < 140 ? 1 : tokens < 1100 ? 37 : 333) {
             // lists of every length; a table of one page has the smallest score rows
             for (int m = 1; m <= kKeep; m += m < 600 ? 1 : 7)
               if (!fits(heads, group, d, page, tokens, 1, 1, m)) return 1;
@@ -40,7 +43,61 @@ static int covers() {
   return 0;
 }
 
+static int64_t need_of(int heads, int group, int d, int page, long tokens, int batch, int max_pages) {
+  return ws_need(heads, page, d, tokens, heads * group, batch, max_pages, kKeep);
+}
+
+// along every size, the others held
+static int grows() {
+  static const long kTokens[] = {1, 2, 5, 16, 17, 33, 64, 65, 100, 255, 512, 1000, 2047, 2048, 20000};
+  static const int kBatches[] = {1, 2, 3, 8, 64, 1000}, kWidths[] = {1, 3, 16, 32, 100, 2048, 60000};
+  for (int heads = 1; heads <= 16; ++heads)
+    for (int d : kDims)
+      for (int page : kPages)
+        for (int group = 1; group <= 64; ++group) {
+          for (int batch : kBatches)
+            for (int width : kWidths) {
+              int64_t last = 0;
+              for (long tokens : kTokens) {
+                const int64_t need = need_of(heads, group, d, page, tokens, batch, width);
+                if (need < last ||
+                    need < need_of(heads, group > 1 ? group - 1 : 1, d, page, tokens, batch, width) ||
+                    need < need_of(heads, group, d, page, tokens - 1, batch, width) ||
+                    need < need_of(heads, group, d, page, tokens, batch > 1 ? batch - 1 : 1, width) ||
+                    need < need_of(heads, group, d, page, tokens, batch, width > 1 ? width - 1 : 1)) {
+                  printf("heads %d group %d d %d page %d tokens %ld batch %d max_pages %d: %lld bytes, "
+                         "more for a smaller size\n", heads, group, d, page, tokens, batch, width,
+                         (long long)need);
+                  return 1;
+                }
+                last = need;
+              }
+            }
+          if (group > 4 && heads > 2) group += 6;
+        }
+  // every count of tokens and of sequences of some shapes
+  for (int heads : {1, 2, 8})
+    for (int group : {1, 4, 7})
+      for (int d : kDims)
+        for (int width : {32, 2048}) {
+          int64_t last = 0;
+          for (long tokens = 0; tokens <= 9000; ++tokens) {
+            const int64_t need = need_of(heads, group, d, 64, tokens, 1, width);
+            if (need < last) return printf("tokens %ld heads %d group %d\n", tokens, heads, group), 1;
+            last = need;
+          }
+          last = 0;
+          for (int batch = 1; batch <= 3000; ++batch) {
+            const int64_t need = need_of(heads, group, d, 64, 3000, batch, width);
+            if (need < last) return printf("batch %d heads %d group %d\n", batch, heads, group), 1;
+            last = need;
+          }
+        }
+  return 0;
+}
+
 int main(int argc, char** argv) {
   if (argc == 2 && !strcmp(argv[1], "covers")) return covers();
+  if (argc == 2 && !strcmp(argv[1], "grows")) return grows();
   return 2;
 }
