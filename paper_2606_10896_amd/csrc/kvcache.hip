@@ -1226,6 +1226,11 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
 // The running maximum is only moved (and the results rescaled) when a step's weights at the old
 // one add up to more than 2^8, or a row sees its first key: a common factor cancels in the end,
 // and weights up to 2^8 are as exact as those up to 1.  So most steps need no maximum at all.
+// A weight is 2^(score scale - maximum), one fma, as long as the rounding of the maximum, a product
+// with the scale itself, is small against 1.  Once a maximum passes 2^10 the wave keeps them
+// unscaled and takes the difference before the scaling, where it is exact for the largest scores,
+// whatever their size (fp32 neighbours at 2^33 lie 1024 apart, and a rounded maximum would make
+// weights of 2^512, or none).
 //
 // Rows of the score tile are keys in the order that makes its accumulator the B operand of the
 // second product: row r is key r with bits 2 and 3 exchanged.
@@ -1393,6 +1398,7 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
   f32x16 o[ND], sc[HV];
   V8 pw[HV][2];
   float mx = -INFINITY, sum = 0.0f;
+  bool coarse = false;                            // of the wave: mx is unscaled
 #pragma unroll
   for (int hv = 0; hv < HV; ++hv) pw[hv][0] = pw[hv][1] = V8((T)0.0f);
 #pragma unroll
@@ -1411,6 +1417,9 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
 
   const auto matrix = [&](auto parity) {
     constexpr int cur = decltype(parity)::value;
+    // nothing of the vector part, nor the scalar loads of page numbers, moves between these
+    // products: a scalar load in flight turns every wait for an operand into one for all of them
+    __builtin_amdgcn_sched_barrier(0);
     products(cur ^ 1);
 #pragma unroll
     for (int hv = 0; hv < HV; ++hv) sc[hv] = f32x16(0.0f);
@@ -1463,9 +1472,8 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
         }
     }
     // weights at the present maximum; their sum says whether it has to move
-    const auto weights = [&] {
+    const auto weights = [&](float base) {
       float z = 0.0f;
-      const float base = mx == -INFINITY ? 0.0f : mx;
 #pragma unroll
       for (int hv = 0; hv < HV; ++hv)
 #pragma unroll
@@ -1477,9 +1485,9 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
       return z;
     };
     float z = 0.0f;
-    bool move = __ballot(mx == -INFINITY && lim >= key0) != 0;
+    bool move = coarse || __ballot(mx == -INFINITY && lim >= key0) != 0;
     if (!move) {
-      z = weights();
+      z = weights(mx == -INFINITY ? 0.0f : mx);
       move = __ballot(!(z <= 256.0f)) != 0;
     }
     if (move) {
@@ -1488,13 +1496,25 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
       for (int hv = 0; hv < HV; ++hv)
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[hv][i]);
-      const float m = fmaxf(mx, fmaxf(top, __shfl_xor(top, 32)) * sc2);
-      const float f = m == -INFINITY ? 1.0f : exp2_fast(mx - m);
+      top = fmaxf(top, __shfl_xor(top, 32));
+      float m = fmaxf(mx, top * sc2);
+      if (!coarse && __ballot(m > -INFINITY && !(fabsf(m) <= 1024.0f)) != 0) {
+        coarse = true;
+        mx /= sc2;                       // of at most 2^10: off by no more than 2^-13 when scaled
+      }
+      if (coarse) m = fmaxf(mx, top);
+      const float f = m == -INFINITY ? 1.0f : exp2_fast(coarse ? (mx - m) * sc2 : mx - m);
       mx = m;
       sum *= f;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) o[dt] *= f;
-      z = weights();
+      float base = m == -INFINITY ? 0.0f : m;
+      if (coarse) {
+#pragma unroll
+        for (int hv = 0; hv < HV; ++hv) sc[hv] -= base;
+        base = 0.0f;
+      }
+      z = weights(base);
     }
     sum += z;
     // the weights are formed in this part, and not where they are next used
@@ -1561,7 +1581,7 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
     products(1);
   }
 
-  const float z = sum + __shfl_xor(sum, 32);
+  const float z = sum + __shfl_xor(sum, 32), top = coarse ? mx * sc2 : mx;
   const int r = wr0 + c32;
   if (r >= rows) return;
   const int rr = r0 + r, ti = rr / G, hh = rr - ti * G;
@@ -1588,9 +1608,9 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
     }
   if (half == 0) {
     if (a.splits == 1) {
-      if (a.lse) a.lse[orow] = z > 0.0f ? (mx + log2_fast(z)) * kLn2 : (z == 0.0f ? -INFINITY : z);
+      if (a.lse) a.lse[orow] = z > 0.0f ? (top + log2_fast(z)) * kLn2 : (z == 0.0f ? -INFINITY : z);
     } else {
-      a.part_ml[pr * 2] = mx;
+      a.part_ml[pr * 2] = top;
       a.part_ml[pr * 2 + 1] = z;
     }
   }
