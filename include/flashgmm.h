@@ -533,7 +533,8 @@ int gmm_kv_select(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
  * dtype, with what the rounding leaves as a second term where a sequence has
  * up to 64 query rows a cache head in the call's mean (tokens x group), and
  * without it above (an error of a unit roundoff of dtype per weight, as the
- * result's own rounding).
+ * result's own rounding).  GMM_F16 has no small numbers: there a weight is kept
+ * down to 2^-40 of the row's largest in the first case, 2^-32 in the second.
  * What slots past a sequence's last key hold does not matter, nor
  * does a key that a row does not see.  A NaN or infinite value (of v) reaches
  * every row whose step of 32 or 64 keys it lies in, also rows of the same call

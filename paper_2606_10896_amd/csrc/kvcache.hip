@@ -878,6 +878,14 @@ __global__ __launch_bounds__(NT) void k_select_top(Seqs s, const float* __restri
 }
 
 // ---------------------------------------------------------------- attention
+// fp16 has no weights below 2^-25 (half its smallest number), and a million of them may weigh as
+// much as the largest one.  Weights of fp16 caches are formed 2^15 times as large by
+// k_attend_few, where they are at most 1 otherwise (2^-40 of the largest still counts), and 2^7
+// times by k_attend_tile, where a step's may add up to 2^8 (2^-32).  The sums carry the same factor,
+// and a row's maximum is given lower by its logarithm, so the joins need not know of it.
+template <typename T> constexpr float kFewShift = std::is_same<T, _Float16>::value ? 15.0f : 0.0f;
+template <typename T> constexpr float kTileShift = std::is_same<T, _Float16>::value ? 7.0f : 0.0f;
+
 struct AttendArgs {
   Seqs s;
   const void* k;
@@ -1100,15 +1108,15 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
       const float base = m == -INFINITY ? 0.0f : m;
       const float alpha = exp2_fast(mx[rt] - base);
       mx[rt] = m;
-      // weights in [0, 1] for the matrix product: rounded to T, and what the rounding leaves (the
-      // matrix unit waits for memory here, a second product costs nothing)
+      // weights in [0, 1] (times 2^kFewShift) for the matrix product: rounded to T, and what the
+      // rounding leaves (the matrix unit waits for memory here, a second product costs nothing)
       V8 p, rest;
       float z = 0.0f;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float e = exp2_fast(sc[t][i] - base);
+          const float e = exp2_fast(sc[t][i] - base + kFewShift<T>);
           z += e;
           p[4 * t + i] = (T)e;
           rest[4 * t + i] = (T)(e - (float)p[4 * t + i]);
@@ -1197,10 +1205,12 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
       }
       if (g == 0) {
         if (a.splits == 1) {
-          if (a.lse) a.lse[orow] = z > 0.0f ? (mm + log2_fast(z)) * kLn2 : (z == 0.0f ? -INFINITY : z);
+          if (a.lse)
+            a.lse[orow] = z > 0.0f ? (mm - kFewShift<T> + log2_fast(z)) * kLn2
+                                   : (z == 0.0f ? -INFINITY : z);
         } else {
           float* ml = a.part_ml + ((int64_t)split * a.tokens * a.hq + orow) * 2;
-          ml[0] = mm;
+          ml[0] = mm - kFewShift<T>;
           ml[1] = z;
         }
       }
@@ -1472,6 +1482,7 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
         }
     }
     // weights at the present maximum; their sum says whether it has to move
+    constexpr float shift = kTileShift<T>, limit = shift > 0.0f ? 0x1p15f : 0x1p8f;
     const auto weights = [&](float base) {
       float z = 0.0f;
 #pragma unroll
@@ -1487,8 +1498,8 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
     float z = 0.0f;
     bool move = coarse || __ballot(mx == -INFINITY && lim >= key0) != 0;
     if (!move) {
-      z = weights(mx == -INFINITY ? 0.0f : mx);
-      move = __ballot(!(z <= 256.0f)) != 0;
+      z = weights(mx == -INFINITY ? 0.0f : mx - shift);
+      move = __ballot(!(z <= limit)) != 0;
     }
     if (move) {
       float top = sc[0][0];
@@ -1514,7 +1525,7 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
         for (int hv = 0; hv < HV; ++hv) sc[hv] -= base;
         base = 0.0f;
       }
-      z = weights(base);
+      z = weights(base - shift);
     }
     sum += z;
     // the weights are formed in this part, and not where they are next used
@@ -1581,7 +1592,7 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
     products(1);
   }
 
-  const float z = sum + __shfl_xor(sum, 32), top = coarse ? mx * sc2 : mx;
+  const float z = sum + __shfl_xor(sum, 32), top = (coarse ? mx * sc2 : mx) - kTileShift<T>;
   const int r = wr0 + c32;
   if (r >= rows) return;
   const int rr = r0 + r, ti = rr / G, hh = rr - ti * G;

@@ -87,3 +87,40 @@ def test_large_scores_that_differ_by_little(gmm, dtype, offset, ramp, seqs, d):
     q = q.to(bt.dt)
     scale = abs(offset) / 128.0
     _check(bt, _attend(gmm, bt, q=q, scale=scale), attend64(bt, scale, q=q))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("seqs,hq,d", [([(1, 60000)], 2, 64), ([(8, 9000)], 1, 64), ([(100, 8300)], 1, 64),
+                                       ([(200, 9000)], 1, 128), ([(1, 9000)], 64, 192)])
+def test_many_small_weights_under_one_large_one(gmm, dtype, seqs, hq, d):
+    """Weights of e^-18.25, each below the smallest number of fp16, that the row's sum keeps and its
+    result has to keep as well."""
+    print(f"small weights {dtype} {seqs} {hq} {d}", flush=True)
+    bt = Batch(seqs, hq, 1, d, 64, dtype, seed=3)
+    n, t = seqs[0]
+    keys = torch.zeros(1, t, d)
+    keys[:, 1:, 0] = -18.25
+    _with_keys(bt, 0, keys)
+    g = torch.Generator().manual_seed(4)
+    bt.vals[0] = (2.0 + torch.randn(1, t, d, generator=g)).to(bt.dt)
+    bt.vals[0][:, 0] = 0.0
+    for s in range(t):
+        bt.v[int(bt.pages[0, s // 64]), :, :, s % 64] = bt.vals[0][:, s]
+    q = torch.zeros(n, hq, d, dtype=bt.dt)
+    q[:, :, 0] = 8.0
+    out, lse = _attend(gmm, bt, q=q, scale=0.125)
+    w, v = math.exp(-18.25), bt.vals[0][0].double()
+    many = n * hq > 64
+    for i in range(n):
+        held = t - n + i + 1
+        z = 1 + (held - 1) * w
+        o = w * v[1:held].sum(0) / z
+        u = 2.0 ** -11 if dtype == "f16" else 2.0 ** -8
+        # one rounding of the result; of a weight, exact to its square where the rest is added; a
+        # fp32 exponential of -26; for fp16 half the spacing of its smallest weights
+        tol = u * o.abs() + (u if many else u * u) * w * v[1:held].abs().sum(0) / z + 1e-5 * o.abs()
+        if dtype == "f16":
+            tol += held * (2.0 ** -32 if many else 2.0 ** -40) * v.abs().max() + 2.0 ** -25
+        for j in range(hq):
+            assert bool(((out[i, j] - o).abs() <= tol).all()), float(((out[i, j] - o).abs() - tol).max())
+            assert abs(float(lse[i, j]) - math.log(z)) <= 2.0 ** -20
