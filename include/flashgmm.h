@@ -506,6 +506,8 @@ size_t gmm_kv_workspace_bytes(const gmm_kv_cache* cache, int64_t tokens, int32_t
  * keep_last visible pages are always taken (keep_last >= 1: the page that holds
  * the token itself may hold later tokens of the same call, whose keys are in
  * its box).
+ * A table entry out of range holds no key and is never taken, also not among
+ * the first and last, which are counted over all entries of visible keys.
  *   q [tokens, hq, d], rows contiguous, strides in elements
  *   idx [tokens, heads, m] int32: indexes into the sequence's page table,
  *   ascending, -1 behind the last where fewer than m pages are visible

@@ -655,7 +655,7 @@ __global__ __launch_bounds__(256, S <= 4 ? 4 : 2) void k_select_score(SelectArgs
 #pragma unroll
       for (int t = 0; t < TB; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) best[t][i] = -INFINITY;
+        for (int i = 0; i < 4; ++i) best[t][i] = -FLT_MAX;
       for (int ct = 0; ct < a.col_tiles; ++ct) {
         const int8_t* qc = q8 + (size_t)(ct * 16 + n16) * stride;
         i32x4 qf[S];
@@ -685,6 +685,15 @@ __global__ __launch_bounds__(256, S <= 4 ? 4 : 2) void k_select_score(SelectArgs
         for (int t = 0; t < TB; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) best[t][i] = fmaxf(best[t][i], __shfl_xor(best[t][i], o));
+      // entries out of range hold no key: below every score
+      const uint64_t none = __ballot(phys < 0);
+      if (none != 0) {
+#pragma unroll
+        for (int t = 0; t < TB; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (none >> (16 * (t0 + t) + 4 * g + i) & 1) best[t][i] = -INFINITY;
+      }
       const int tt = n16 >> a.col_shift;
       if ((n16 & ((1 << a.col_shift) - 1)) == 0 && tt < toks) {
         float* out = a.score + ((int64_t)(row0 + tok0 + tt) * a.heads + head) * a.row;
@@ -726,8 +735,28 @@ __global__ __launch_bounds__(NT) void k_select_top(Seqs s, const float* __restri
   const int64_t nv64 = slot < 0 ? 0 : (slot >> s.page_shift) + 1;
   const int nv = (int)min(nv64, (int64_t)s.max_pages);
   int32_t* out = idx + r * m;
-  if (nv <= m) {
-    for (int i = tid; i < m; i += NT) out[i] = i < nv ? i : -1;
+  if (nv <= m) {                          // all that hold keys
+    int at = 0;
+    for (int i0 = 0; i0 < nv; i0 += NT) {
+      const int i = i0 + tid;
+      const bool in = i < nv && phys_page(s, sq.b, i) >= 0;
+      const uint64_t any = __ballot(in);
+      int mine = at + __popcll(any & ((1ull << lane) - 1));
+      if constexpr (NW == 1) {
+        at += __popcll(any);
+      } else {
+        if (lane == 0) scan[wave] = __popcll(any);
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          if (w < wave) mine += scan[w];
+          at += scan[w];
+        }
+        __syncthreads();
+      }
+      if (in) out[mine] = i;
+    }
+    for (int i = at + tid; i < m; i += NT) out[i] = -1;
     return;
   }
   const float* sc = score + r * row;
@@ -743,9 +772,10 @@ __global__ __launch_bounds__(NT) void k_select_top(Seqs s, const float* __restri
     for (int j = 0; j < 4; ++j) {
       const int p = first + i + j;
       const bool keep = p < keep_first || p >= nv - keep_last;
+      const bool none = p >= nv || f[j] == -INFINITY;       // past the last, or out of range
       const uint32_t k = score_key(f[j]);
-      key[i + j] = p >= nv ? 0 : keep ? 0xFFFFFFFFu : k;
-      if (p < nv && !keep) {
+      key[i + j] = none ? 0 : keep ? 0xFFFFFFFFu : k;
+      if (!none && !keep) {
         kmin = min(kmin, k);
         kmax = max(kmax, k);
       }
@@ -800,13 +830,17 @@ __global__ __launch_bounds__(NT) void k_select_top(Seqs s, const float* __restri
       for (int j = 0; j < 3; ++j) n[j] += cnt[buf][w][j];
     buf ^= 1;
   };
-  // more than m keys are >= lo, less than m are >= hi (nv > m; the kept ones are at most m)
+  // more than m keys are >= lo, less than m are >= hi (or m or fewer hold keys: all are taken; the
+  // kept ones are at most m)
   uint32_t lo = kmin, hi = kmax + 1, above = 0;       // above: take every key > above
   int ties = 0, n[3];
   bool exact = false;
-  count(hi, hi, hi, n);
+  count(hi, 1, 1, n);
   int n_hi = n[0];
-  if (n_hi == m) {
+  const int held = n[1];
+  if (held <= m) {
+    exact = true;
+  } else if (n_hi == m) {
     above = hi - 1;
     exact = true;
   }
@@ -875,6 +909,7 @@ __global__ __launch_bounds__(NT) void k_select_top(Seqs s, const float* __restri
 #pragma unroll
   for (int i = 0; i < PT; ++i)
     if ((take[i >> 5] >> (i & 31) & 1) && at < m) out[at++] = first + i;
+  for (int i = held + tid; i < m; i += NT) out[i] = -1;
 }
 
 // ---------------------------------------------------------------- attention
