@@ -2041,6 +2041,7 @@ int gmm_kv_select(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
   a.q = q;
   a.qt = q_token_stride;
   a.qh = q_head_stride;
+  a.q_vec = aligned16(q) && (q_token_stride | q_head_stride) % 8 == 0;
   a.heads = cache->heads;
   a.group = hq / cache->heads;
   a.d = cache->d;

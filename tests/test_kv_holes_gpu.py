@@ -89,3 +89,26 @@ def test_a_table_without_a_page(gmm):
     assert bool((got[:2] == -1).all())
     assert got[2, 0].tolist() == [0, 1, 2, -1, -1]
     assert bool((_select(gmm, bt, box, scale, 20)[:2] == -1).all())
+
+
+@pytest.mark.parametrize("d", [16, 96, 128, 240])
+def test_query_rows_of_any_alignment(gmm, d):
+    """Rows that allow 16-byte loads and rows that do not: by address, by token and by head stride."""
+    bt = Batch([(5, 900), (1, 70)], 6, 2, d, 32, "bf16", seed=d)
+    box, scale = bt.boxes()
+    cache = gmm.KVCache(bt.k.cuda(), bt.v.cuda(), box.cuda(), scale.cuda())
+    ws = gmm.kv_workspace(cache, bt.rows, 6, 2, bt.width)
+    args = bt.cu.cuda(), bt.total.cuda(), bt.pages.cuda()
+    want = select_held(bt, box, scale, 6, 1, 1)
+    q = bt.q.cuda()
+
+    def view(offset, token, head):
+        flat = torch.zeros(offset + bt.rows * token, dtype=bt.dt, device="cuda")
+        x = flat.as_strided((bt.rows, 6, d), (token, head, 1), offset)
+        x.copy_(q)
+        return x
+    for x in (q, view(0, 6 * d, d), view(8, 6 * d + 8, d), view(1, 6 * d, d), view(0, 6 * d + 3, d),
+              view(0, 6 * d + 24, d + 4), view(0, 6 * d + 48, d + 8)):
+        idx = torch.full((bt.rows, 2, 6), 77, dtype=torch.int32, device="cuda")
+        gmm.gmm_kv_select(cache, x, *args, idx, ws)
+        assert torch.equal(idx.cpu(), want)
