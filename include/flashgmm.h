@@ -537,10 +537,11 @@ int gmm_kv_select(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
  * without it above (an error of a unit roundoff of dtype per weight, as the
  * result's own rounding).  GMM_F16 has no small numbers: there a weight is kept
  * down to 2^-40 of the row's largest in the first case, 2^-32 in the second.
- * What slots past a sequence's last key hold does not matter, nor
- * does a key that a row does not see.  A NaN or infinite value (of v) reaches
- * every row whose step of 32 or 64 keys it lies in, also rows of the same call
- * that do not see its key (a weight of 0 times it).
+ * What slots past a sequence's last key hold does not matter, nor does a key or
+ * a value that a row does not see, whatever it holds.  A NaN or infinite value
+ * (of v) is, in its dimension, the result of every row that sees it (calls that
+ * meet one take up to three times as long); a score that is NaN or +infinity
+ * makes its row NaN.
  */
 int gmm_kv_attend(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t tokens,
                   const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t hq,

@@ -954,6 +954,173 @@ __device__ __forceinline__ void mark_empty(const AttendArgs& a, int split, int r
   ml[1] = 0.0f;
 }
 
+// Values that some rows of a tile do not see pass through the same matrix product as those they do
+// see, with a weight of 0, and 0 times a NaN or an infinity would reach them.  Where a step of
+// 32 keys holds such keys (later tokens', or of windows that have moved on: before `low` or from
+// `from` on), the kernels put 0 for every value that is not finite, and if there was any,
+// add_not_finite gives it to the rows that see it: a positive weight times it is itself.  A result
+// that is no number although the row's sum is one starts from 0 and gets what the row sees of all
+// keys (an infinity times the rest of a weight's rounding, which may be 0 or negative, is not what
+// the row holds).
+__device__ __forceinline__ bool mixed_step(int key0, int from, int low) {
+  return key0 + 32 > from || key0 < low;
+}
+
+// The signs of a word's two elements are set where the exponent is all ones, of an infinity or a
+// NaN: adding the lowest exponent bit carries.
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite_signs(uint32_t w) {
+  constexpr bool f16 = std::is_same<T, _Float16>::value;
+  return ((w & (f16 ? 0x7C007C00u : 0x7F807F80u)) + (f16 ? 0x04000400u : 0x00800080u)) & 0x80008000u;
+}
+
+// Puts 0 in N operands of 8 slots from key for what is not finite, and for slots from `end` on,
+// which may hold anything; returns 0 unless a key before `end` had such a value.
+template <typename T, int N>
+__device__ __forceinline__ uint32_t put_zeros(typename Vec8<T>::type* v, int key, int end) {
+  uint4 u[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) u[i] = __builtin_bit_cast(uint4, v[i]);
+  uint32_t any = 0;
+  const auto word = [&](int j, auto at) {
+    const int k = key + 2 * j;
+    const uint32_t held = k + 1 < end ? 0xFFFFFFFFu : k < end ? 0xFFFFu : 0u;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      uint32_t& w = at(u[i]);
+      w &= held;
+      const uint32_t bad = not_finite_signs<T>(w) >> 15;
+      any |= bad;
+      asm volatile("" : "+v"(any));      // one after another: a tree would keep all in registers
+      w &= ~((bad << 16) - bad);
+    }
+  };
+  word(0, [](uint4& x) -> uint32_t& { return x.x; });
+  word(1, [](uint4& x) -> uint32_t& { return x.y; });
+  word(2, [](uint4& x) -> uint32_t& { return x.z; });
+  word(3, [](uint4& x) -> uint32_t& { return x.w; });
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = __builtin_bit_cast(typename Vec8<T>::type, u[i]);
+  return any;
+}
+
+// A workgroup's tile, kept in LDS for what comes after its loop.
+struct Tile {
+  int b, row0, n, total;     // of its sequence
+  int r0, rows, tok;         // its rows, of the sequence's; its token (selection)
+};
+
+// The kernel's arguments, read again where they are used.
+__device__ __forceinline__ const AttendArgs& args_again() {
+  auto* p = (const __attribute__((address_space(4))) AttendArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const AttendArgs*)p;
+}
+
+// The rows of a tile, ra .. rb - 1, that a dimension's results have got an infinity of one sign
+// for: those before lo and those from hi on.  (A NaN is both signs.)
+struct Had {
+  int lo, hi;
+  __device__ __forceinline__ void take(int first, int last) {
+    if (first <= lo) lo = max(lo, last);
+    if (last >= hi) hi = min(hi, first);
+  }
+};
+
+// x, not finite, is added to dimension dim of the results of the rows that see the key, unless they
+// have got it: the same again changes nothing.
+template <typename T>
+__device__ __forceinline__ void add_to_rows(const Tile& tile, int ra, int rb, int key, int dim, float x,
+                                            Had& pos, Had& neg) {
+  const AttendArgs& a = args_again();
+  const int64_t slot0 = (int64_t)tile.total - tile.n;
+  const int first = (int)max((int64_t)ra, (key - slot0) * a.group - tile.r0);
+  const int last = a.window > 0
+      ? (int)min((int64_t)rb, (key + (int64_t)a.window - slot0) * a.group - tile.r0) : rb;
+  if (first >= last) return;
+  const bool p = !(x < 0.0f), n = !(x > 0.0f);
+  const int begin = max(first, min(p ? pos.lo : rb, n ? neg.lo : rb));
+  const int end = min(last, max(p ? pos.hi : ra, n ? neg.hi : ra));
+#pragma unroll 1
+  for (int r = begin; r < end; ++r) {
+    const int rr = tile.r0 + r, ti = rr / a.group;
+    const int64_t orow = (int64_t)(tile.row0 + ti) * a.hq + blockIdx.x % a.heads * a.group +
+                         (rr - ti * a.group);
+    if (a.splits == 1) {
+      T* o = (T*)a.out + orow * a.d + dim;
+      *o = (T)((float)*o + x);
+    } else {
+      a.part_o[((int64_t)blockIdx.y * a.tokens * a.hq + orow) * a.d + dim] += x;
+    }
+  }
+  if (p) pos.take(first, last);
+  if (n) neg.take(first, last);
+}
+
+// By a wave, for the rows ra .. rb - 1 of the workgroup's tile; whole: over all its keys, and not
+// only those of mixed steps.  It is rare: what it needs is read again, so that
+// nothing is kept for it in registers through a kernel's loop.
+template <typename T, bool SEL>
+__device__ void add_not_finite(const Tile& tile, int ra, int rb, bool whole) {
+  const AttendArgs& a = args_again();
+  __threadfence_block();               // other lanes wrote the rows
+  const int lane = threadIdx.x & 63, P = 1 << a.s.page_shift, d = a.d;
+  const int head = blockIdx.x % a.heads, split = blockIdx.y, sub_shift = a.s.page_shift - 5;
+  const int b = __builtin_amdgcn_readfirstlane(tile.b);
+  const int total = __builtin_amdgcn_readfirstlane(tile.total);
+  const int n = __builtin_amdgcn_readfirstlane(tile.n);
+  const int r0 = __builtin_amdgcn_readfirstlane(tile.r0);
+  const int32_t* list = nullptr;
+  int st0, st1, kend, from, low = 0;
+  {
+    const int rows = __builtin_amdgcn_readfirstlane(tile.rows);
+    const int64_t first = (int64_t)total - n + r0 / a.group;          // slots of the first and last row
+    const int64_t last = SEL ? first : (int64_t)total - n + (r0 + rows - 1) / a.group;
+    const int64_t held = min((int64_t)total, (int64_t)a.s.max_pages << a.s.page_shift);
+    if constexpr (SEL) {               // all rows are one token's
+      kend = (int)max((int64_t)0, min(held, first + 1));
+      st0 = (split * a.chunk) << sub_shift;
+      st1 = min((split + 1) * a.chunk, a.m) << sub_shift;
+      list = a.sel + ((int64_t)__builtin_amdgcn_readfirstlane(tile.tok) * a.heads + head) * a.m;
+    } else {
+      const int64_t klo = a.window > 0 ? max((int64_t)0, first - a.window + 1) : 0;
+      kend = (int)max((int64_t)0, min(min(held, last + 1), ((int64_t)split + 1) * a.chunk));
+      st0 = (int)(max((int64_t)split * a.chunk, klo) >> 5);
+      st1 = (kend + 31) >> 5;
+      if (a.window > 0) low = (int)max((int64_t)0, last - a.window + 1);
+    }
+    from = (int)max((int64_t)0, min(first + 1, (int64_t)kend));
+  }
+#pragma unroll 1
+  for (int dim = lane; dim - lane < d; dim += 64) {
+    Had pos{ra, rb}, neg{ra, rb};
+#pragma unroll 1
+    for (int st = st0; st < st1; ++st) {
+      if (__ballot(dim < d && (pos.lo < pos.hi || neg.lo < neg.hi)) == 0) break;
+      int64_t key64 = (int64_t)st << 5;
+      if constexpr (SEL)
+        key64 = ((int64_t)list[st >> sub_shift] << a.s.page_shift) + 32 * (st & ((1 << sub_shift) - 1));
+      if (key64 < 0 || key64 >= kend) continue;
+      const int key0 = (int)key64;
+      if (!whole && !mixed_step(key0, from, low)) continue;
+      const int phys = phys_page(a.s, b, key0 >> a.s.page_shift);
+      if (phys < 0 || dim >= d) continue;
+      const T* v = (const T*)a.v + (((int64_t)phys * a.heads + head) * d + dim) * P + (key0 & (P - 1));
+#pragma unroll 1
+      for (int at = 0; at < 32; at += 8) {
+        const uint4 u = load16<uint4>(v + at);
+        if ((not_finite_signs<T>(u.x) | not_finite_signs<T>(u.y) | not_finite_signs<T>(u.z) |
+             not_finite_signs<T>(u.w)) == 0)
+          continue;
+#pragma unroll 1
+        for (int e = at; e < at + 8 && key0 + e < kend; ++e)
+          if (!(fabsf((float)v[e]) <= FLT_MAX))
+            add_to_rows<T>(tile, ra, rb, key0 + e, dim, (float)v[e], pos, neg);
+      }
+    }
+  }
+}
+
 // A few query rows (16 RT: tokens x heads of a group) against a range of keys; the NW waves take
 // every NW-th step of 32 keys each, straight from memory into matrix operands, and are joined at
 // the end.  Every byte of the cache is read by one wave once, so LDS would only add a trip.  The
@@ -964,12 +1131,14 @@ __device__ __forceinline__ void mark_empty(const AttendArgs& a, int split, int r
 // the weights' rounding as a second product takes 3 % of the former (633 us without) and brings
 // the error from 1.3 times the result's rounding to that rounding.
 template <typename T, int NS, int RT, bool SEL, int NW>
-__global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(AttendArgs a) {
+__global__ __launch_bounds__(64 * NW, NS * RT <= 6 ? 2 : 1) void k_attend_few(AttendArgs a) {
   typedef typename Vec8<T>::type V8;
   constexpr int ND = 2 * NS;                 // 16-dimension tiles of the result
   constexpr int R = 16 * RT;
   constexpr int BUF = NS * RT <= 4 ? 2 : 1;  // steps in registers
   __shared__ float sm[NW][R], sl[NW][R];
+  __shared__ int spoilt[NW];                 // a value of a mixed step is not finite
+  __shared__ Tile tile;
   __shared__ f32x4 so[NW / 2][ND][64];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1000,6 +1169,13 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
   const int khi = (int)max((int64_t)0, min(held, (int64_t)total - n + (r0 + rows - 1) / G + 1));
   const int klo = a.window > 0
       ? (int)max((int64_t)0, (int64_t)total - n + r0 / G - a.window + 1) : 0;
+  // mixed steps (selected pages: all rows are one token's)
+  int from = khi, low0 = 0;
+  if constexpr (!SEL) {
+    from = (int)max((int64_t)0, min((int64_t)khi, (int64_t)total - n + r0 / G + 1));
+    if (a.window > 0)
+      low0 = (int)max((int64_t)0, (int64_t)total - n + (r0 + rows - 1) / G - a.window + 1);
+  }
   // steps of 32 keys: [st0, st1) in units of 32 keys, or of (list entry, part of its page)
   int st0, st1;
   const int sub_shift = a.s.page_shift - 5;
@@ -1020,6 +1196,8 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
     }
   }
 
+  if (lane == 0) tile = Tile{b, row0, n, total, r0, rows, (int)tok};
+  uint32_t not_finite = 0;                   // not 0: a value of a mixed step
   // this wave's steps, 64 at a time: a lane's page and first key
   const int32_t* list = SEL ? a.sel + (tok * a.heads + head) * a.m : nullptr;
   int ahead = st0 + wave, lphys = -1, lkey = 0;
@@ -1111,14 +1289,7 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
   }
   const auto compute = [&](auto buf) {
     constexpr int B = decltype(buf)::value;
-    if (key[B] + 32 > khi) {
-      // slots past the last key may hold anything: 0 x NaN must not reach the sums
-#pragma unroll
-      for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          vf[B][dt][e] = key[B] + 8 * g + e < khi ? vf[B][dt][e] : (T)0.0f;
-    }
+    if (mixed_step(key[B], from, low0)) not_finite |= put_zeros<T, ND>(vf[B], key[B] + 8 * g, khi);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       f32x4 sc[2];
@@ -1183,6 +1354,8 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
     }
   }
 
+  // arguments once more: kept through the loop, they would cost it registers
+  const AttendArgs ar = args_again();
   // join the waves
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -1193,7 +1366,11 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
       sl[wave][rt * 16 + n16] = sum[rt];
     }
   }
+  const uint64_t any_lane = __ballot(not_finite != 0);
+  if (lane == 0) spoilt[wave] = any_lane != 0;
   __syncthreads();
+  const int tile_rows = __builtin_amdgcn_readfirstlane(tile.rows);
+  bool no_number = false;                  // a result is none, though its row's sum is
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int c = rt * 16 + n16;
@@ -1219,38 +1396,61 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 4 ? 2 : 1) void k_attend_few(At
         for (int dt = 0; dt < ND; ++dt) o[rt][dt] += so[wave][dt][lane];
       __syncthreads();
     }
-    if (wave == 0 && c < rows) {
-      const int rr = r0 + c, ti = rr / G, hh = rr - ti * G;
-      const int64_t orow = (int64_t)(row0 + ti) * a.hq + head * G + hh;
+    if (wave != 0) continue;
+    bool none = false;
+    float zero = 0.0f;                     // NaN where a result is not finite
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) zero = fmaf(o[rt][dt][i], 0.0f, zero);
+    if (zero != 0.0f && z > 0.0f) {
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          none |= o[rt][dt][i] != o[rt][dt][i];
+          o[rt][dt][i] = o[rt][dt][i] != o[rt][dt][i] ? 0.0f : o[rt][dt][i];
+        }
+    }
+    no_number |= __ballot(none && c < tile_rows) != 0;
+    if (c < tile_rows) {
+      const int rr = tile.r0 + c, ti = rr / ar.group, hh = rr - ti * ar.group;
+      const int64_t orow = (int64_t)(tile.row0 + ti) * ar.hq + blockIdx.x % ar.heads * ar.group + hh;
+      const int64_t pr = (int64_t)blockIdx.y * ar.tokens * ar.hq + orow;
       const float inv = z > 0.0f ? 1.0f / z : 0.0f;
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) {
         const f32x4 v = o[rt][dt];
         const int dim = 16 * dt + 4 * g;
-        if (dim >= d) continue;
-        if (a.splits == 1) {
+        if (dim >= ar.d) continue;
+        if (ar.splits == 1) {
           alignas(8) T w[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) w[i] = (T)(z > 0.0f ? v[i] * inv : z);
-          *reinterpret_cast<uint2*>((T*)a.out + orow * d + dim) = *reinterpret_cast<uint2*>(w);
+          *reinterpret_cast<uint2*>((T*)ar.out + orow * ar.d + dim) = *reinterpret_cast<uint2*>(w);
         } else {
-          const int64_t pr = (int64_t)split * a.tokens * a.hq + orow;
-          *reinterpret_cast<f32x4*>(a.part_o + pr * d + dim) = v;
+          *reinterpret_cast<f32x4*>(ar.part_o + pr * ar.d + dim) = v;
         }
       }
       if (g == 0) {
-        if (a.splits == 1) {
-          if (a.lse)
-            a.lse[orow] = z > 0.0f ? (mm - kFewShift<T> + log2_fast(z)) * kLn2
+        if (ar.splits == 1) {
+          if (ar.lse)
+            ar.lse[orow] = z > 0.0f ? (mm - kFewShift<T> + log2_fast(z)) * kLn2
                                    : (z == 0.0f ? -INFINITY : z);
         } else {
-          float* ml = a.part_ml + ((int64_t)split * a.tokens * a.hq + orow) * 2;
+          float* ml = ar.part_ml + pr * 2;
           ml[0] = mm - kFewShift<T>;
           ml[1] = z;
         }
       }
     }
   }
+  if (wave != 0) return;
+  int any = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) any |= spoilt[w];
+  if (no_number || __builtin_amdgcn_readfirstlane(any) != 0)
+    add_not_finite<T, SEL>(tile, 0, tile_rows, no_number);
 }
 
 // Many query rows (NW waves x 32) against a range of keys.  Steps of 64 keys (32 with four waves)
@@ -1298,6 +1498,8 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
   constexpr int R = 32 * NW;
   __shared__ V8 ks[2][HV][32 * CK];
   __shared__ V8 vs[2][HV][KCH];
+  __shared__ int spoilt;                          // a value of a mixed step is not finite
+  __shared__ Tile tile;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c32 = lane & 31, half = lane >> 5;
@@ -1326,6 +1528,9 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
     return;
   }
   const int kend = (int)min(k1, khi64);           // first key that is not this workgroup's
+  const int from = (int)max((int64_t)0, min((int64_t)total - n + r0 / G + 1, (int64_t)kend));
+  const int low0 = a.window > 0      // mixed steps
+      ? (int)max((int64_t)0, (int64_t)total - n + (r0 + rows - 1) / G - a.window + 1) : 0;
 
   // queries, slots of this wave's rows
   V8 qf[NS];
@@ -1362,7 +1567,8 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
 
   // where this thread's chunks of a block's keys and values come from (bytes) and go to
   uint32_t kg[PER], vg[PER];
-  int kl[PER], vl[PER], vkey[PER];
+  int kl[PER], vl[PER];
+  const int vkey = 8 * (tid & 3);              // of a thread's values: NT is a multiple of 4
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const int i = min(tid + NT * j, KCH - 1);
@@ -1373,7 +1579,6 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
     const int dim = i >> 2, cv = i & 3;
     vg[j] = (min(dim, d - 1) * P + 8 * cv) * 2;
     vl[j] = dim * 4 + (cv ^ ((dim >> 2) & 3));
-    vkey[j] = 8 * cv;
   }
   const auto mine = [&](int j) { return KCH % NT == 0 || tid + NT * j < KCH; };
 
@@ -1423,17 +1628,12 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
       for (int j = 0; j < PER; ++j)
         if (mine(j)) ks[slot][hv][kl[j]] = kreg[hv][j];
   };
-  // slots past the last key may hold anything: they become 0, for 0 x NaN must not reach a sum
-  const auto store_v = [&](int slot, const Block* k) {
+  const auto store_v = [&](int slot, const Block* k, int key0) {
 #pragma unroll
     for (int hv = 0; hv < HV; ++hv) {
-      if (k[hv].live < 32) {
-#pragma unroll
-        for (int j = 0; j < PER; ++j)
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            vreg[hv][j][e] = vkey[j] + e < k[hv].live ? vreg[hv][j][e] : (T)0.0f;
-      }
+      const int kb = key0 + 32 * hv;
+      if (k[hv].live < 32 || mixed_step(kb, from, low0))
+        if (put_zeros<T, PER>(vreg[hv], kb + vkey, kb + k[hv].live) != 0) spoilt = 1;
 #pragma unroll
       for (int j = 0; j < PER; ++j)
         if (mine(j)) vs[slot][hv][vl[j]] = vreg[hv][j];
@@ -1465,17 +1665,29 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
     // nothing of the vector part, nor the scalar loads of page numbers, moves between these
     // products: a scalar load in flight turns every wait for an operand into one for all of them
     __builtin_amdgcn_sched_barrier(0);
-    products(cur ^ 1);
+    constexpr int NP = HV * 2 * ND, M = NP + NS * HV;       // products of weights, then of scores
+    const auto operand = [&](int i) {
+      if (i < NP) {
+        const int hv = i / (2 * ND), u = i / ND % 2, dt = i % ND;
+        return vs[cur ^ 1][hv][(32 * dt + c32) * 4 + ((2 * u + half) ^ ((c32 >> 2) & 3))];
+      }
+      const int s = (i - NP) / HV, hv = (i - NP) % HV;
+      return ks[cur][hv][c32 * CK + ((2 * s + half) ^ (c32 & KX))];
+    };
 #pragma unroll
     for (int hv = 0; hv < HV; ++hv) sc[hv] = f32x16(0.0f);
+    // operands are read a few products ahead, in this order also where the compiler keeps to the
+    // source's (short of registers it does: every product then waits for its operand, 8 % of a
+    // chunk's time)
+    V8 op[4];
 #pragma unroll
-    for (int s = 0; s < NS; ++s)
+    for (int i = 0; i < 4; ++i) op[i] = operand(i);
 #pragma unroll
-      for (int hv = 0; hv < HV; ++hv) {
-        const V8 kf = ks[cur][hv][c32 * CK + ((2 * s + half) ^ (c32 & KX))];
-        sc[hv] = mfma32(kf, qf[s], sc[hv]);
-      }
-    // operands are read a few products ahead
+    for (int i = 0; i < M; ++i) {
+      if (i < NP) o[i % ND] = mfma32(op[i & 3], pw[i / (2 * ND)][i / ND % 2], o[i % ND]);
+      else sc[(i - NP) % HV] = mfma32(op[i & 3], qf[(i - NP) / HV], sc[(i - NP) % HV]);
+      if (i + 4 < M) op[i & 3] = operand(i + 4);
+    }
     __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
     for (int i = 0; i < HV * 4 * ND; ++i) {
@@ -1490,7 +1702,7 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
   const auto pass_on = [&](int p, auto parity) {
     constexpr int cur = decltype(parity)::value;
     store_k(cur ^ 1);
-    store_v(cur, b0);
+    store_v(cur, b0, kbeg + p * KEYS);
     load_k(b2);
     load_v(b1);
 #pragma unroll
@@ -1569,6 +1781,11 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
     __builtin_amdgcn_sched_barrier(0);
   };
 
+  if (tid == 0) {
+    spoilt = 0;
+    tile = Tile{b, row0, n, total, r0, rows, 0};
+  }
+  if (steps == 0) __syncthreads();
   if (steps > 0) {
 #pragma unroll
     for (int hv = 0; hv < HV; ++hv) {
@@ -1628,38 +1845,60 @@ __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_atte
   }
 
   const float z = sum + __shfl_xor(sum, 32), top = (coarse ? mx * sc2 : mx) - kTileShift<T>;
+  // arguments and tile once more: kept through the loop, they would cost it registers
+  const AttendArgs ar = args_again();
+  const int tile_rows = __builtin_amdgcn_readfirstlane(tile.rows);
   const int r = wr0 + c32;
-  if (r >= rows) return;
-  const int rr = r0 + r, ti = rr / G, hh = rr - ti * G;
-  const int64_t orow = (int64_t)(row0 + ti) * a.hq + head * G + hh;
-  const int64_t pr = (int64_t)split * a.tokens * a.hq + orow;
-  const float inv = z > 0.0f ? 1.0f / z : 0.0f;
+  bool no_number = false;                  // a result is none, though its row's sum is
+  float zero = 0.0f;                       // NaN where a result is not finite
 #pragma unroll
   for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4) {
-      const int dim = 32 * dt + 8 * i4 + 4 * half;
-      if (dim >= d) continue;
-      if (a.splits == 1) {
-        alignas(8) T w[4];
+    for (int i = 0; i < 16; ++i) zero = fmaf(o[dt][i], 0.0f, zero);
+  if (zero != 0.0f && z > 0.0f) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (T)(z > 0.0f ? o[dt][4 * i4 + i] * inv : z);
-        *reinterpret_cast<uint2*>((T*)a.out + orow * d + dim) = *reinterpret_cast<uint2*>(w);
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        no_number |= o[dt][i] != o[dt][i];
+        o[dt][i] = o[dt][i] != o[dt][i] ? 0.0f : o[dt][i];
+      }
+  }
+  if (r < tile_rows) {
+    const int rr = tile.r0 + r, ti = rr / ar.group, hh = rr - ti * ar.group;
+    const int64_t orow = (int64_t)(tile.row0 + ti) * ar.hq + blockIdx.x % ar.heads * ar.group + hh;
+    const int64_t pr = (int64_t)blockIdx.y * ar.tokens * ar.hq + orow;
+    const float inv = z > 0.0f ? 1.0f / z : 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const int dim = 32 * dt + 8 * i4 + 4 * half;
+        if (dim >= ar.d) continue;
+        if (ar.splits == 1) {
+          alignas(8) T w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = (T)(z > 0.0f ? o[dt][4 * i4 + i] * inv : z);
+          *reinterpret_cast<uint2*>((T*)ar.out + orow * ar.d + dim) = *reinterpret_cast<uint2*>(w);
+        } else {
+          f32x4 v;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = o[dt][4 * i4 + i];
+          *reinterpret_cast<f32x4*>(ar.part_o + pr * ar.d + dim) = v;
+        }
+      }
+    if (half == 0) {
+      if (ar.splits == 1) {
+        if (ar.lse) ar.lse[orow] = z > 0.0f ? (top + log2_fast(z)) * kLn2 : (z == 0.0f ? -INFINITY : z);
       } else {
-        f32x4 v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = o[dt][4 * i4 + i];
-        *reinterpret_cast<f32x4*>(a.part_o + pr * d + dim) = v;
+        ar.part_ml[pr * 2] = top;
+        ar.part_ml[pr * 2 + 1] = z;
       }
     }
-  if (half == 0) {
-    if (a.splits == 1) {
-      if (a.lse) a.lse[orow] = z > 0.0f ? (top + log2_fast(z)) * kLn2 : (z == 0.0f ? -INFINITY : z);
-    } else {
-      a.part_ml[pr * 2] = top;
-      a.part_ml[pr * 2 + 1] = z;
-    }
   }
+  no_number = __ballot(no_number && r < tile_rows) != 0;
+  if (wr0 < tile_rows && (no_number || spoilt != 0))
+    add_not_finite<T, false>(tile, wr0, min(wr0 + 32, tile_rows), no_number);
 }
 
 // Joins the partial results of the key ranges, in their order.  Ranges without a key of the row
@@ -1677,6 +1916,14 @@ __device__ __forceinline__ void store_lse(const AttendArgs& a, int64_t orow, flo
   if (a.lse) a.lse[orow] = z > 0.0f ? (mm + log2_fast(z)) * kLn2 : (z == 0.0f ? -INFINITY : z);
 }
 
+// A range's weight, from its maximum and sum; 0 without a key, and -0 where the weight is too small
+// for fp32: what is not finite there still reaches the row.
+__device__ __forceinline__ float join_weight(float2 v, float mm) {
+  const float f = v.y != 0.0f ? exp2_fast(v.x - mm) : 0.0f;   // mm is finite where one is not 0
+  return f == 0.0f && v.y != 0.0f ? -0.0f : f;
+}
+__device__ __forceinline__ bool has_keys(float w) { return __float_as_uint(w) != 0; }
+
 // up to 16 ranges: a wave a row, 4 dimensions a lane
 template <typename T>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
@@ -1690,7 +1937,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) mm = fmaxf(mm, __shfl_xor(mm, o));
   mm = __shfl(mm, 0);
-  const float f = v.y != 0.0f ? exp2_fast(v.x - mm) : 0.0f;   // mm is finite where one is not 0
+  const float f = join_weight(v, mm);
   float z = f * v.y;
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) z += __shfl_xor(z, o);
@@ -1704,7 +1951,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
     for (int j = 0; j < 8; ++j) {
       w[j] = c0 + j < a.splits ? __shfl(f, c0 + j) : 0.0f;
       o[j] = f32x4{0, 0, 0, 0};
-      if (w[j] != 0.0f) o[j] = *reinterpret_cast<const f32x4*>(po + (c0 + j) * nrows * a.d);
+      if (has_keys(w[j])) o[j] = *reinterpret_cast<const f32x4*>(po + (c0 + j) * nrows * a.d);
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc += w[j] * o[j];
@@ -1729,7 +1976,7 @@ __global__ __launch_bounds__(256) void k_attend_join_many(AttendArgs a) {
   if (lane == 0) red[wave][0] = mm;
   __syncthreads();
   mm = fmaxf(fmaxf(red[0][0], red[1][0]), fmaxf(red[2][0], red[3][0]));
-  const float f = v.y != 0.0f ? exp2_fast(v.x - mm) : 0.0f;
+  const float f = join_weight(v, mm);
   if (tid < kMaxSplits) w[tid] = f;
   float z = f * v.y;
 #pragma unroll
@@ -1749,7 +1996,7 @@ __global__ __launch_bounds__(256) void k_attend_join_many(AttendArgs a) {
       const int c = c0 + j * groups;
       f8[j] = c < a.splits ? w[c] : 0.0f;
       o[j] = f32x4{0, 0, 0, 0};
-      if (f8[j] != 0.0f) o[j] = *reinterpret_cast<const f32x4*>(po + c * nrows * a.d);
+      if (has_keys(f8[j])) o[j] = *reinterpret_cast<const f32x4*>(po + c * nrows * a.d);
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc += f8[j] * o[j];
