@@ -10,7 +10,8 @@ namespace kv {
 constexpr int kCUs = 256;
 // partial results of a row at most: 1024 keys each at 131,072 keys
 constexpr int kMaxSplits = 128;
-// a launch has fewer than 2^32 threads
+// a launch has fewer than 2^32 threads: so many workgroups of 256
+constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 1;
 constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 1;
 
 constexpr int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -44,9 +45,10 @@ inline int few_rows(int64_t rows, int d) { return rows <= 16 ? 1 : rows <= 32 ||
 
 // One workgroup of eight waves takes all keys of a row tile where these are few or there are
 // tiles for half of the CUs: nothing to join, one launch less.  (2048 keys, whole and split with
-// its join: 256 tiles 45 us, 48; 32 tiles 35 us, 18; 8 tiles of 1000 keys 21 us, 13.)
+// its join: 256 tiles 45 us, 48; 32 tiles 35 us, 18; 8 tiles of 1000 keys 21 us, 13.)  From 2^23
+// tiles on a launch holds no eight waves for each.
 inline bool whole_rows(int64_t keys, int64_t tiles, int rt, int d) {
-  return rt == 1 && d <= 128 && keys <= (tiles >= kCUs / 2 ? 2048 : 512);
+  return rt == 1 && d <= 128 && tiles * 512 <= kMaxThreads && keys <= (tiles >= kCUs / 2 ? 2048 : 512);
 }
 
 inline Plan plan_dense(int heads, int page, int d, int64_t tokens, int32_t batch, int group,
@@ -101,6 +103,10 @@ inline Plan plan_sel(int heads, int page, int d, int64_t tokens, int group, int3
   p.chunk = (int)chunk;
   p.splits = (int)cdiv(m, chunk);
   return p;
+}
+
+inline int64_t plan_threads(const Plan& p, int heads) {
+  return p.items * heads * p.splits * (p.rt > 0 ? 64 * p.waves : 2 * p.rows);
 }
 
 inline int64_t part_bytes(int64_t tokens, int hq, int d, int splits) {

@@ -2373,8 +2373,7 @@ int gmm_kv_attend(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
   a.tiles_token = p.tiles_token;
   a.part_o = (float*)ws;
   a.part_ml = a.part_o + (int64_t)p.splits * tokens * hq * a.d;
-  if (p.items * a.heads * p.splits > kMaxBlocks || p.splits > 65535 ||
-      tokens * hq > kMaxBlocks)
+  if (plan_threads(p, a.heads) > kMaxThreads || p.splits > 65535 || tokens * hq > kMaxBlocks)
     return GMM_ERR_UNSUPPORTED;
   if (cache->dtype == GMM_BF16) launch_attend<__bf16>(a, p, stream);
   else launch_attend<_Float16>(a, p, stream);

@@ -2,6 +2,7 @@
 // the first size that breaks the rule and returns 1, or returns 0.
 //   covers   what a call's plan writes fits into the workspace of its sizes
 //   grows    a workspace for larger sizes serves smaller ones
+//   launches the largest calls of up to 2^24 rows fit into a launch of fewer than 2^32 threads
 #include <stdio.h>
 #include <string.h>
 
@@ -96,8 +97,30 @@ static int grows() {
   return 0;
 }
 
+static int launches() {
+  for (int heads : {1, 2, 3})
+    for (int group : {1, 2, 3})
+      for (int d : kDims)
+        for (int page : kPages)
+          for (long tokens = 1 << 20; tokens * heads * group < 1 << 24; tokens += tokens / 3 + 1)
+            for (int n : {1, 2, 5, 16, 60}) {
+              const Plan plans[] = {plan_sel(heads, page, d, tokens, group, n),
+                                    plan_dense(heads, page, d, tokens, 1 << 20, group, n)};
+              for (const Plan& p : plans) {
+                const int threads = p.rt > 0 ? 64 * p.waves : 2 * p.rows;
+                if (p.items * heads * p.splits >= 1 << 24) continue;       // refused in any case
+                if (p.items * heads * p.splits * threads >= 1LL << 32)
+                  return printf("heads %d group %d d %d page %d tokens %ld pages %d: %lld workgroups of %d\n",
+                                heads, group, d, page, tokens, n,
+                                (long long)(p.items * heads * p.splits), threads), 1;
+              }
+            }
+  return 0;
+}
+
 int main(int argc, char** argv) {
   if (argc == 2 && !strcmp(argv[1], "covers")) return covers();
   if (argc == 2 && !strcmp(argv[1], "grows")) return grows();
+  if (argc == 2 && !strcmp(argv[1], "launches")) return launches();
   return 2;
 }

@@ -33,6 +33,10 @@ def test_a_workspace_for_larger_sizes_serves_smaller_ones(check):
     check("grows")
 
 
+def test_the_largest_calls_fit_into_a_launch(check):
+    check("launches")
+
+
 def test_the_workspace_of_no_tokens(check):
     """A server's empty step: a size, and not a division by its zero tiles."""
     cache = _CCache(1 << 20, 1 << 20, None, None, 10, 2, 64, 128, 1)
