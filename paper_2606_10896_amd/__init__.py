@@ -151,6 +151,16 @@ def _dev(t, dtype, name, numel=None):
     return t
 
 
+def _ws(ws):
+    """(address, bytes) of a workspace; None: no workspace, which the library refuses."""
+    import torch
+    if ws is None:
+        return 0, 0
+    if not (isinstance(ws, torch.Tensor) and ws.is_cuda and ws.is_contiguous()):
+        raise TypeError("ws must be a contiguous CUDA tensor")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def workspace(n: int, d: int, k: int, m: int = 0, device="cuda"):
     """A workspace tensor (uint8, 256-byte aligned by the caching allocator)."""
     import torch
@@ -174,7 +184,7 @@ def gmm_estep_accumulate(x, weights, means, variances, nk, s, q, loglik, ws, str
         _ptr(_dev(variances, torch.float32, "vars", k * d)),
         _ptr(_dev(nk, torch.float64, "nk", k)), _ptr(_dev(s, torch.float64, "s", k * d)),
         _ptr(_dev(q, torch.float64, "q", k * d)), _ptr(_dev(loglik, torch.float64, "loglik", 1)),
-        _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream))
+        *_ws(ws), _stream(stream))
     _check(_fn, rc)
 
 
@@ -211,8 +221,7 @@ def gmm_fit(x, weights, means, variances, n_iters, loglik_hist, ws, var_floor=1e
         _ptr(_dev(weights, torch.float32, "weights", k)),
         _ptr(_dev(means, torch.float32, "means", k * d)),
         _ptr(_dev(variances, torch.float32, "vars", k * d)),
-        _ptr(_dev(loglik_hist, torch.float64, "loglik_hist", n_iters)), _ptr(ws),
-        ws.numel() if ws is not None else 0, _stream(stream))
+        _ptr(_dev(loglik_hist, torch.float64, "loglik_hist", n_iters)), *_ws(ws), _stream(stream))
     _check(_fn, rc)
 
 
@@ -234,8 +243,7 @@ def gmm_assign_topk(x, weights, means, variances, m, tau, idx, resp, ws, stream=
         _ptr(_dev(means, torch.float32, "means", k * d)),
         _ptr(_dev(variances, torch.float32, "vars", k * d)),
         int(m), float(tau), _ptr(_dev(idx, torch.int32, "idx", n * m)),
-        _ptr(_dev(resp, torch.float32, "resp", n * m)), _ptr(ws),
-        ws.numel() if ws is not None else 0, _stream(stream))
+        _ptr(_dev(resp, torch.float32, "resp", n * m)), *_ws(ws), _stream(stream))
     _check("gmm_assign_topk", rc)
 
 
@@ -252,8 +260,7 @@ def gmm_kmeans(x, weights, means, variances, n_iters, assign, ws, var_floor=1e-6
         _ptr(_dev(weights, torch.float32, "weights", k)),
         _ptr(_dev(means, torch.float32, "means", k * d)),
         _ptr(_dev(variances, torch.float32, "vars", k * d)),
-        _ptr(_dev(assign, torch.int32, "assign", n)), _ptr(ws),
-        ws.numel() if ws is not None else 0, _stream(stream))
+        _ptr(_dev(assign, torch.int32, "assign", n)), *_ws(ws), _stream(stream))
     _check("gmm_kmeans", rc)
 
 
@@ -271,7 +278,7 @@ def gmm_kmeanspp(x, u, idx, centers, ws=None, stream=None):
     rc = load_library().gmm_kmeanspp(
         _ptr(x), n, d, k, _ptr(_dev(u, torch.float64, "u", k)),
         _ptr(_dev(idx, torch.int64, "idx", k)), _ptr(_dev(centers, torch.float32, "centers", k * d)),
-        _ptr(ws), ws.numel(), _stream(stream))
+        *_ws(ws), _stream(stream))
     _check("gmm_kmeanspp", rc)
 
 
@@ -295,8 +302,8 @@ def gmm_estep_accumulate_streamed(x_host, weights, means, variances, nk, s, q, l
         _ptr(_dev(variances, torch.float32, "vars", k * d)),
         _ptr(_dev(nk, torch.float64, "nk", k)), _ptr(_dev(s, torch.float64, "s", k * d)),
         _ptr(_dev(q, torch.float64, "q", k * d)), _ptr(_dev(loglik, torch.float64, "loglik", 1)),
-        int(chunk_rows), _ptr(_dev(staging, torch.float32, "staging", 2 * rows * d)), _ptr(ws),
-        ws.numel() if ws is not None else 0, _stream(stream), _stream(copy_stream))
+        int(chunk_rows), _ptr(_dev(staging, torch.float32, "staging", 2 * rows * d)), *_ws(ws),
+        _stream(stream), _stream(copy_stream))
     _check("gmm_estep_accumulate_streamed", rc)
 
 
@@ -355,8 +362,8 @@ def gmm_estep_accumulate_ring(source, n, weights, means, variances, nk, s, q, lo
         _ptr(_dev(nk, torch.float64, "nk", k)), _ptr(_dev(s, torch.float64, "s", k * d)),
         _ptr(_dev(q, torch.float64, "q", k * d)), _ptr(_dev(loglik, torch.float64, "loglik", 1)),
         int(chunk_rows), ctypes.c_void_p(ring.data_ptr()), slots,
-        _ptr(_dev(staging, torch.float32, "staging", 2 * rows * d)), _ptr(ws),
-        ws.numel() if ws is not None else 0, _stream(stream), _stream(copy_stream))
+        _ptr(_dev(staging, torch.float32, "staging", 2 * rows * d)), *_ws(ws),
+        _stream(stream), _stream(copy_stream))
     if failure:
         raise failure[0]
     _check("gmm_estep_accumulate_ring", rc)
@@ -375,7 +382,7 @@ def gmm_estep_accumulate_iso(x, weights, means, variances, nk, s, q, loglik, ws,
         _ptr(_dev(variances, torch.float32, "vars", k)),
         _ptr(_dev(nk, torch.float64, "nk", k)), _ptr(_dev(s, torch.float64, "s", k * d)),
         _ptr(_dev(q, torch.float64, "q", k)), _ptr(_dev(loglik, torch.float64, "loglik", 1)),
-        _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream))
+        *_ws(ws), _stream(stream))
     _check("gmm_estep_accumulate_iso", rc)
 
 
@@ -404,8 +411,7 @@ def gmm_fit_iso(x, weights, means, variances, n_iters, loglik_hist, ws, var_floo
         _ptr(_dev(weights, torch.float32, "weights", k)),
         _ptr(_dev(means, torch.float32, "means", k * d)),
         _ptr(_dev(variances, torch.float32, "vars", k)),
-        _ptr(_dev(loglik_hist, torch.float64, "loglik_hist", n_iters)), _ptr(ws),
-        ws.numel() if ws is not None else 0, _stream(stream))
+        _ptr(_dev(loglik_hist, torch.float64, "loglik_hist", n_iters)), *_ws(ws), _stream(stream))
     _check("gmm_fit_iso", rc)
 
 

@@ -89,10 +89,6 @@ def _flat(t, dtype, numel, name):
     return t.data_ptr()
 
 
-def _ws(ws):
-    return (0, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
-
-
 class KVCache:
     """Pages of keys and values: k [pages, heads, page, d], v [pages, heads, d, page] (a page's
     values transposed), bfloat16 or float16; box [pages, heads, 2, d] int8 and box_scale
@@ -255,7 +251,7 @@ def gmm_kv_select(cache, q, cu, total, pages, idx, ws, keep_first=1, keep_last=1
         raise ValueError(f"idx must be [{tokens}, {cache.heads}, m]")
     rc = _base.load_library().gmm_kv_select(
         cache._ref, _batch(cu, total, pages), tokens, *_rows(q, cache.k.dtype, tokens, hq, cache.d, "q"),
-        hq, idx.shape[2], keep_first, keep_last, _flat(idx, torch.int32, 0, "idx"), *_ws(ws),
+        hq, idx.shape[2], keep_first, keep_last, _flat(idx, torch.int32, 0, "idx"), *_base._ws(ws),
         _stream(stream, q))
     if rc:
         raise _base.GMMError("gmm_kv_select", rc)
@@ -277,7 +273,7 @@ def gmm_kv_attend(cache, q, cu, total, pages, out, ws, lse=None, scale=None, win
         cache._ref, _batch(cu, total, pages), tokens, *_rows(q, dt, tokens, hq, d, "q"), hq,
         1.0 / math.sqrt(d) if scale is None else scale, window, sp, m,
         _flat(out, dt, tokens * hq * d, "out"),
-        0 if lse is None else _flat(lse, torch.float32, tokens * hq, "lse"), *_ws(ws),
+        0 if lse is None else _flat(lse, torch.float32, tokens * hq, "lse"), *_base._ws(ws),
         _stream(stream, q))
     if rc:
         raise _base.GMMError("gmm_kv_attend", rc)
