@@ -59,14 +59,13 @@ inline Plan plan_dense(int heads, int page, int d, int64_t tokens, int32_t batch
   int64_t want, unit;
   if (rows > 64) {
     // eight waves share a step's operands from 65 to 128 dimensions (2048 tokens on 34,816 keys:
-    // 0.97 ms, 1.12 in workgroups of four waves; 512 on 8512: 90 us, 132), but not for prompts
+    // 0.98 ms, 1.11 in workgroups of four waves; 512 on 8512: 93 us, 136), but not for prompts
     // that are most of their own context, whose few steps a tile of 128 rows ends earlier at the
-    // diagonal (32 heads on 8, eight waves and four: 2 prompts of 700 tokens 48 us, 30; 4: 54, 44;
-    // 16: 153, 132; one of 2000 91, 85; but 4 of 500 31, 33, and 8 of 2000 372, between 367 and
-    // 388).  Up to 64 the vector part
-    // takes longer than the matrix part, and three workgroups of four waves a CU hide more of it
-    // (prompts of 4000 tokens with a window, when it was chosen: 0.21 ms, 0.23); above 128 there
-    // are registers for four waves
+    // diagonal (32 heads on 8, eight waves and four: 2 prompts of 700 tokens 52 us, 32; 4: 57, 47;
+    // 16: 181, 151; one of 2000 97, 90; 8 of 2000 415, 395; but 4 of 500 33, 35).  Up to 64 the
+    // vector part takes longer than the matrix part, and three workgroups of four waves a CU hide
+    // more of it (prompts of 4000 tokens with a window, when it was chosen: 0.21 ms, 0.23); above
+    // 128 there are registers for four waves
     const bool prompt = keys <= 2048 && keys * batch <= 2 * tokens;
     p.rows = rows > 128 && d > 64 && d <= 128 && !prompt ? 256 : 128;
     const int64_t tiles = tokens * group / p.rows;

@@ -279,7 +279,7 @@ __global__ __launch_bounds__(256) void k_rope_table(const double* __restrict__ f
 
 // A unit a thread: 16 elements (W = 8: 16-byte accesses) where rot, d, the strides and the
 // addresses allow it, else one pair.  An odd count of dimensions past rot ends in a unit of its
-// own (W = 1).  Bound by the bytes: 8192 x 32 x 128 bf16, half rotated, 28.6 us a call, 4.8 TB/s
+// own (W = 1).  Bound by the bytes: 8192 x 32 x 128 bf16, half rotated, 28.5 us a call, 4.8 TB/s
 // (a 2 GiB copy: 5.0); a single token's 40 heads take 2 us.
 template <typename T, int W, bool INTER>
 __global__ __launch_bounds__(256) void k_rope(const T* x, int64_t xt, int64_t xh, T* out,
@@ -332,7 +332,7 @@ struct AppendArgs {
 // Small pages share a workgroup, 128 or 64 threads a head.  The queries' rotation rides along in
 // workgroups of its own: one launch for the step.  Bound by the bytes for prompts (7498 tokens, 16
 // heads of 64: 28 us, about 130 MB), for single tokens by the chain sequence, page, keys, barrier
-// (64 sequences, 8 heads of 128: 9.6 us).
+// (64 sequences, 8 heads of 128: 9.4 us).
 template <typename T, int W, bool INTER>
 __global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
   typedef typename Vec8<T>::type V8;
@@ -535,8 +535,8 @@ __device__ __forceinline__ float score_of(float query_unit, float page_unit, int
 // negative parts) through LDS.  A wave takes 64 pages: their numbers are one load, their boxes
 // (8 KB at a time at d = 128) are in flight while the queries are rounded to 8 bits.  S: 64-byte
 // steps of a box.  Bound by the boxes' bytes, 2 d + 4 a (page, head), and the loads before them:
-// 32 sequences of up to 2049 pages, 8 heads of 128, 18.8 us, 2.6 TB/s; a few sequences of a few
-// hundred pages 7.4 us.
+// 32 sequences of up to 2049 pages, 8 heads of 128, 19.4 us, 2.5 TB/s; a few sequences of a few
+// hundred pages 7.7 us.
 template <typename T, int S>
 __global__ __launch_bounds__(256, S <= 4 ? 4 : 2) void k_select_score(SelectArgs a) {
   typedef typename Vec8<T>::type V8;
@@ -715,11 +715,12 @@ __device__ __forceinline__ uint32_t score_key(float v) {
   return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-// The m best pages of a row, one workgroup a row, PT pages a thread in registers.  The m-th
+// The m best pages of a row, one workgroup a row, PT pages a thread in registers (of 64, which
+// tables of more than 16,384 pages need, a part is spilled: 1024 threads have 128 each).  The m-th
 // largest key is bracketed by counting the keys at or above three values between the bounds
 // (ballots, no atomics) until a count is m or the bounds meet; then the pages above it and the
 // lowest ones equal to it are written in page order.  Bound by the rounds' latency: about ten,
-// a barrier each: 7.4 us at up to 2049 pages, m = 32, 6.1 at a few hundred.
+// a barrier each: 7.6 us at up to 2049 pages, m = 32, 6.4 at a few hundred.
 template <int NT, int PT>
 __global__ __launch_bounds__(NT) void k_select_top(Seqs s, const float* __restrict__ score,
                                                    int64_t row, int heads, int m, int keep_first,
@@ -1127,9 +1128,9 @@ __device__ void add_not_finite(const Tile& tile, int ra, int rb, bool whole) {
 // page numbers of 64 steps are one load, a lane a step; while a step is computed the next one's
 // operands are in flight (16 KB at d = 128) where registers allow it.  Bound by the cache's bytes,
 // for short contexts by the chain of loads: sequence, page numbers, keys.  64 sequences of up to
-// 32,768 keys, 32 heads on 8 of 128: 647 us, 5.4 TB/s; one token on 1000 keys 7.8 us.  The rest of
-// the weights' rounding as a second product takes 3 % of the former (633 us without) and brings
-// the error from 1.3 times the result's rounding to that rounding.
+// 32,768 keys, 32 heads on 8 of 128: 634 us a call, 5.5 TB/s; one token on 1000 keys 8.2 us.  The
+// rest of the weights' rounding as a second product costs nothing (634 us without) and brings the
+// error from 1.3 times the result's rounding to that rounding.
 template <typename T, int NS, int RT, bool SEL, int NW>
 __global__ __launch_bounds__(64 * NW, NS * RT <= 6 ? 2 : 1) void k_attend_few(AttendArgs a) {
   typedef typename Vec8<T>::type V8;
@@ -1480,9 +1481,9 @@ __global__ __launch_bounds__(64 * NW, NS * RT <= 6 ? 2 : 1) void k_attend_few(At
 // Rows of the score tile are keys in the order that makes its accumulator the B operand of the
 // second product: row r is key r with bits 2 and 3 exchanged.
 //
-// 2048 tokens on 34,816 keys, 32 heads on 8 of 128: 974 us a call, 1164 TFLOP/s (a product of 8192^3
-// 1274): matrix unit busy 59 % of the cycles, vector unit 44, LDS 37.  Up to 64 dimensions the
-// vector unit bounds it (51 %, matrix unit 30): prompts with a window, 168 us.
+// 2048 tokens on 34,816 keys, 32 heads on 8 of 128: 997 us a call, 1137 TFLOP/s (a product of 8192^3
+// 1274): matrix unit busy 56 % of the cycles, vector unit 42, LDS 35.  Up to 64 dimensions the
+// vector unit bounds it (51 %, matrix unit 28): prompts with a window, 178 us.
 template <typename T, int ND, int NW>
 __global__ __launch_bounds__(64 * NW, ND <= 2 ? 3 : ND <= 4 ? 2 : 1) void k_attend_tile(AttendArgs a) {
   typedef typename Vec8<T>::type V8;
