@@ -396,8 +396,9 @@ int gmm_timing_read(double* ms, int32_t n_phases, int64_t* calls);
  * Types: keys, values, queries and results are GMM_BF16 or GMM_F16 (gmm_rope:
  * GMM_F32 too).  Head widths: d a multiple of 16, 16 <= d <= 256; pages of 32,
  * 64, 128 or 256 keys (a 32-key matrix step lies in one page).  Query heads
- * are a multiple of the cache's heads, at most GMM_KV_MAX_GROUP times as many; query head j reads cache head
- * j / (hq / heads).
+ * are a multiple of the cache's heads, at most GMM_KV_MAX_GROUP times as many;
+ * query head j reads cache head j / (hq / heads).  k, v and box of a cache are
+ * aligned to 16 bytes, out of gmm_kv_attend to 8, workspaces to 256.
  * ---------------------------------------------------------------------- */
 
 typedef enum { GMM_F32 = 0, GMM_BF16 = 1, GMM_F16 = 2 } gmm_dtype;
