@@ -549,6 +549,135 @@ int gmm_kv_attend(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
                   float scale, int32_t window, const int32_t* sel, int32_t m, void* out,
                   float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * The cache's pages as a pool, and beam search over it.
+ *
+ * Counts: ref [cache pages] int32 (device, zero at first) says how many table
+ * entries name a page, over every table that the caller keeps; 0 is a free
+ * page.  Tables are those of gmm_kv_batch: row b holds total[b] keys, and its
+ * first ceil(total[b] / page) entries (no more than max_pages) name pages.
+ * Entries out of range are never counted, read or written through.  The calls
+ * below keep counts and tables consistent; all of it happens on the GPU, so a
+ * decoding step runs without a wait of the host and can be captured:
+ *   gmm_beam_select -> gmm_kv_fork -> gmm_kv_grow -> gmm_kv_append ->
+ *   gmm_kv_attend -> logits -> gmm_beam_select
+ * Calls that change one pool (its counts, tables or pages) must be ordered on
+ * one stream.  At most GMM_KV_MAX_ROWS rows in a call.
+ * ---------------------------------------------------------------------- */
+
+#define GMM_KV_MAX_ROWS 65536
+#define GMM_BEAM_MAX 64
+#define GMM_BEAM_MAX_VOCAB (1 << 24)
+
+/*
+ * Copies pages: keys, values and boxes of page src_pages[i] of src into page
+ * dst_pages[i] of dst, i < n <= 2^30.  The caches (which may be one) have the
+ * same heads, page, d, dtype, and both or neither have boxes; their sizes may
+ * differ.  A pair with a number out of range is skipped.  A page that is the
+ * destination of two pairs, or in one cache the source of one pair and the
+ * destination of another, holds parts of either afterwards.
+ */
+int gmm_kv_copy(const gmm_kv_cache* src, const gmm_kv_cache* dst, const int32_t* src_pages,
+                const int32_t* dst_pages, int64_t n, hipStream_t stream);
+
+/*
+ * Forks rows of a table: new row i holds the first
+ *   total_out[i] = min(total[p], keep[i]),  p = parent[i]  (keep null: total[p])
+ * keys of old row p: the same pages, whose counts grow by one, and -1 behind
+ * them.  A parent outside [0, batch) gives an empty row.  With `release` the
+ * old rows are given up: their entries no longer count, and a page whose count
+ * reaches 0 is free.  So beams take their parents' tables (parent from
+ * gmm_beam_select), drafted tokens are rolled back (keep), a prompt's pages
+ * serve several sequences (release 0), and sequences that end are freed
+ * (release, without a child; rows may be 0).
+ *   total [batch], pages [batch, max_pages] rows pages_stride apart (read)
+ *   parent, keep [rows]; total_out [rows], pages_out [rows, out_max_pages],
+ *   rows out_stride apart, out_max_pages >= max_pages: written whole; they must
+ *   not overlap the old ones (refused)
+ */
+int gmm_kv_fork(const gmm_kv_cache* cache, int32_t* ref, const int32_t* total,
+                const int32_t* pages, int32_t batch, int32_t max_pages, int64_t pages_stride,
+                const int32_t* parent, const int32_t* keep, int32_t rows, int32_t release,
+                int32_t* total_out, int32_t* pages_out, int32_t out_max_pages,
+                int64_t out_stride, hipStream_t stream);
+
+/* Workspace of gmm_kv_grow and gmm_kv_compact for tables of up to `batch`
+ * rows; 0 when the shape is unsupported. */
+size_t gmm_kv_pool_workspace_bytes(const gmm_kv_cache* cache, int32_t batch);
+
+/*
+ * Gives the rows pages for growing from held[b] to total[b] keys, to be called
+ * before gmm_kv_append with that total: entries ceil(held / page) to
+ * ceil(total / page) - 1 (below max_pages) get free pages, with count 1.  A row
+ * whose new keys begin in a page that other entries name too (a fork's partly
+ * filled last page) gets a copy of it instead, keys, values and box; the first
+ * of the rows of this call that write into a page keeps it if no other entry
+ * names it.  Free pages are given out from the lowest number on, row after
+ * row, a row's copy before its further pages.  Rows with total[b] <= held[b]
+ * stay as they are.
+ * All or nothing: if the rows need more pages than are free, nothing changes,
+ * and short_by (one int32, device) says how many are missing; 0 otherwise.  The
+ * caller looks at it before appending, or knows from its own count of keys
+ * that the pool suffices.
+ */
+int gmm_kv_grow(const gmm_kv_cache* cache, int32_t* ref, const int32_t* held,
+                const int32_t* total, int32_t* pages, int32_t batch, int32_t max_pages,
+                int64_t pages_stride, int32_t* short_by, void* ws, size_t ws_bytes,
+                hipStream_t stream);
+
+/*
+ * Pushes a pool together: with U pages in use, the used pages U and above move,
+ * in order, to the free ones below U, with their counts; afterwards pages 0 to
+ * U - 1 are in use and all others free.  The tables' entries follow.  where
+ * [cache pages] says for every page where its contents are now (itself if it
+ * did not move, -1 if it was free), for tables that are not in this call; used
+ * (one int32, device) is U.  Every entry that counts must be in `pages` or be
+ * rewritten by the caller.
+ */
+int gmm_kv_compact(const gmm_kv_cache* cache, int32_t* ref, const int32_t* total, int32_t* pages,
+                   int32_t batch, int32_t max_pages, int64_t pages_stride, int32_t* where,
+                   int32_t* used, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Workspace of gmm_beam_select (any m, any dtype); 0 when unsupported. */
+size_t gmm_beam_workspace_bytes(int32_t batch, int32_t beams, int32_t vocab);
+
+/*
+ * Beam search's selection: for every sequence the m best continuations of its
+ * beams.  Beam j of sequence b is row b beams + j.  Word v after a live beam
+ * has the score
+ *   l = score[row] + (scale x_v - log sum_u exp(scale x_u))
+ * over the words u that the mask allows; a finished beam has one continuation,
+ * itself: word eos with l = score[row].  The m largest weight[row] l are
+ * returned in descending order, compared in fp64, ties to the lower beam, then
+ * the lower word; the log-sum-exp has the precision of fp32, of the same value
+ * for beams of the same logits.
+ *   logits x: beam j of sequence b begins at b seq_stride + j beam_stride
+ *   (elements), its vocab words contiguous; GMM_F32, GMM_BF16 or GMM_F16, aligned to
+ *   an element
+ *   score [batch, beams] fp32: a beam whose score is not finite has no
+ *   continuation (-infinity: a place without a beam, as in the first step)
+ *   weight [batch, beams] fp32 or null (1): e.g. a length's normalisation; a
+ *   beam whose weight is not positive and finite has no continuation
+ *   done [batch, beams] bytes or null: beams that are finished (not 0)
+ *   mask [batch beams] rows, mask_stride (>= ceil(vocab / 32)) words apart, or
+ *   null: word v is allowed if bit v % 32 of word v / 32 is set
+ *   out_score [batch, m] fp32 l, out_parent [batch, m] row, out_token
+ *   [batch, m]; -infinity, -1 and -1 where there are fewer continuations
+ *   out_done [batch, m] bytes (null: not written; needed with done): the
+ *   continuation is finished, by its beam or by the word eos
+ * A word of logit -infinity is no continuation.  A beam with a NaN or +infinity
+ * among its allowed logits has none; logits of forbidden words, of finished
+ * beams and of beams without a score do not matter.
+ * 1 <= m, beams <= GMM_BEAM_MAX, vocab <= GMM_BEAM_MAX_VOCAB, 1e-6 <= scale <= 1e6,
+ * eos < vocab (negative: no end word; not with done).
+ */
+int gmm_beam_select(const void* logits, int32_t dtype, int64_t seq_stride, int64_t beam_stride,
+                    int32_t batch, int32_t beams, int32_t vocab, const float* score,
+                    const float* weight, const uint8_t* done, int32_t eos, const int32_t* mask,
+                    int64_t mask_stride, double scale, int32_t m, float* out_score,
+                    int32_t* out_parent, int32_t* out_token, uint8_t* out_done, void* ws,
+                    size_t ws_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

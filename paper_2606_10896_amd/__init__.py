@@ -1,9 +1,8 @@
 """Python binding of ``libflashgmm.so``: the fused diagonal-GMM EM iteration on MI355X.
 
 Argument marshalling only: every step of the computation runs in the HIP
-kernels of ``csrc/flashgmm.hip`` and ``csrc/kvcache.hip``.  PyTorch provides the device memory (CUDA
-tensors on ROCm) and the stream (``torch.cuda.current_stream()``); the entry
-points take the same names and arguments as the C ABI in
+kernels of ``csrc/*.hip``.  PyTorch provides the device memory (CUDA tensors on
+ROCm) and the stream (``torch.cuda.current_stream()``); the entry points take the same names and arguments as the C ABI in
 ``include/flashgmm.h``.  There is no CPU fallback: without the built library
 every call raises.
 """
@@ -35,7 +34,9 @@ EXPORTS = ("gmm_status_string", "gmm_workspace_bytes", "gmm_estep_accumulate", "
            "gmm_set_stats_chunk_limit", "gmm_estep_accumulate_static",
            "gmm_estep_accumulate_ring", "gmm_fill_pageable",
            "gmm_rope_table", "gmm_rope", "gmm_kv_append", "gmm_kv_workspace_bytes",
-           "gmm_kv_select", "gmm_kv_attend")
+           "gmm_kv_select", "gmm_kv_attend", "gmm_kv_copy", "gmm_kv_fork",
+           "gmm_kv_pool_workspace_bytes", "gmm_kv_grow", "gmm_kv_compact",
+           "gmm_beam_workspace_bytes", "gmm_beam_select")
 
 _lib = None
 
@@ -110,6 +111,7 @@ def load_library():
     lib.gmm_set_stats_chunk_limit.argtypes = [i32]
     lib.gmm_set_stats_chunk_limit.restype = ctypes.c_int
     kv.bind(lib)
+    pool.bind(lib)
     _lib = lib
     return lib
 
@@ -461,3 +463,7 @@ def gmm_estep_accumulate_static(x, weights, means, variances, nk, s, q, loglik, 
 from . import kv  # noqa: E402
 from .kv import (KVCache, gmm_kv_append, gmm_kv_attend, gmm_kv_select, gmm_rope,  # noqa: E402,F401
                  gmm_rope_table, kv_cache, kv_workspace, kv_workspace_bytes, rope_frequencies)
+from . import pool  # noqa: E402
+from .pool import (beam_workspace, beam_workspace_bytes, gmm_beam_select,  # noqa: E402,F401
+                   gmm_kv_compact, gmm_kv_copy, gmm_kv_fork, gmm_kv_grow, kv_pool,
+                   kv_pool_workspace, kv_pool_workspace_bytes)

@@ -9,7 +9,8 @@ from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = [os.path.join(HERE, "csrc", name) for name in ("flashgmm.hip", "kvcache.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("flashgmm.hip", "kvcache.hip", "kvpool.hip",
+                                                        "beam.hip")]
 LIB = os.path.join(HERE, "libflashgmm.so")
 INCLUDE = os.path.join(ROOT, "include")
 

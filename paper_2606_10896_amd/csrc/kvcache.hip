@@ -27,6 +27,7 @@
 #include <type_traits>
 
 #include "flashgmm.h"
+#include "kv_host.h"
 #include "kv_plan.h"
 
 namespace {
@@ -2011,31 +2012,6 @@ __global__ __launch_bounds__(256) void k_attend_join_many(AttendArgs a) {
 }
 
 // ---------------------------------------------------------------- host
-int launch_status() {
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? GMM_OK : GMM_ERR_DEVICE;
-}
-
-inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-inline bool is_pow2(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }
-inline int log2i(int v) {
-  int s = 0;
-  while ((1 << s) < v) ++s;
-  return s;
-}
-
-int check_cache(const gmm_kv_cache* c) {
-  if (!c || !c->k || !c->v) return GMM_ERR_INVALID_ARG;
-  if (c->pages < 1 || c->heads < 1 || c->page < 1 || c->d < 1) return GMM_ERR_INVALID_ARG;
-  if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->box)) return GMM_ERR_INVALID_ARG;
-  if ((c->box == nullptr) != (c->box_scale == nullptr)) return GMM_ERR_INVALID_ARG;
-  if (c->dtype != GMM_BF16 && c->dtype != GMM_F16) return GMM_ERR_UNSUPPORTED;
-  if (c->d % 16 || c->d > GMM_KV_MAX_D || !is_pow2(c->page) || c->page < 32 || c->page > 256 ||
-      c->heads > GMM_KV_MAX_HEADS)
-    return GMM_ERR_UNSUPPORTED;
-  return GMM_OK;
-}
-
 int check_seqs(const gmm_kv_cache* c, const gmm_kv_batch* s, int64_t tokens, Seqs* o) {
   if (!s || !s->cu || !s->total || !s->pages) return GMM_ERR_INVALID_ARG;
   if (s->batch < 1 || s->max_pages < 1 || s->pages_stride < s->max_pages || tokens < 0)
@@ -2057,11 +2033,6 @@ int check_heads(const gmm_kv_cache* c, int32_t hq) {
 
 int64_t ws_need(const gmm_kv_cache* c, int64_t tokens, int hq, int32_t batch, int32_t max_pages) {
   return kv::ws_need(c->heads, c->page, c->d, tokens, hq, batch, max_pages, GMM_KV_MAX_KEEP);
-}
-
-int check_kv_ws(void* ws, size_t have, int64_t need) {
-  if (!ws || ((uintptr_t)ws & 255) || (int64_t)have < need) return GMM_ERR_WORKSPACE;
-  return GMM_OK;
 }
 
 template <typename T>

@@ -1,0 +1,243 @@
+"""Beam search's selection against its definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2606_10896_amd as gmm
+from poolcheck import INF, check_beam
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def _inputs(batch, beams, vocab, dtype, seed=0, pad=0):
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn(batch, beams, vocab + pad, generator=g) * 3).to(TYPES[dtype]).cuda()
+    s = -10.0 - 2.0 * torch.rand(batch, beams, generator=g)
+    return x[..., :vocab], s.cuda(), g
+
+
+def _select(x, s, m, done=None, **kw):
+    batch = x.shape[0]
+    out = (torch.empty(batch, m, device="cuda"), *(torch.empty(batch, m, dtype=torch.int32,
+                                                              device="cuda") for _ in range(2)))
+    od = torch.empty(batch, m, dtype=torch.bool, device="cuda") if done is not None else None
+    ws = gmm.beam_workspace(*x.shape).fill_(255)
+    gmm.gmm_beam_select(x, s, *out, ws, done=done, out_done=od, **kw)
+    torch.cuda.synchronize()
+    return (*out, od)
+
+
+def _check(x, s, m, **kw):
+    out = _select(x, s, m, **kw)
+    check_beam(out, x, s, m, **kw)
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("batch,beams,vocab,m", [
+    (1, 1, 1, 1), (1, 1, 1, 4), (2, 3, 2, 6), (1, 4, 63, 4), (3, 2, 257, 64), (1, 64, 100, 64),
+    (2, 5, 2047, 5), (2, 5, 2048, 5), (2, 5, 2049, 10), (1, 1, 4097, 64), (1, 2, 9000, 1),
+    (3, 8, 20011, 16), (1, 64, 10007, 64), (2, 4, 131072, 8), (70, 2, 300, 2)])
+def test_sizes(batch, beams, vocab, m, dtype):
+    x, s, _ = _inputs(batch, beams, vocab, dtype, seed=vocab + m)
+    _check(x, s, m)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [40, 2500, 50001])
+def test_masks_finished_beams_weights(vocab, dtype):
+    x, s, g = _inputs(4, 6, vocab, dtype, seed=vocab, pad=5)
+    words = (vocab + 31) // 32
+    mask = torch.randint(-2 ** 31, 2 ** 31, (4, 6, words), generator=g).to(torch.int32)
+    mask[1, 2] = 0                                       # nothing allowed
+    mask[2] = 0                                          # in a whole sequence
+    mask[3, 0] = 0
+    mask[3, 0, vocab // 64] = 1 << 3                     # one word
+    done = torch.rand(4, 6, generator=g) < 0.4
+    weight = (0.1 + torch.rand(4, 6, generator=g)).cuda()
+    eos = vocab - 1
+    _check(x, s, 12, mask=mask.cuda())
+    _check(x, s, 12, done=done.cuda(), eos=eos)
+    _check(x, s, 7, weight=weight, scale=0.37)
+    _check(x, s, 12, mask=mask.cuda(), done=done.cuda(), eos=eos, weight=weight, scale=2.5)
+    none = torch.zeros_like(mask)
+    out = _check(x, s, 3, mask=none.cuda())
+    assert (out[1] == -1).all()
+    out = _check(x, s, 3, done=torch.ones_like(done).cuda(), eos=0)
+    assert (out[2] == 0).all() and out[3].all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_values_that_are_not_finite(dtype):
+    vocab = 5000
+    x, s, _ = _inputs(3, 8, vocab, dtype, seed=5)
+    x = x.clone()
+    mask = torch.full((3, 8, (vocab + 31) // 32), -1, dtype=torch.int32)
+    mask[0, 3, 100] = ~(1 << 7)
+    x[0, 0, 4999] = math.nan
+    x[0, 1, 0] = INF
+    x[0, 2, :] = -INF
+    x[0, 3, 3207] = math.nan                             # forbidden: word 100, bit 7
+    x[0, 4, 17:] = -INF
+    x[0, 5, 2048:4096] = -INF                            # a whole run
+    x[1] = -INF
+    x[2, 0] = math.nan
+    s[0, 6] = math.nan
+    s[0, 7] = INF
+    done = torch.zeros(3, 8, dtype=torch.bool)
+    done[2, 0] = True                                    # its logits do not matter
+    w = torch.ones(3, 8, device="cuda")
+    w[2, 1:4] = torch.tensor([0.0, -1.0, math.nan])
+    w[2, 4] = INF
+    _check(x, s, 20, mask=mask.cuda(), done=done.cuda(), eos=11, weight=w)
+    out = _check(x, s, 64)
+    assert (out[1][1] == -1).all()
+
+
+def test_extreme_logits():
+    """Differences and products past the type's range: their weight is 0."""
+    x, s, _ = _inputs(1, 2, 3000, "f32")
+    x = x.clone()
+    x[0, 0, :] = -3e38
+    x[0, 0, 77] = 3e38
+    for scale in (1e-6, 1.0, 1e6):
+        out = _check(x, s, 2, scale=scale)
+        assert torch.isfinite(out[0]).all()
+    # logits whose differences vanish in the scores: ties
+    out = _select(x[:, 1:] * 1e-30, s[:, 1:].contiguous(), 9)
+    assert out[2][0].tolist() == list(range(9))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ties_go_to_the_lower_index(dtype):
+    """Equal logits, equal beams, logits in ascending and descending order."""
+    s = torch.full((1, 5), -3.0, device="cuda")
+    flat = torch.ones(1, 5, 9001, dtype=TYPES[dtype], device="cuda")
+    out = _select(flat, s, 64)
+    assert out[1][0].tolist() == [0] * 64 and out[2][0].tolist() == list(range(64))
+    one = (torch.randn(9001, generator=torch.Generator().manual_seed(3)) * 2).to(TYPES[dtype])
+    same = one.cuda().expand(1, 5, 9001)                 # strides 0
+    out = _select(same, s, 15)
+    assert out[1][0].tolist() == [0, 1, 2, 3, 4] * 3 or dtype == "bf16"
+    order = torch.sort(one.double(), descending=True, stable=True)
+    cand = sorted((-float(v), j, int(i)) for j in range(5)
+                  for v, i in zip(order.values[:15], order.indices[:15]))[:15]
+    assert out[1][0].tolist() == [c[1] for c in cand]
+    assert out[2][0].tolist() == [c[2] for c in cand]
+    up = torch.arange(9001, device="cuda").float().view(1, 1, -1) * 1e-3
+    up = up.expand(1, 5, 9001).contiguous()
+    out = _check(up, s - torch.arange(5, device="cuda") * 2e-4, 33)
+    _check(up.flip(2).contiguous(), s, 33)
+
+
+def test_first_step_and_places_without_a_beam():
+    x, s, _ = _inputs(3, 4, 777, "f32")
+    s[:, 1:] = -INF
+    out = _check(x, s, 8)
+    assert (out[1].cpu() == (torch.arange(3) * 4)[:, None]).all()
+    s[1] = -INF
+    out = _check(x, s, 8)
+    assert (out[1][1] == -1).all() and (out[0][1] == -INF).all()
+
+
+@pytest.mark.parametrize("pad,off", [(0, 0), (1, 0), (3, 1), (24, 7)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_strides_and_addresses(dtype, pad, off):
+    """The same words at any address give the same bits."""
+    vocab = 4101
+    x, s, _ = _inputs(2, 3, vocab, dtype, seed=9)
+    want = _select(x.contiguous(), s, 6)
+    big = torch.full((2 * 3 * (vocab + pad) + 64,), 9.0, dtype=x.dtype, device="cuda")
+    view = big[off:off + 6 * (vocab + pad)].view(2, 3, vocab + pad)[..., :vocab]
+    view.copy_(x)
+    got = _select(view, s, 6)
+    swapped = big[off:off + 6 * (vocab + pad)].view(3, 2, vocab + pad)[..., :vocab].transpose(0, 1)
+    swapped.copy_(x)
+    again = _select(swapped, s, 6)
+    for a, b, c in zip(want[:3], got, again):
+        assert torch.equal(a, b) and torch.equal(a, c)
+
+
+def test_offsets_past_32_bits():
+    step = (1 << 31) + 12345
+    try:
+        big = torch.empty(step + 40000, dtype=torch.bfloat16, device="cuda")
+    except torch.OutOfMemoryError:
+        pytest.skip("no memory")
+    x = big.as_strided((2, 2, 20000), (step, 20000, 1))
+    src, s, _ = _inputs(2, 2, 20000, "bf16", seed=4)
+    x.copy_(src)
+    a, b = _select(x, s, 4), _select(src, s, 4)
+    for u, v in zip(a[:3], b):
+        assert torch.equal(u, v)
+
+
+def test_largest_row():
+    """A long vocabulary: thousands of runs a beam."""
+    vocab = (1 << 22) + 3
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.empty(1, 2, vocab, device="cuda").normal_(generator=g)
+    s = torch.tensor([[-1.0, -1.5]], device="cuda")
+    _check(x, s, 5)
+
+
+def test_nothing_else_is_written():
+    x, s, _ = _inputs(2, 3, 500, "f32")
+    m = 5
+    guard = [torch.full((4, m), f, dtype=t, device="cuda")
+             for f, t in ((7.0, torch.float32), (7, torch.int32), (7, torch.int32))]
+    gmm.gmm_beam_select(x, s, *(t[1:3] for t in guard), gmm.beam_workspace(2, 3, 500))
+    for t in guard:
+        assert (t[0] == 7).all() and (t[3] == 7).all() and (t[1:3] != 7).any()
+
+
+def test_no_sequences():
+    x = torch.empty(0, 3, 500, device="cuda")
+    e = lambda t: torch.empty(0, 4, dtype=t, device="cuda")
+    gmm.gmm_beam_select(x, torch.empty(0, 3, device="cuda"), e(torch.float32), e(torch.int32),
+                        e(torch.int32), gmm.beam_workspace(1, 3, 500))
+
+
+def test_two_graphs_share_a_workspace():
+    cases = [_inputs(3, 4, 5001, "bf16", seed=1)[:2], _inputs(2, 6, 3000, "f32", seed=2)[:2]]
+    ws = torch.empty(max(gmm.beam_workspace_bytes(*x.shape) for x, _ in cases), dtype=torch.uint8,
+                     device="cuda")
+    runs = []
+    for x, s in cases:
+        m = 5
+        out = (torch.zeros(x.shape[0], m, device="cuda"),
+               *(torch.zeros(x.shape[0], m, dtype=torch.int32, device="cuda") for _ in range(2)))
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            gmm.gmm_beam_select(x, s, *out, ws)
+        runs.append((graph, x, s, out, m))
+    for turn in range(4):
+        for graph, x, s, out, m in runs:
+            x.copy_(x.roll(turn + 1, 2).clone())
+            for t in out:
+                t.zero_()
+            graph.replay()
+        torch.cuda.synchronize()
+        for graph, x, s, out, m in runs:
+            for a, b in zip(out, _select(x, s, m)):
+                assert torch.equal(a, b), turn
+
+
+def test_calls_on_two_streams():
+    cases = [_inputs(8, 4, 30001, "bf16", seed=i)[:2] for i in range(2)]
+    want = [_select(x, s, 4) for x, s in cases]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [(torch.empty(8, 4, device="cuda"), *(torch.empty(8, 4, dtype=torch.int32, device="cuda")
+                                                 for _ in range(2))) for _ in range(2)]
+    ws = [gmm.beam_workspace(8, 4, 30001) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for i, (x, s) in enumerate(cases):
+            gmm.gmm_beam_select(x, s, *outs[i], ws[i], stream=streams[i])
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        for a, b in zip(o, w):
+            assert torch.equal(a, b)
