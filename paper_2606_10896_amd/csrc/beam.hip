@@ -12,6 +12,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <float.h>
+#include <limits.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -26,7 +28,6 @@ using namespace kv;
 constexpr double kLog2eD = 1.4426950408889634;
 constexpr int kRun = 2048;        // words of a run
 constexpr int kJoinWaves = 8;     // waves of a sequence's workgroup
-constexpr uint32_t kNone = 0xffffffffu;
 
 struct BeamArgs {
   const void* x;
@@ -49,33 +50,127 @@ struct BeamArgs {
 
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) < INFINITY; }
 
-// 16 bytes of a row, whose address is a multiple of an element only
-template <typename T>
-__device__ __forceinline__ void load_vec(const T* p, float* o) {
-  constexpr int N = 16 / sizeof(T);
-  typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-  const V v = *reinterpret_cast<const V*>(p);
-#pragma unroll
-  for (int e = 0; e < N; ++e) o[e] = (float)v[e];
+// A lane's value from another lane of the wave, by the data path of the vector instructions; lanes
+// without a source get `old`.  The steps below join 2, 4, 8, 16 lanes (row_shr), rows of 16
+// (row_bcast:15) and halves (row_bcast:31); lane 63 holds the result.
+template <int kCtrl>
+__device__ __forceinline__ uint32_t dpp(uint32_t old, uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)v, kCtrl, 0xf, 0xf, false);
+}
+template <typename Op>
+__device__ __forceinline__ uint32_t wave_join(uint32_t v, uint32_t none, Op op) {
+  v = op(v, dpp<0x111>(none, v));
+  v = op(v, dpp<0x112>(none, v));
+  v = op(v, dpp<0x114>(none, v));
+  v = op(v, dpp<0x118>(none, v));
+  v = op(v, dpp<0x142>(none, v));
+  v = op(v, dpp<0x143>(none, v));
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  return wave_join(v, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+__device__ __forceinline__ uint32_t bits_of(float v) { return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ float float_of(uint32_t v) { return __builtin_bit_cast(float, v); }
+__device__ __forceinline__ float wave_max(float v) {
+  return float_of(wave_join(bits_of(v), bits_of(-INFINITY), [](uint32_t a, uint32_t b) {
+    return bits_of(fmaxf(float_of(a), float_of(b)));
+  }));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  return float_of(wave_join(bits_of(v), 0u, [](uint32_t a, uint32_t b) {
+    return bits_of(float_of(a) + float_of(b));
+  }));
+}
+// lane `i`'s value, of a lane that is the same for the wave
+__device__ __forceinline__ uint64_t lane_value(uint64_t v, int i) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((int)v, i);
+}
+template <int kCtrl>
+__device__ __forceinline__ double add_from(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return v + __builtin_bit_cast(double, (uint64_t)dpp<kCtrl>(0, (uint32_t)(u >> 32)) << 32 |
+                                            dpp<kCtrl>(0, (uint32_t)u));
+}
+__device__ __forceinline__ double wave_sum(double v) {
+  v = add_from<0x111>(v);
+  v = add_from<0x112>(v);
+  v = add_from<0x114>(v);
+  v = add_from<0x118>(v);
+  v = add_from<0x142>(v);
+  v = add_from<0x143>(v);
+  return __builtin_bit_cast(double, lane_value(__builtin_bit_cast(uint64_t, v), 63));
+}
+// sum over the lanes up to this one
+__device__ __forceinline__ int lanes_sum(int v) {
+  v += (int)dpp<0x111>(0, v);
+  v += (int)dpp<0x112>(0, v);
+  v += (int)dpp<0x114>(0, v);
+  v += (int)dpp<0x118>(0, v);
+  // rows of 16 lanes: the sum of the first and of the third to the next, that of the first half
+  // to the second
+  v += (int)__builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+  v += (int)__builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+// set bits of the lanes before
+__device__ __forceinline__ int below(uint64_t bits) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32),
+                                   __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
 }
 
-// Words at .. at + N - 1 of a beam; -inf past the vocabulary and where the mask forbids them.
+// 16 bytes of words: at an address that is a multiple of an element only, past the vocabulary
+// -inf, and -inf where the mask forbids
 template <typename T>
-__device__ __forceinline__ void load_words(const BeamArgs& a, const T* x, const uint32_t* mask,
-                                           int at, float* o) {
-  constexpr int N = 16 / sizeof(T);
-  if (at + N <= a.vocab) {
-    load_vec<T>(x + at, o);
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e) o[e] = at + e < a.vocab ? (float)x[at + e] : -INFINITY;
+struct Words {
+  static constexpr int N = 16 / sizeof(T);
+  typedef T V __attribute__((ext_vector_type(N)));
+  typedef V Unaligned __attribute__((aligned(sizeof(T))));
+  static constexpr int kSteps = kRun / (64 * N);       // of a run
+
+  __device__ __forceinline__ static int at(int run, int step) {
+    return run * kRun + (step * 64 + (int)(threadIdx.x & 63)) * N;
   }
-  if (mask && at < a.vocab) {
-    const uint32_t bits = mask[at >> 5] >> (at & 31);
+  // a run's words; all loads are issued before any is waited for
+  __device__ __forceinline__ static void load(const BeamArgs& a, const T* x, const uint32_t* mask,
+                                              int run, V* v) {
+    uint32_t bits[kSteps];
+    if (mask) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) o[e] = bits >> e & 1 ? o[e] : -INFINITY;
+      for (int i = 0; i < kSteps; ++i) bits[i] = mask[min(at(run, i), a.vocab - 1) >> 5];
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int p = at(run, i);
+      if (p + N <= a.vocab) {
+        v[i] = *reinterpret_cast<const Unaligned*>(x + p);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[i][e] = (T)-INFINITY;
+      }
+    }
+    const int last = a.vocab & -N;                      // the words of an incomplete vector
+    if (last < a.vocab && last / kRun == run) {
+      V t;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        t[e] = (T)-INFINITY;
+        if (last + e < a.vocab) t[e] = x[last + e];
+      }
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i)
+        if (at(run, i) == last) v[i] = t;
+    }
+    if (!mask) return;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const uint32_t b = bits[i] >> (at(run, i) & 31);
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[i][e] = b >> e & 1 ? v[i][e] : (T)-INFINITY;
+    }
   }
-}
+};
 
 template <typename T>
 __device__ __forceinline__ const T* row_of(const BeamArgs& a, int64_t row) {
@@ -94,221 +189,487 @@ __global__ __launch_bounds__(256) void k_beam_run(BeamArgs a) {
   const int64_t row = item / a.runs;
   if (row >= a.rows) return;
   if (!finite(a.score[row]) || (a.done && a.done[row])) return;
-  constexpr int N = 16 / sizeof(T), L = kRun / (64 * N);
+  constexpr int N = Words<T>::N, L = Words<T>::kSteps;
   const int run = (int)(item - row * a.runs);
-  const T* x = row_of<T>(a, row);
-  const uint32_t* mask = mask_of(a, row);
-  float v[L][N];
-#pragma unroll
-  for (int i = 0; i < L; ++i)
-    load_words<T>(a, x, mask, run * kRun + (i * 64 + lane) * N, v[i]);
+  typename Words<T>::V v[L];
+  Words<T>::load(a, row_of<T>(a, row), mask_of(a, row), run, v);
   float mx = -INFINITY;
 #pragma unroll
   for (int i = 0; i < L; ++i)
 #pragma unroll
-    for (int e = 0; e < N; ++e) mx = fmaxf(mx, v[i][e]);
-  for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    for (int e = 0; e < N; ++e) mx = fmaxf(mx, (float)v[i][e]);
+  mx = wave_max(mx);
   const float base = mx > -INFINITY ? mx : 0.f;
   // the difference before the product: its rounding, not that of a large maximum's product
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < L; ++i)
 #pragma unroll
-    for (int e = 0; e < N; ++e) sum[e & 3] += __builtin_amdgcn_exp2f((v[i][e] - base) * a.c);
+    for (int e = 0; e < N; ++e) sum[e & 3] += __builtin_amdgcn_exp2f(((float)v[i][e] - base) * a.c);
   float z = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-  for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o);
+  z = wave_sum(z);
   if (lane == 0) a.part[item] = make_float2(mx, z);
 }
 
-// ---------------------------------------------------------------- sorted lists
-// A wave's list: lane i holds the i-th best of what it has seen, by (key, lower index).
-struct Entry {
-  double key;
-  uint32_t at;
+// ---------------------------------------------------------------- the best of many
+// Scores as whole numbers of the same order; 0 is no candidate.
+__device__ __forceinline__ uint64_t ordered(double v) {
+  const int64_t u = __builtin_bit_cast(int64_t, v + 0.0);      // -0 is 0
+  return (uint64_t)(u ^ (u >> 63 | INT64_MIN));
+}
+__device__ __forceinline__ double value_of(uint64_t k) {
+  const int64_t u = (int64_t)k;
+  return __builtin_bit_cast(double, u < 0 ? u ^ INT64_MIN : ~u);
+}
+
+// What pick() takes of the numbers given to it: those above `least`, and the first `ties` equal to it.
+struct Picked {
+  uint64_t least;
+  int ties, count;
+  // a number that comes later, behind these in order, is among the best only from here on
+  __device__ __forceinline__ uint64_t floor() const { return least + (ties != INT_MAX); }
 };
-__device__ __forceinline__ Entry no_entry() { return Entry{-INFINITY, kNone}; }
-__device__ __forceinline__ bool before(const Entry& a, const Entry& b) {
-  return a.key > b.key || (a.key == b.key && a.at < b.at);
+
+// The m largest of the numbers in v (64 a step; 0 is none), ties to the first in the order of
+// steps and lanes: the threshold is built bit by bit from the first bit in which the numbers
+// differ, until m numbers reach it.  Some ten rounds for scores.  Equal numbers (logits of 8
+// bits, say) never give m: every few rounds one of those still in question is tried.
+template <int C>
+__device__ __forceinline__ Picked pick(const uint64_t* v, int m) {
+  const auto reach = [&](uint64_t t) {
+    int n = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) n += __popcll(__ballot(v[c] >= t));
+    return n;
+  };
+  int n = reach(1);
+  if (n <= m) return Picked{1, INT_MAX, n};
+  uint32_t hi = 0, lo = 0;             // of the upper halves: the largest, the smallest's complement
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const uint32_t h = (uint32_t)(v[c] >> 32);
+    hi = max(hi, h);
+    lo = max(lo, v[c] ? ~h : 0u);
+  }
+  hi = wave_max(hi);
+  lo = ~wave_max(lo);
+  // bits above the first that differs are those of every number
+  uint32_t diff = hi ^ lo;
+  uint64_t t = (uint64_t)hi << 32, step = (uint64_t)1 << 32;        // the bit above the next one to try
+  if (diff) {
+    const int top = 31 - __builtin_clz(diff);
+    t = top == 31 ? 0 : (uint64_t)(hi >> (top + 1) << (top + 1)) << 32;
+    step <<= top;                                    // the first to try
+  } else {
+    step >>= 1;
+  }
+  for (int rounds = 10; step; rounds = 5) {
+    do {
+      const uint64_t up = t | step;
+      step >>= 1;
+      n = reach(up);
+      t = n >= m ? up : t;
+    } while (n != m && step && --rounds);
+    if (n == m) return Picked{t, INT_MAX, m};
+    uint64_t probe = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const uint64_t in = __ballot(v[c] >= t && v[c] - t < 2 * step);
+      if (probe == 0 && in) probe = lane_value(v[c], __builtin_ctzll(in));
+    }
+    const int more = reach(probe + 1);
+    if (probe && more < m && reach(probe) >= m) return Picked{probe, m - more, m};
+  }
+  return Picked{t, m - reach(t + 1), m};
 }
-__device__ __forceinline__ Entry shuffle_xor(const Entry& e, int o) {
-  return Entry{__shfl_xor(e.key, o), (uint32_t)__shfl_xor((int)e.at, o)};
+
+// The place of a lane's number among the first n lanes': how many are larger, or equal and before.
+__device__ __forceinline__ int place_of(uint64_t v, int n) {
+  int place = 0;
+  for (int i = 0; i < n; i += 4) {
+#pragma unroll
+    for (int k = i; k < i + 4; ++k) {                // past n: lanes of 0
+      const uint64_t other = lane_value(v, k);
+      place += other > v || (other == v && k < (int)(threadIdx.x & 63));
+    }
+  }
+  return place;
 }
-__device__ __forceinline__ Entry shuffle(const Entry& e, int lane) {
-  return Entry{__shfl(e.key, lane), (uint32_t)__shfl((int)e.at, lane)};
+
+// Is v among what was picked?  `seen`: numbers equal to `least` in the steps before.
+__device__ __forceinline__ bool taken(const Picked& p, uint64_t v, int* seen) {
+  const uint64_t same = __ballot(v == p.least && v != 0);
+  const bool in = v > p.least ||
+                  (v == p.least && v != 0 && *seen + below(same) < p.ties);
+  *seen += __popcll(same);
+  return in;
 }
-__device__ __forceinline__ void stage(Entry& e, int o, bool up) {
-  const Entry p = shuffle_xor(e, o);
-  const bool low = (threadIdx.x & o) == 0;
-  if (before(p, e) == (low != up)) e = p;
-}
-// bitonic: 64 entries in any order
-__device__ __forceinline__ void sort64(Entry& e) {
-  for (int k = 2; k <= 64; k <<= 1)
-    for (int o = k >> 1; o > 0; o >>= 1) stage(e, o, (threadIdx.x & k & 63) != 0);
-}
-// the 64 best of two sorted lists
-__device__ __forceinline__ void merge64(Entry& a, const Entry& b) {
-  const Entry r = shuffle(b, 63 - (threadIdx.x & 63));
-  if (before(r, a)) a = r;
-  for (int o = 32; o > 0; o >>= 1) stage(a, o, false);
-}
+
+constexpr int kChunk = 1024;           // runs looked at together
+constexpr int kLane = 1 + kChunk / 64; // of a lane: neighbours, odd for the banks of LDS
+constexpr int kBuffer = GMM_BEAM_MAX + 512;       // words that a wave holds
+
+struct Word {
+  uint64_t key;
+  uint32_t at;                         // beam * vocab + word
+  float x;
+};
 
 struct Join {
-  double key[kJoinWaves][64];
-  uint32_t at[kJoinWaves][64];
-  float top[GMM_BEAM_MAX];          // a beam's largest logit
-  double logz[GMM_BEAM_MAX];        // log sum exp(scale (x - top))
-  float score[GMM_BEAM_MAX];
+  double logz[GMM_BEAM_MAX];           // log sum exp(scale (x - top))
   double weight[GMM_BEAM_MAX];
-  int kind[GMM_BEAM_MAX];           // 0: no candidate, 1: live, 2: finished
-  Entry buf[kJoinWaves][128];
+  float top[GMM_BEAM_MAX];             // a beam's largest logit
+  float score[GMM_BEAM_MAX];
+  int kind[GMM_BEAM_MAX];              // 0: no candidate, 1: live, 2: finished
+  uint32_t hi[64 * kLane], lo[64 * kLane];   // scores of the best runs so far, then of a chunk
+  int run[64];                         // the best runs, in order
+  uint64_t list[64];                   // few runs while they are picked from
+  int list_run[64];
+  uint64_t least;
+  int kept;
+  int count[kJoinWaves];
+  Word word[kJoinWaves][kBuffer];
 };
-
-// the waves' lists into wave 0's; all lists are the joined one afterwards
-__device__ __forceinline__ void join_lists(Join& s, Entry& e) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  for (int n = kJoinWaves; n > 1; n >>= 1) {
-    s.key[w][lane] = e.key;
-    s.at[w][lane] = e.at;
-    __syncthreads();
-    if (w < n / 2) merge64(e, Entry{s.key[w + n / 2][lane], s.at[w + n / 2][lane]});
-    __syncthreads();
-  }
-  s.key[w][lane] = e.key;
-  s.at[w][lane] = e.at;
-  __syncthreads();
-  e = Entry{s.key[0][lane], s.at[0][lane]};
-  __syncthreads();
-}
 
 // l of a live beam's logit, from its difference to the largest: products of large logits would
 // cancel, and not alike everywhere (multiply and add may be fused)
 __device__ __forceinline__ double total_of(const BeamArgs& a, const Join& s, int j, float x) {
   return (double)s.score[j] + fma(a.scale, (double)x - (double)s.top[j], -s.logz[j]);
 }
-__device__ __forceinline__ double key_of(const BeamArgs& a, const Join& s, int j, float x) {
-  return x > -INFINITY ? s.weight[j] * total_of(a, s, j, x) : -INFINITY;
+__device__ __forceinline__ uint64_t key_of(const BeamArgs& a, const Join& s, int j, float x) {
+  return x > -INFINITY ? ordered(s.weight[j] * total_of(a, s, j, x)) : 0;
+}
+
+// the score of a run's largest logit
+__device__ __forceinline__ uint64_t run_key(const BeamArgs& a, const Join& s, int j, int run, float x) {
+  if (s.kind[j] == 1) return key_of(a, s, j, x);
+  // a finished beam has one run, that of its end word
+  return s.kind[j] == 2 && run == a.eos / kRun ? ordered(s.weight[j] * (double)s.score[j]) : 0;
+}
+
+// A logit below which no word of beam j has the score `floor`: the logit of that score in fp32, less
+// what its roundings may be (each of the four terms has a few units of 2^-24, of its size).  The
+// smallest number, which -infinity does not reach, if there is none.
+__device__ __forceinline__ float logit_of(const BeamArgs& a, const Join& s, int j, uint64_t floor) {
+  if (floor <= 1) return -FLT_MAX;
+  const float l = (float)value_of(floor) * __builtin_amdgcn_rcpf((float)s.weight[j]);
+  const float z = (float)s.logz[j], inv = __builtin_amdgcn_rcpf((float)a.scale);
+  const float x = s.top[j] + ((l - s.score[j]) + z) * inv;
+  const float less = ((fabsf(l) + fabsf(s.score[j]) + fabsf(z)) * inv + fabsf(x)) * 0x1p-20f + 1e-30f;
+  return x - less > -FLT_MAX ? x - less : -FLT_MAX;      // also for what is no number
+}
+
+// All runs of the sequence fit a chunk, those of a beam a wave: their scores are formed with log Z.
+__device__ __forceinline__ bool one_chunk(const BeamArgs& a) {
+  return a.runs <= 64 && a.beams * a.runs <= kChunk;
+}
+__device__ __forceinline__ void put_run(Join& s, int i, uint64_t key) {
+  s.hi[i] = (uint32_t)(key >> 32);
+  s.lo[i] = (uint32_t)key;
+}
+
+// log Z of up to two beams of a wave, j and j + kJoinWaves: their loads go together
+__device__ __forceinline__ void join_beams(const BeamArgs& a, Join& s, int64_t row0, int j0) {
+  const int lane = threadIdx.x & 63;
+  float sc[2], wt[2];
+  int fin[2];
+  float2 v[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int64_t row = row0 + min(j0 + i * kJoinWaves, a.beams - 1);
+    sc[i] = a.score[row];
+    wt[i] = a.weight ? a.weight[row] : 1.f;
+    fin[i] = a.done ? a.done[row] : 0;
+    v[i] = a.part[row * a.runs + min(lane, a.runs - 1)];
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int j = j0 + i * kJoinWaves;
+    if (j >= a.beams) break;
+    int kind = finite(sc[i]) && wt[i] > 0.f && finite(wt[i]) ? fin[i] ? 2 : 1 : 0;
+    double logz = 0.0;
+    float mx = -INFINITY;
+    if (kind == 1) {
+      const float2* p = a.part + (row0 + j) * a.runs;
+      float2 u = v[i];
+      if (lane < a.runs) mx = u.x;
+      for (int r = lane + 64; r < a.runs; r += 64) mx = fmaxf(mx, p[r].x);
+      mx = wave_max(mx);
+      double z = 0.0;
+      for (int r = lane; r < a.runs; r += 64) {
+        if (r >= 64) u = p[r];
+        // a run without a word adds its sum, 0, or NaN
+        z += (double)(u.y * (u.x > -INFINITY ? __builtin_amdgcn_exp2f((u.x - mx) * a.c) : 1.f));
+      }
+      z = wave_sum(z);
+      logz = log(z);
+      if (!finite(mx) || !(z > 0.0)) kind = 0;       // no word, NaN or +infinity
+    }
+    if (lane == 0) {
+      s.logz[j] = logz;
+      s.weight[j] = wt[i];
+      s.top[j] = mx;
+      s.score[j] = sc[i];
+      s.kind[j] = kind;
+    }
+    if (one_chunk(a) && lane < a.runs) put_run(s, j * a.runs + lane, run_key(a, s, j, lane, v[i].x));
+  }
+}
+
+// Those of a lane's numbers (bits of `more`, and of `same`, which equal the threshold) that were
+// picked: of the equal ones the first `ties`, lane after lane.
+__device__ __forceinline__ uint32_t taken(uint32_t more, uint32_t same, int ties) {
+  const int n = __popc(same);
+  int left = ties == INT_MAX ? n : ties - (lanes_sum(n) - n);
+  for (int k = n; k > max(left, 0); --k) same &= ~(0x80000000u >> __builtin_clz(same));
+  return more | same;
+}
+
+// The best of the first n of s.hi / s.lo (`kept` runs, then those from `base` on), by one wave:
+// first those that reach the m-th largest of the lanes' maxima, in their upper halves; that
+// leaves few.
+__device__ __forceinline__ void pick_runs(const BeamArgs& a, Join& s, int base, int kept, int n) {
+  const int lane = threadIdx.x & 63;
+  const int per = (n + 63) / 64 | 1, first = lane * per;
+  const auto has = [&](int c) { return c < per && first + c < n; };
+  uint32_t h[kLane], top = 0, more = 0, same = 0;
+#pragma unroll
+  for (int c = 0; c < kLane; ++c) {
+    h[c] = has(c) ? s.hi[first + c] : 0;
+    top = max(top, h[c]);
+  }
+  // the m-th largest: the smallest of those that fewer than m are larger than
+  const int lanes = (n + per - 1) / per;
+  int larger = 0;
+  for (int i = 0; i < lanes; i += 4) {
+#pragma unroll
+    for (int k = i; k < i + 4; ++k)
+      larger += (uint32_t)__builtin_amdgcn_readlane((int)top, k) > top;
+  }
+  uint32_t least = ~wave_max(larger < a.m ? ~top : 0u);
+  least = max(least, 1u);              // a number is not 0 in its upper half
+#pragma unroll
+  for (int c = 0; c < kLane; ++c) more |= (uint32_t)(h[c] >= least) << c;
+  int upto = lanes_sum(__popc(more)), all = __builtin_amdgcn_readlane(upto, 63);
+  if (all > 64) {                      // many of one size
+    uint64_t v[kLane];
+#pragma unroll
+    for (int c = 0; c < kLane; ++c) v[c] = has(c) ? (uint64_t)h[c] << 32 | s.lo[first + c] : 0;
+    const Picked q = pick<kLane>(v, a.m);
+    more = 0;
+#pragma unroll
+    for (int c = 0; c < kLane; ++c) {
+      more |= (uint32_t)(v[c] > q.least) << c;
+      same |= (uint32_t)(v[c] && v[c] == q.least) << c;
+    }
+    more = taken(more, same, q.ties);
+    upto = lanes_sum(__popc(more));
+    all = q.count;
+  }
+  for (int at = upto - __popc(more); more; more &= more - 1) {
+    const int i = first + __builtin_ctz(more);
+    s.list[at] = (uint64_t)s.hi[i] << 32 | s.lo[i];
+    s.list_run[at++] = i < kept ? s.run[i] : base + i - kept;
+  }
+  const uint64_t key = lane < all ? s.list[lane] : 0;
+  const int run = s.list_run[lane], place = place_of(key, all);
+  const bool in = lane < all && place < a.m;
+  const uint64_t bal = __ballot(in), last = __ballot(in && place == a.m - 1);
+  if (in) {
+    const int at = below(bal);
+    s.hi[at] = (uint32_t)(key >> 32);
+    s.lo[at] = (uint32_t)key;
+    s.run[at] = run;
+  }
+  if (lane == 0) {
+    s.kept = __popcll(bal);
+    // the m-th run's score, 1 as long as there are fewer
+    s.least = last ? lane_value(key, __builtin_ctzll(last)) : 1;
+  }
+}
+
+// The m best runs of the sequence, in order, into s.run, their scores into s.hi / s.lo, their number
+// into s.kept, and the m-th one's score into s.least.
+__device__ __forceinline__ void best_runs(const BeamArgs& a, Join& s, int64_t row0) {
+  const int tid = threadIdx.x;
+  const int runs = a.beams * a.runs;
+  const float inv = 1.f / (float)a.runs;
+  const float2* part = a.part + row0 * a.runs;
+  int kept = 0;
+  uint64_t least = 1;
+  for (int base = 0; base < runs; base += kChunk) {
+    if (!one_chunk(a)) {
+      bool any = false;
+      for (int t = tid; t < min(kChunk, runs - base); t += 64 * kJoinWaves) {
+        const int i = base + t, j = (int)(((float)i + 0.5f) * inv);    // i / runs: exact below 2^21
+        uint64_t k = run_key(a, s, j, i - j * a.runs, part[i].x);
+        // an equal one is behind the m kept
+        if (k < least || (kept == a.m && k == least)) k = 0;
+        put_run(s, kept + t, k);
+        any |= k != 0;
+      }
+      if (!__syncthreads_or(any) && base > 0) continue;
+    }
+    if (tid < 64) pick_runs(a, s, base, kept, kept + min(kChunk, runs - base));
+    __syncthreads();
+    kept = s.kept;
+    least = s.least;
+  }
+}
+
+// Leaves the m best of a wave's n words, in their order.
+__device__ __forceinline__ Picked keep_words(Word* buf, int n, int m) {
+  constexpr int C = kBuffer / 64;
+  const int lane = threadIdx.x & 63;
+  uint64_t v[C];
+  Word e[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    v[c] = 0;
+    if (c * 64 + lane < n) {
+      e[c] = buf[c * 64 + lane];
+      v[c] = e[c].key;
+    }
+  }
+  const Picked p = pick<C>(v, m);
+  int k = 0, seen = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const bool in = taken(p, v[c], &seen);
+    const uint64_t bal = __ballot(in);
+    if (in) buf[k + below(bal)] = e[c];
+    k += __popcll(bal);
+  }
+  return p;
 }
 
 // A workgroup a sequence: log Z of its beams, its m best runs, their m best words.
 template <typename T>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(BeamArgs a) {
   __shared__ Join s;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t row0 = (int64_t)blockIdx.x * a.beams;
-  for (int j = w; j < a.beams; j += kJoinWaves) {
-    const float sc = a.score[row0 + j];
-    int kind = finite(sc) ? a.done && a.done[row0 + j] ? 2 : 1 : 0;
-    double logz = 0.0;
-    float mx = -INFINITY;
-    if (kind == 1) {
-      const float2* p = a.part + (row0 + j) * a.runs;
-      for (int r = lane; r < a.runs; r += 64) mx = fmaxf(mx, p[r].x);
-      for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-      double z = 0.0;
-      for (int r = lane; r < a.runs; r += 64) {
-        const float2 v = p[r];
-        // a run without a word adds its sum, 0, or NaN
-        z += (double)(v.y * (v.x > -INFINITY ? __builtin_amdgcn_exp2f((v.x - mx) * a.c) : 1.f));
-      }
-      for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o);
-      logz = log(z);
-      if (!finite(mx) || !(z > 0.0)) kind = 0;     // no word, NaN or +infinity
-    }
-    if (lane == 0) {
-      s.top[j] = mx;
-      s.logz[j] = logz;
-      s.score[j] = sc;
-      const float wt = a.weight ? a.weight[row0 + j] : 1.f;
-      s.weight[j] = wt;
-      s.kind[j] = wt > 0.f && finite(wt) ? kind : 0;
-    }
-  }
+  for (int j = w; j < a.beams; j += 2 * kJoinWaves) join_beams(a, s, row0, j);
   __syncthreads();
+  best_runs(a, s, row0);
 
-  // runs, numbered over the beams; a finished beam's is the one of its end word
-  Entry top = no_entry();
-  const int runs = a.beams * a.runs;
-  for (int c = w * 64; c < runs; c += 64 * kJoinWaves) {
-    Entry e = no_entry();
-    if (c + lane < runs) {
-      const int j = (c + lane) / a.runs, r = c + lane - j * a.runs;
-      e.at = c + lane;
-      if (s.kind[j] == 1) e.key = key_of(a, s, j, a.part[row0 * a.runs + c + lane].x);
-      else if (s.kind[j] == 2 && r == a.eos / kRun) e.key = s.weight[j] * (double)s.score[j];
-    }
-    if (c >= 64 * kJoinWaves && !__ballot(before(e, shuffle(top, 63)))) continue;
-    sort64(e);
-    merge64(top, e);
-  }
-  join_lists(s, top);
-  const int found = __popcll(__ballot(lane < a.m && top.key > -INFINITY));
-  const double least = found == a.m ? __shfl(top.key, a.m - 1) : -INFINITY;
-
-  // their words; index: beam * vocab + word
-  constexpr int N = 16 / sizeof(T);
-  Entry best = no_entry();
-  int held = 0;                     // entries of the wave's buffer
-  Entry* buf = s.buf[w];
-  const auto flush = [&](int n) {
-    Entry e = lane < n ? buf[lane] : no_entry();
-    sort64(e);
-    merge64(best, e);
-  };
-  for (int q = w; q < found; q += kJoinWaves) {
-    const int gid = __shfl((int)top.at, q);
+  // the words that reach the m-th best run's maximum; a wave takes neighbouring runs, so that
+  // the waves' words, one after the other, are in order
+  typedef Words<T> W;
+  Word* buf = s.word[w];
+  uint64_t floor = s.least;
+  int held = 0;
+  const int q1 = (w + 1) * s.kept / kJoinWaves;
+  for (int q = w * s.kept / kJoinWaves; q < q1; ++q) {
+    const int gid = __builtin_amdgcn_readfirstlane(s.run[q]);
     const int j = gid / a.runs, r = gid - j * a.runs;
-    const int64_t row = row0 + j;
+    typename W::V v[W::kSteps];
+    uint32_t steps = 0;                      // with words that may count
+    float least = -INFINITY;
     if (s.kind[j] == 2) {
-      if (lane == 0) buf[held] = Entry{s.weight[j] * (double)s.score[j],
-                                       (uint32_t)j * (uint32_t)a.vocab + (uint32_t)a.eos};
-      if (++held >= 64) {
-        flush(64);
-        held -= 64;
-      }
-      continue;
-    }
-    const T* x = row_of<T>(a, row);
-    const uint32_t* mask = mask_of(a, row);
-    for (int i = 0; i < kRun / (64 * N); ++i) {
-      const int at = r * kRun + (i * 64 + lane) * N;
-      float v[N];
-      load_words<T>(a, x, mask, at, v);
-      const Entry last = shuffle(best, a.m - 1);
+      steps = 1;
+    } else {
+      W::load(a, row_of<T>(a, row0 + j), mask_of(a, row0 + j), r, v);
+      least = logit_of(a, s, j, floor);
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const Entry c{key_of(a, s, j, v[e]), (uint32_t)j * (uint32_t)a.vocab + (uint32_t)(at + e)};
-        const bool in = c.key > -INFINITY && c.key >= least && before(c, last);
-        const uint64_t bal = __ballot(in);
-        if (!bal) continue;
-        if (in) buf[held + __popcll(bal & ((1ull << lane) - 1))] = c;
-        held += __popcll(bal);
-        if (held >= 64) {
-          flush(64);
-          held -= 64;
-          if (lane < held) buf[lane] = buf[64 + lane];
+      for (int i = 0; i < W::kSteps; ++i) {
+        float mx = (float)v[i][0];
+#pragma unroll
+        for (int e = 1; e < W::N; ++e) mx = fmaxf(mx, (float)v[i][e]);
+        if (__ballot(mx >= least)) steps |= 1u << i;
+      }
+    }
+    while (steps) {
+      const int i = __builtin_ctz(steps);
+      steps &= steps - 1;
+      if (s.kind[j] == 2) {
+        if (lane == 0)
+          buf[held] = Word{(uint64_t)s.hi[q] << 32 | s.lo[q], (uint32_t)j * a.vocab + a.eos, s.score[j]};
+        ++held;
+      } else {
+        typename W::V x = v[0];
+#pragma unroll
+        for (int c = 1; c < W::kSteps; ++c)
+          if (c == i) x = v[c];
+        // in the order of the words: those of the lanes before, and of this one.  What passes
+        // for its logit but has not the score is held as none.
+        int at = held, n = 0;
+#pragma unroll
+        for (int e = 0; e < W::N; ++e) {
+          const uint64_t bal = __ballot((float)x[e] >= least);
+          at += below(bal);
+          n += __popcll(bal);
         }
+#pragma unroll
+        for (int e = 0; e < W::N; ++e) {
+          if ((float)x[e] >= least) {
+            const uint64_t key = key_of(a, s, j, (float)x[e]);
+            buf[at++] = Word{key < floor ? 0 : key, (uint32_t)j * a.vocab + W::at(r, i) + e, (float)x[e]};
+          }
+        }
+        held += n;
+      }
+      if (held > GMM_BEAM_MAX) {
+        const Picked p = keep_words(buf, held, a.m);
+        held = p.count;
+        if (held == a.m) floor = max(floor, p.floor());
       }
     }
   }
-  if (held > 0) flush(held);
-  join_lists(s, best);
-  if (w != 0 || lane >= a.m) return;
-  const int64_t o = (int64_t)blockIdx.x * a.m + lane;
-  if (!(best.key > -INFINITY)) {
-    a.out_score[o] = -INFINITY;
-    a.out_parent[o] = -1;
-    a.out_token[o] = -1;
-    if (a.out_done) a.out_done[o] = 0;
-    return;
+  if (lane == 0) s.count[w] = held;
+  __syncthreads();
+  if (w != 0) return;
+
+  // all waves' words into wave 0's lanes
+  int total = 0;
+  for (int c = 0; c < kJoinWaves; ++c) total += s.count[c];
+  Word e{0, 0, 0.f};
+  if (total <= 64) {
+    int first = 0;
+    for (int c = 0; c < kJoinWaves; ++c) {
+      const int i = lane - first;
+      if (i >= 0 && i < s.count[c]) e = s.word[c][i];
+      first += s.count[c];
+    }
+  } else {
+    uint64_t v[kJoinWaves];
+    Word all[kJoinWaves];
+#pragma unroll
+    for (int c = 0; c < kJoinWaves; ++c) {
+      v[c] = 0;
+      if (lane < s.count[c]) {
+        all[c] = s.word[c][lane];
+        v[c] = all[c].key;
+      }
+    }
+    const Picked p = pick<kJoinWaves>(v, a.m);
+    int k = 0, seen = 0;
+#pragma unroll
+    for (int c = 0; c < kJoinWaves; ++c) {
+      const bool in = taken(p, v[c], &seen);
+      const uint64_t bal = __ballot(in);
+      if (in) s.word[0][k + below(bal)] = all[c];
+      k += __popcll(bal);
+    }
+    total = p.count;
+    if (lane < total) e = s.word[0][lane];
   }
-  const int j = (int)(best.at / (uint32_t)a.vocab), word = (int)(best.at - (uint32_t)j * a.vocab);
-  const bool fin = s.kind[j] == 2;
-  a.out_score[o] = fin ? s.score[j]
-                       : (float)total_of(a, s, j, (float)row_of<T>(a, row0 + j)[word]);
-  a.out_parent[o] = (int32_t)(row0 + j);
-  a.out_token[o] = word;
-  if (a.out_done) a.out_done[o] = fin || word == a.eos;
+  const int place = place_of(e.key, total), found = __popcll(__ballot(e.key != 0));
+  const int64_t o = (int64_t)blockIdx.x * a.m;
+  if (e.key != 0 && place < a.m) {
+    const int j = (int)(e.at / (uint32_t)a.vocab), word = (int)(e.at - (uint32_t)j * a.vocab);
+    const bool fin = s.kind[j] == 2;
+    a.out_score[o + place] = fin ? e.x : (float)total_of(a, s, j, e.x);
+    a.out_parent[o + place] = (int32_t)(row0 + j);
+    a.out_token[o + place] = word;
+    if (a.out_done) a.out_done[o + place] = fin || word == a.eos;
+  }
+  if (lane >= found && lane < a.m) {
+    a.out_score[o + lane] = -INFINITY;
+    a.out_parent[o + lane] = -1;
+    a.out_token[o + lane] = -1;
+    if (a.out_done) a.out_done[o + lane] = 0;
+  }
 }
 
 // ---------------------------------------------------------------- host
