@@ -23,7 +23,6 @@ using namespace kv;
 
 constexpr int kWaves = 16;                        // of the workgroup that ranks pages
 constexpr int kSpan = kWaves * 64 * 64;           // pages it ranks at a time
-constexpr int kPart = 16384;                      // bytes of a copy's work item
 
 __device__ __forceinline__ int pages_of(int keys, int shift) {
   return keys <= 0 ? 0 : (keys >> shift) + ((keys & ((1 << shift) - 1)) != 0);
@@ -42,62 +41,65 @@ struct CopyArgs {
   Pages src, dst;
   int bytes;                  // of a page's keys, and of its values: up to 2^27
   int box_bytes, heads;
-  int parts;                  // work items of a page's keys
   const int32_t* from;
   const int32_t* to;
   const int32_t* count;       // pairs, or null: n
   int n;
 };
 
-__device__ __forceinline__ void copy_part(const char* from, char* to, int n) {
-  const uint4* f = reinterpret_cast<const uint4*>(from);
-  uint4* t = reinterpret_cast<uint4*>(to);
-  if (n == kPart / 16) {
-    uint4 v[kPart / 4096];
-#pragma unroll
-    for (int i = 0; i < kPart / 4096; ++i) v[i] = f[threadIdx.x + i * 256];
-#pragma unroll
-    for (int i = 0; i < kPart / 4096; ++i) t[threadIdx.x + i * 256] = v[i];
-  } else {
-    for (int i = threadIdx.x; i < n; i += 256) t[i] = f[i];
-  }
-}
-
-// Work items 2 parts a pair: kPart bytes of the keys or of the values; the first also the box.
+// Work items of a pair: `parts` of its keys, as many of its values, and its box.  A thread moves 16
+// bytes in each of kSteps steps, all loads before the stores, streamed past the caches.
+template <int kThreads, int kSteps>
 __device__ __forceinline__ void copy_items(const CopyArgs& a, int block, int blocks) {
-  // a workgroup's items: `blocks` apart, counted in pairs and parts, without a division each
-  const int n = a.count ? *a.count : a.n, per = 2 * a.parts;
+  typedef uint32_t V __attribute__((ext_vector_type(4)));
+  constexpr int kBytes = kThreads * 16, kPart = kBytes * kSteps;
+  const int n = a.count ? *a.count : a.n;
+  const int parts = (a.bytes + kPart - 1) / kPart, per = 2 * parts + (a.dst.box != nullptr);
   const int step_pair = blocks / per, step_part = blocks - step_pair * per;
-  int pair = block / per, next = block - pair * per;
+  int pair = block / per, part = block - pair * per;
   while (pair < n) {
-    const int at_pair = pair;
-    int part = next;
+    const int from = a.from[pair], to = a.to[pair];
+    if (from >= 0 && from < a.src.pages && to >= 0 && to < a.dst.pages) {
+      if (part < 2 * parts) {
+        const bool values = part >= parts;
+        const int at = (values ? part - parts : part) * kPart + threadIdx.x * 16;
+        const char* f = (values ? a.src.v : a.src.k) + (int64_t)from * a.bytes + at;
+        char* t = (values ? a.dst.v : a.dst.k) + (int64_t)to * a.bytes + at;
+        V v[kSteps];
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+          if (at + i * kBytes < a.bytes)
+            v[i] = __builtin_nontemporal_load(reinterpret_cast<const V*>(f + i * kBytes));
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+          if (at + i * kBytes < a.bytes)
+            __builtin_nontemporal_store(v[i], reinterpret_cast<V*>(t + i * kBytes));
+      } else {
+        const char* f = a.src.box + (int64_t)from * a.box_bytes;
+        char* t = a.dst.box + (int64_t)to * a.box_bytes;
+        for (int at = threadIdx.x * 16; at < a.box_bytes; at += kBytes)
+          *reinterpret_cast<V*>(t + at) = *reinterpret_cast<const V*>(f + at);
+        for (int i = threadIdx.x; i < a.heads; i += kThreads)
+          a.dst.scale[(int64_t)to * a.heads + i] = a.src.scale[(int64_t)from * a.heads + i];
+      }
+    }
     pair += step_pair;
-    next += step_part;
-    if (next >= per) {
-      next -= per;
+    part += step_part;
+    if (part >= per) {
+      part -= per;
       ++pair;
     }
-    const int from = a.from[at_pair], to = a.to[at_pair];
-    if (from < 0 || from >= a.src.pages || to < 0 || to >= a.dst.pages) continue;
-    if (part == 0 && a.dst.box) {
-      const uint4* f = reinterpret_cast<const uint4*>(a.src.box + (int64_t)from * a.box_bytes);
-      uint4* t = reinterpret_cast<uint4*>(a.dst.box + (int64_t)to * a.box_bytes);
-      for (int i = threadIdx.x; i < a.box_bytes / 16; i += 256) t[i] = f[i];
-      for (int i = threadIdx.x; i < a.heads; i += 256)
-        a.dst.scale[(int64_t)to * a.heads + i] = a.src.scale[(int64_t)from * a.heads + i];
-    }
-    const bool values = part >= a.parts;
-    if (values) part -= a.parts;
-    const int at = part * kPart;
-    copy_part((values ? a.src.v : a.src.k) + (int64_t)from * a.bytes + at,
-              (values ? a.dst.v : a.dst.k) + (int64_t)to * a.bytes + at,
-              min(a.bytes - at, kPart) / 16);
   }
 }
 
+// The number of pairs is known to the host: a workgroup an item, in the order of the addresses.
 __global__ __launch_bounds__(256) void k_kv_copy(CopyArgs a) {
-  copy_items(a, blockIdx.x, gridDim.x);
+  copy_items<256, 1>(a, blockIdx.x, gridDim.x);
+}
+
+// It is not: few workgroups with more in flight each.
+__global__ __launch_bounds__(1024) void k_kv_copy_some(CopyArgs a) {
+  copy_items<1024, 4>(a, blockIdx.x, gridDim.x);
 }
 
 // ---------------------------------------------------------------- fork
@@ -163,6 +165,17 @@ __global__ __launch_bounds__(256) void k_kv_fork(ForkArgs a) {
 }
 
 // ---------------------------------------------------------------- ranks of pages
+// lane `i`'s value, of a lane that is the same for the wave
+__device__ __forceinline__ uint64_t lane_value(uint64_t v, int i) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((int)v, i);
+}
+// set bits of the lanes before
+__device__ __forceinline__ int below(uint64_t bits) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32),
+                                   __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
+}
+
 // Inclusive sum over the wave's lanes.
 template <typename T>
 __device__ __forceinline__ T wave_sum(T v) {
@@ -227,7 +240,7 @@ struct GrowArgs {
   int32_t* count;             // copies
   int32_t* from;              // [batch]
   int32_t* to;                // [batch]
-  int32_t* base;              // [batch + 1] pages needed by the rows before
+  int32_t* base;              // [batch] pages needed by the rows before
   int32_t* cow;               // [batch] the shared page that the row writes into, or -1
   int32_t* first;             // [cache pages] first row that writes into a shared page
   int32_t* writers;           // [cache pages] rows that do
@@ -240,99 +253,149 @@ __device__ __forceinline__ int load_agent(const int32_t* p) {
 __device__ __forceinline__ void store_agent(int32_t* p, int v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// what a thread of the workgroup wrote to memory is seen by all after it
-__device__ __forceinline__ void memory_barrier() {
-  __threadfence();
-  __syncthreads();
-}
 
-// The shared page that row r writes into, or -1.
-__device__ __forceinline__ int shared_page(const GrowArgs& a, int r) {
-  const int held = a.held[r], total = a.total[r];
+// The shared page that a row writes into, or -1.
+__device__ __forceinline__ int shared_page(const GrowArgs& a, int r, int held, int total) {
   if (held <= 0 || total <= held || (held & ((1 << a.shift) - 1)) == 0) return -1;
   const int e = held >> a.shift;
   if (e >= a.max_pages) return -1;
   const int p = a.pages[r * a.stride + e];
   return p >= 0 && p < a.cache_pages && a.ref[p] > 1 ? p : -1;
 }
+__device__ __forceinline__ int fresh_pages(const GrowArgs& a, int held, int total) {
+  return max(0, min(pages_of(total, a.shift), a.max_pages) - pages_of(held, a.shift));
+}
 
+// Free pages of a span, a word of 64 in a lane.
+__device__ __forceinline__ uint64_t free_words(const GrowArgs& a, int first, int words) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int p0 = first + (w * words + lane) * 64;
+  uint64_t bits = 0;
+  if (lane < words && p0 < a.cache_pages)
+    bits = a.cache_pages - p0 >= 64 ? ~0ull : (1ull << (a.cache_pages - p0)) - 1;
+  return bits & ~load_words(a.ref, a.cache_pages, first, words);
+}
+
+constexpr int kRows = 64 * kWaves;     // rows that a workgroup takes at once
+constexpr int kSlots = 2 * kRows;      // of their table of shared pages
+constexpr int kList = 4096;            // free pages kept in LDS
+
+// kFew: up to kRows rows, which stay in LDS; else they pass through the workspace.
+template <bool kFew>
 __global__ __launch_bounds__(64 * kWaves) void k_kv_grow(GrowArgs a) {
   __shared__ int tmp[kWaves];
   __shared__ int64_t tmp64[kWaves];
   __shared__ int copies;
+  __shared__ int slot_page[kFew ? kSlots : 1], slot_first[kFew ? kSlots : 1], slot_rows[kFew ? kSlots : 1];
+  __shared__ int row_base[kFew ? kRows : 1], row_held[kFew ? kRows : 1], row_cow[kFew ? kRows : 1];
+  __shared__ int list[kList];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  if (tid == 0) copies = 0;
-  // rows that write into one page: their number and the first of them
-  for (int r = tid; r < a.batch; r += 64 * kWaves) {
-    const int p = shared_page(a, r);
-    a.cow[r] = p;
-    if (p >= 0) {
-      store_agent(a.first + p, INT_MAX);
-      store_agent(a.writers + p, 0);
-    }
-  }
-  memory_barrier();
-  for (int r = tid; r < a.batch; r += 64 * kWaves) {
-    const int p = a.cow[r];
-    if (p >= 0) {
-      atomicMin(a.first + p, r);
-      atomicAdd(a.writers + p, 1);
-    }
-  }
-  memory_barrier();
-  // pages that every row needs; the first writer keeps the page if no other row holds it
   int64_t want = 0;
-  for (int r0 = 0; r0 < a.batch; r0 += 64 * kWaves) {
-    const int r = r0 + tid;
-    int64_t need = 0;               // up to 2^25 a row
-    if (r < a.batch) {
-      need = max(0, min(pages_of(a.total[r], a.shift), a.max_pages) - pages_of(a.held[r], a.shift));
-      const int p = a.cow[r];
+  uint64_t bits = 0;
+  const int words0 = words_of(a.cache_pages);
+  if (tid == 0) copies = 0;
+  // what a row needs; of the rows that write into one shared page, the first keeps it if no other
+  // row holds it
+  if constexpr (kFew) {
+    const bool in = tid < a.batch;
+    const int held = in ? a.held[tid] : 0, total = in ? a.total[tid] : 0;
+    bits = free_words(a, 0, words0);                 // needed later: under way meanwhile
+    for (int i = tid; i < kSlots; i += kRows) {
+      slot_page[i] = -1;
+      slot_first[i] = INT_MAX;
+      slot_rows[i] = 0;
+    }
+    const int p = in ? shared_page(a, tid, held, total) : -1;
+    const int holders = p >= 0 ? a.ref[p] : 0;
+    __syncthreads();
+    int slot = (int)((uint32_t)p * 2654435761u >> 21);
+    if (p >= 0) {
+      for (;; slot = (slot + 1) & (kSlots - 1)) {    // half of the slots stay empty
+        const int was = atomicCAS(slot_page + slot, -1, p);
+        if (was == -1 || was == p) break;
+      }
+      atomicMin(slot_first + slot, tid);
+      atomicAdd(slot_rows + slot, 1);
+    }
+    __syncthreads();
+    const bool keeps = p >= 0 && holders <= slot_rows[slot] && slot_first[slot] == tid;
+    const int cow = keeps ? -1 : p;
+    const int64_t before =
+        group_sum((int64_t)fresh_pages(a, held, total) + (cow >= 0), tmp64, &want);
+    row_base[tid] = (int)min(before, (int64_t)INT_MAX);
+    row_held[tid] = held;
+    row_cow[tid] = cow;
+  } else {
+    for (int r = tid; r < a.batch; r += kRows) {
+      const int p = shared_page(a, r, a.held[r], a.total[r]);
+      a.cow[r] = p;
       if (p >= 0) {
-        if (a.ref[p] <= load_agent(a.writers + p) && load_agent(a.first + p) == r) a.cow[r] = -1;
-        else ++need;
+        store_agent(a.first + p, INT_MAX);
+        store_agent(a.writers + p, 0);
       }
     }
-    int64_t all;
-    const int64_t before = group_sum(need, tmp64, &all);
-    // a sum past the pool's size is capped: what it says is that the pool is short
-    if (r < a.batch) a.base[r] = (int)min(want + before, (int64_t)INT_MAX);
-    want += all;
+    __syncthreads();
+    for (int r = tid; r < a.batch; r += kRows) {
+      const int p = a.cow[r];
+      if (p >= 0) {
+        atomicMin(a.first + p, r);
+        atomicAdd(a.writers + p, 1);
+      }
+    }
+    __syncthreads();
+    for (int r0 = 0; r0 < a.batch; r0 += kRows) {
+      const int r = r0 + tid;
+      int64_t need = 0;               // up to 2^25 a row
+      if (r < a.batch) {
+        need = fresh_pages(a, a.held[r], a.total[r]);
+        const int p = a.cow[r];
+        if (p >= 0) {
+          if (a.ref[p] <= load_agent(a.writers + p) && load_agent(a.first + p) == r) a.cow[r] = -1;
+          else ++need;
+        }
+      }
+      int64_t all;
+      const int64_t before = group_sum(need, tmp64, &all);
+      // a sum past the pool's size is capped: what it says is that the pool is short
+      if (r < a.batch) a.base[r] = (int)min(want + before, (int64_t)INT_MAX);
+      want += all;
+    }
+    bits = free_words(a, 0, words0);
   }
-  if (tid == 0) a.base[a.batch] = (int)min(want, (int64_t)INT_MAX);
   // the first `want` free pages
   int64_t have = 0;
   for (int first = 0; first < a.cache_pages && have < want; first += kSpan) {
     const int words = words_of(a.cache_pages - first);
-    const int p0 = first + (w * words + lane) * 64;        // pages of the lane's word
-    uint64_t bits = 0;
-    if (lane < words && p0 < a.cache_pages)
-      bits = a.cache_pages - p0 >= 64 ? ~0ull : (1ull << (a.cache_pages - p0)) - 1;
-    bits &= ~load_words(a.ref, a.cache_pages, first, words);
+    if (first > 0) bits = free_words(a, first, words);
     int all;
-    int rank = group_sum((int)__popcll(bits), tmp, &all);
+    const int rank = group_sum((int)__popcll(bits), tmp, &all);
     for (int i = 0; i < words; ++i) {
-      const uint64_t b = __shfl(bits, i);
-      const int64_t at = have + __shfl(rank, i);
+      const uint64_t b = lane_value(bits, i);
+      const int64_t at = have + __builtin_amdgcn_readlane(rank, i);
       if (at >= want) break;
-      const int64_t k = at + __popcll(b & ((1ull << lane) - 1));
-      if ((b >> lane & 1) && k < want) a.free_list[k] = first + (w * words + i) * 64 + lane;
+      const int64_t k = at + below(b);
+      if ((b >> lane & 1) && k < want) {
+        const int page = first + (w * words + i) * 64 + lane;
+        if (k < kList) list[k] = page;
+        else a.free_list[k] = page;
+      }
     }
     have += all;
   }
   if (tid == 0) a.short_by[0] = have < want ? (int)min(want - have, (int64_t)INT_MAX) : 0;
-  memory_barrier();
+  __syncthreads();
   if (have >= want) {
-    for (int k = tid; k < want; k += 64 * kWaves) {
+    const int* base = kFew ? row_base : a.base;
+    for (int k = tid; k < want; k += kRows) {
       int lo = 0, hi = a.batch;        // the last row with base <= k
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (a.base[mid] <= k) lo = mid;
+        if (base[mid] <= k) lo = mid;
         else hi = mid;
       }
-      const int page = a.free_list[k];
-      int i = k - a.base[lo];
-      const int held = a.held[lo], old = a.cow[lo];
+      const int page = k < kList ? list[k] : a.free_list[k];
+      int i = k - base[lo];
+      const int held = kFew ? row_held[lo] : a.held[lo], old = kFew ? row_cow[lo] : a.cow[lo];
       if (old >= 0 && i-- == 0) {
         const int c = atomicAdd(&copies, 1);
         a.from[c] = old;
@@ -367,52 +430,66 @@ struct CompactArgs {
 // With U used pages, those at U and above go to the free ones below, in order.
 __global__ __launch_bounds__(64 * kWaves) void k_kv_compact(CompactArgs a) {
   __shared__ int tmp[kWaves];
+  __shared__ int holes, list[kList];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  int used = 0;
+  // a pool of one span: its words and ranks stay in registers
+  const bool one = a.cache_pages <= kSpan;
+  int used = 0, all = 0, rank = 0;
+  uint64_t bits = 0;
   for (int first = 0; first < a.cache_pages; first += kSpan) {
-    int all;
-    group_sum((int)__popcll(load_words(a.ref, a.cache_pages, first,
-                                       words_of(a.cache_pages - first))),
-              tmp, &all);
+    bits = load_words(a.ref, a.cache_pages, first, words_of(a.cache_pages - first));
+    rank = group_sum((int)__popcll(bits), tmp, &all);
     used += all;
   }
-  int below = 0, moves = 0;            // used pages before; pages moved
+  int moves = 0;
   bool passed = false;                 // is `used` behind: moves is known then
-  for (int first = 0; first < a.cache_pages; first += kSpan) {
-    const int words = words_of(a.cache_pages - first);
-    const uint64_t bits = load_words(a.ref, a.cache_pages, first, words);
-    int all;
-    const int rank = below + group_sum((int)__popcll(bits), tmp, &all);
-    if (!passed && used <= first + kSpan) {
-      // free pages below `used`: those before the word that holds it, and in it
-      __shared__ int holes;
-      const int p0 = first + (w * words + lane) * 64;
-      if (tid == 0) holes = used - (below + all);       // `used` at or behind the last word
-      __syncthreads();
-      if (lane < words && p0 <= used && used < p0 + 64)
-        holes = used - (rank + __popcll(bits & ((1ull << (used - p0)) - 1)));
-      __syncthreads();
-      moves = holes;
-      passed = true;
+  // first the holes, then what fills them
+  for (int pass = 0; pass < 2; ++pass) {
+    int below_u = 0;                   // used pages before the span
+    for (int first = 0; first < a.cache_pages; first += kSpan) {
+      const int words = words_of(a.cache_pages - first);
+      if (!one) {
+        bits = load_words(a.ref, a.cache_pages, first, words);
+        rank = below_u + group_sum((int)__popcll(bits), tmp, &all);
+      }
+      if (!passed && used <= first + kSpan) {
+        // free pages below `used`: those before the word that holds it, and in it
+        const int p0 = first + (w * words + lane) * 64;
+        if (tid == 0) holes = used - (below_u + all);     // `used` at or behind the last word
+        __syncthreads();
+        if (lane < words && p0 <= used && used < p0 + 64)
+          holes = used - (rank + (int)__popcll(bits & ((1ull << (used - p0)) - 1)));
+        __syncthreads();
+        moves = holes;
+        passed = true;
+      }
+      for (int i = 0; i < words; ++i) {
+        const uint64_t b = lane_value(bits, i);
+        const int p = first + (w * words + i) * 64 + lane;
+        const int before = __builtin_amdgcn_readlane(rank, i) + below(b);
+        if (p >= a.cache_pages) continue;
+        const bool in = b >> lane & 1;
+        if (pass == 0) {
+          if (p < used && !in) {
+            const int k = p - before;
+            if (k < kList) list[k] = p;
+            a.to[k] = p;
+          }
+        } else {
+          int to = in ? p : -1;
+          if (p >= used && in) {
+            const int k = before - (used - moves);
+            to = k < kList ? list[k] : a.to[k];
+            a.from[k] = p;
+            a.ref[to] = a.ref[p];
+            a.ref[p] = 0;
+          }
+          a.where[p] = to;
+        }
+      }
+      below_u += all;
     }
-    for (int i = 0; i < words; ++i) {
-      const uint64_t b = __shfl(bits, i);
-      const int before = __shfl(rank, i) + __popcll(b & ((1ull << lane) - 1));
-      const int p = first + (w * words + i) * 64 + lane;
-      if (p >= a.cache_pages) continue;
-      const bool in = b >> lane & 1;
-      a.where[p] = in ? p : -1;
-      if (p < used && !in) a.to[p - before] = p;
-      if (p >= used && in) a.from[before - (used - moves)] = p;
-    }
-    below += all;
-  }
-  memory_barrier();
-  for (int i = tid; i < moves; i += 64 * kWaves) {
-    const int from = a.from[i], to = a.to[i];
-    a.where[from] = to;
-    a.ref[to] = a.ref[from];
-    a.ref[from] = 0;
+    __syncthreads();
   }
   if (tid == 0) {
     a.used[0] = used;
@@ -421,19 +498,18 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv_compact(CompactArgs a) {
 }
 
 // The first `blocks` workgroups copy, the others rewrite the tables: a row, 1024 entries each.
-__global__ __launch_bounds__(256) void k_kv_move(CopyArgs c, CompactArgs a, int blocks,
+__global__ __launch_bounds__(1024) void k_kv_move(CopyArgs c, CompactArgs a, int blocks,
                                                  int spans) {
   if ((int)blockIdx.x < blocks) {
-    copy_items(c, blockIdx.x, blocks);
+    copy_items<1024, 4>(c, blockIdx.x, blocks);
     return;
   }
   const int item = (int)blockIdx.x - blocks, row = item / spans;
   const int e0 = (item - row * spans) * 1024;
   const int n = min(pages_of(a.total[row], a.shift), a.max_pages);
-  for (int e = e0 + threadIdx.x; e < min(n, e0 + 1024); e += 256) {
+  if (const int e = e0 + threadIdx.x; e < n) {
     const int p = a.pages[(int64_t)row * a.stride + e];
-    if (p < 0 || p >= a.cache_pages) continue;
-    const int to = a.where[p];
+    const int to = p >= 0 && p < a.cache_pages ? a.where[p] : -1;
     if (to >= 0 && to != p) a.pages[(int64_t)row * a.stride + e] = to;
   }
 }
@@ -449,11 +525,11 @@ void set_copy(const gmm_kv_cache* src, const gmm_kv_cache* dst, CopyArgs* a) {
   a->bytes = dst->heads * dst->page * dst->d * 2;
   a->box_bytes = dst->heads * 2 * dst->d;
   a->heads = dst->heads;
-  a->parts = (int)cdiv(a->bytes, kPart);
 }
 
-int64_t copy_blocks(const CopyArgs& a, int64_t pairs) {
-  const int64_t items = pairs * 2 * a.parts, most = 16 * kCUs;
+// workgroups of a copy of up to `pairs` pages in items of `part` bytes
+int64_t copy_blocks(const CopyArgs& a, int64_t pairs, int part, int64_t most) {
+  const int64_t items = pairs * (2 * cdiv(a.bytes, part) + 1);
   return items < most ? items : most;
 }
 
@@ -499,7 +575,7 @@ int gmm_kv_copy(const gmm_kv_cache* src, const gmm_kv_cache* dst, const int32_t*
   a.from = src_pages;
   a.to = dst_pages;
   a.n = (int)n;
-  hipLaunchKernelGGL(k_kv_copy, dim3((unsigned)copy_blocks(a, n)), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(k_kv_copy, dim3((unsigned)copy_blocks(a, n, 4096, 1 << 20)), dim3(256), 0, stream, a);
   return launch_status();
 }
 
@@ -584,17 +660,19 @@ int gmm_kv_grow(const gmm_kv_cache* cache, int32_t* ref, const int32_t* held,
   a.from = a.count + 64;
   a.to = a.from + batch;
   a.base = a.to + batch;
-  a.cow = a.base + batch + 1;
+  a.cow = a.base + batch;
   a.first = a.cow + batch;
   a.writers = a.first + cache->pages;
   a.free_list = a.writers + cache->pages;
-  hipLaunchKernelGGL(k_kv_grow, dim3(1), dim3(64 * kWaves), 0, stream, a);
+  if (batch <= kRows) hipLaunchKernelGGL(k_kv_grow<true>, dim3(1), dim3(kRows), 0, stream, a);
+  else hipLaunchKernelGGL(k_kv_grow<false>, dim3(1), dim3(kRows), 0, stream, a);
   CopyArgs c{};
   set_copy(cache, cache, &c);
   c.from = a.from;
   c.to = a.to;
   c.count = a.count;
-  hipLaunchKernelGGL(k_kv_copy, dim3((unsigned)copy_blocks(c, batch)), dim3(256), 0, stream, c);
+  hipLaunchKernelGGL(k_kv_copy_some, dim3((unsigned)copy_blocks(c, batch, 65536, 8 * kCUs)),
+                     dim3(1024), 0, stream, c);
   return launch_status();
 }
 
@@ -629,9 +707,9 @@ int gmm_kv_compact(const gmm_kv_cache* cache, int32_t* ref, const int32_t* total
   c.to = a.to;
   c.count = a.count;
   const int spans = (int)cdiv(max_pages, 1024);
-  const int64_t blocks = copy_blocks(c, cdiv(cache->pages, 2));
-  if (blocks + (int64_t)batch * spans > kMaxBlocks) return GMM_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL(k_kv_move, dim3((unsigned)(blocks + (int64_t)batch * spans)), dim3(256), 0,
+  const int64_t blocks = copy_blocks(c, cdiv(cache->pages, 2), 65536, 8 * kCUs);
+  if (blocks + (int64_t)batch * spans > kMaxBlocks / 4) return GMM_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL(k_kv_move, dim3((unsigned)(blocks + (int64_t)batch * spans)), dim3(1024), 0,
                      stream, c, a, (int)blocks, spans);
   return launch_status();
 }

@@ -31,57 +31,71 @@ SIGNATURES = {
 }
 
 
+_FN = {}
+
+
 def bind(lib):
     """Sets the entry points' argument and result types."""
     for name, args in SIGNATURES.items():
         fn = getattr(lib, name)
         fn.argtypes = args
         fn.restype = ctypes.c_size_t if name.endswith("_bytes") else ctypes.c_int
+        _FN[name] = fn
 
 
-def _call(name, device, *args):
-    """Calls an entry point with `device` as the current one."""
-    fn = getattr(_base.load_library(), name)
-    if device.index == torch._C._cuda_getDevice():
-        rc = fn(*args)
+# A decoding step's bookkeeping takes a few microseconds on the GPU: the checks look at each tensor
+# once, and only a tensor that fails is looked at for what is wrong.
+
+def _call(name, dev, *args):
+    """Calls an entry point with device `dev` as the current one."""
+    if not _FN:
+        _base.load_library()
+    if dev == torch._C._cuda_getDevice():
+        rc = _FN[name](*args)
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args)
+        with torch.cuda.device(dev):
+            rc = _FN[name](*args)
     if rc:
         raise _base.GMMError(name, rc)
 
 
-def _flat(t, dtype, numel, name, device):
-    """Address of a contiguous CUDA tensor of `numel` elements or more on `device`."""
+def _wrong(t, dtype, numel, name, dev):
+    """The error of a tensor that is not a contiguous `dtype` one on device `dev`."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.is_contiguous()):
-        raise TypeError(f"{name} must be a contiguous {dtype} CUDA tensor")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the call's other tensors on {device}")
-    if t.numel() < numel:
-        raise ValueError(f"{name} holds {t.numel()} elements, {numel} needed")
-    return t.data_ptr()
+        return TypeError(f"{name} must be a contiguous {dtype} CUDA tensor")
+    if t.get_device() != dev:
+        return ValueError(f"{name} is on {t.device}, the call's other tensors on cuda:{dev}")
+    return ValueError(f"{name} holds {t.numel()} elements, {numel} needed")
 
 
-def _table(total, pages, device, names=("total", "pages")):
+def _flat(t, dtype, numel, name, dev):
+    """Address of a contiguous CUDA tensor of `numel` elements or more on device `dev`."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous() and \
+            t.get_device() == dev and t.numel() >= numel:
+        return t.data_ptr()
+    raise _wrong(t, dtype, numel, name, dev)
+
+
+def _table(total, pages, dev, names=("total", "pages")):
     """(total, pages, rows, max_pages, stride) of a table."""
     if not (isinstance(pages, torch.Tensor) and pages.is_cuda and pages.dtype is torch.int32 and
-            pages.dim() == 2 and (pages.stride(1) == 1 or pages.shape[1] == 1)):
-        raise TypeError(f"{names[1]} must be an int32 CUDA tensor [rows, max_pages] with "
-                        "contiguous rows")
-    if pages.device != device:
-        raise ValueError(f"{names[1]} is on {pages.device}, the call's other tensors on {device}")
-    rows, width = pages.shape
-    at = _flat(total, torch.int32, rows, names[0], device)
+            pages.dim() == 2):
+        raise TypeError(f"{names[1]} must be an int32 CUDA tensor [rows, max_pages]")
+    (rows, width), (stride, inner) = pages.shape, pages.stride()
+    if inner != 1 and width > 1:
+        raise TypeError(f"{names[1]} must have contiguous rows")
+    if pages.get_device() != dev:
+        raise ValueError(f"{names[1]} is on {pages.device}, the call's other tensors on cuda:{dev}")
+    at = _flat(total, torch.int32, rows, names[0], dev)
     if total.numel() != rows:
         raise ValueError(f"{names[1]} has {rows} rows for {total.numel()} in {names[0]}")
-    return at, pages.data_ptr(), rows, width, max(pages.stride(0), width) if rows < 2 else \
-        pages.stride(0)
+    return at, pages.data_ptr(), rows, width, stride if rows > 1 else max(stride, width)
 
 
-def _ws(ws, device):
+def _ws(ws, dev):
     at, size = _base._ws(ws)
-    if ws is not None and ws.device != device:
-        raise ValueError(f"ws is on {ws.device}, the call's other tensors on {device}")
+    if ws is not None and ws.get_device() != dev:
+        raise ValueError(f"ws is on {ws.device}, the call's other tensors on cuda:{dev}")
     return at, size
 
 
@@ -106,9 +120,9 @@ def kv_pool_workspace(cache, rows):
 def gmm_kv_copy(src, dst, src_pages, dst_pages, stream=None):
     """Copies pages src_pages [n] int32 of the cache src to pages dst_pages [n] of the cache dst
     (which may be src): keys, values and boxes."""
-    dev, n = src.k.device, src_pages.numel()
-    if dst.k.device != dev:
-        raise ValueError(f"dst is on {dst.k.device}, src on {dev}")
+    dev, n = src.k.get_device(), src_pages.numel()
+    if dst.k.get_device() != dev:
+        raise ValueError(f"dst is on {dst.k.device}, src on {src.k.device}")
     if dst_pages.numel() != n:
         raise ValueError(f"{n} source pages, {dst_pages.numel()} destinations")
     _call("gmm_kv_copy", dev, src._ref, dst._ref, _flat(src_pages, torch.int32, n, "src_pages", dev),
@@ -120,7 +134,7 @@ def gmm_kv_fork(cache, ref, total, pages, parent, total_out, pages_out, keep=Non
     """New rows total_out [rows], pages_out [rows, >= max_pages] with the pages of the rows
     parent [rows] of (total, pages), of their first keep [rows] keys if given.  release: the old
     rows are given up, and pages that nobody names any more are free."""
-    dev, rows = cache.k.device, parent.numel()
+    dev, rows = cache.k.get_device(), parent.numel()
     new = _table(total_out, pages_out, dev, ("total_out", "pages_out"))
     if new[2] != rows:
         raise ValueError(f"pages_out has {new[2]} rows for {rows} parents")
@@ -134,7 +148,7 @@ def gmm_kv_grow(cache, ref, held, total, pages, short_by, ws, stream=None):
     """Gives the rows of `pages` [rows, max_pages] pages for growing from held [rows] to total
     [rows] keys, copies of shared pages that they write into among them; short_by [1] int32: how
     many pages are missing (then nothing changes), or 0."""
-    dev = cache.k.device
+    dev = cache.k.get_device()
     tb = _table(total, pages, dev)
     _call("gmm_kv_grow", dev, cache._ref, _flat(ref, torch.int32, cache.pages, "ref", dev),
           _flat(held, torch.int32, tb[2], "held", dev), *tb,
@@ -144,7 +158,7 @@ def gmm_kv_grow(cache, ref, held, total, pages, short_by, ws, stream=None):
 def gmm_kv_compact(cache, ref, total, pages, where, used, ws, stream=None):
     """Moves the used pages to the numbers below their count used [1] int32, rewrites the tables,
     and says in where [cache pages] int32 where every page's contents are now (-1: it was free)."""
-    dev = cache.k.device
+    dev = cache.k.get_device()
     _call("gmm_kv_compact", dev, cache._ref, _flat(ref, torch.int32, cache.pages, "ref", dev),
           *_table(total, pages, dev), _flat(where, torch.int32, cache.pages, "where", dev),
           _flat(used, torch.int32, 1, "used", dev), *_ws(ws, dev), _stream(stream, pages))
@@ -174,7 +188,7 @@ def gmm_beam_select(logits, score, out_score, out_parent, out_token, ws, done=No
     if not (isinstance(logits, torch.Tensor) and logits.is_cuda and logits.dim() == 3):
         raise TypeError("logits must be a CUDA tensor [batch, beams, vocab]")
     batch, beams, vocab = logits.shape
-    dev, rows = logits.device, batch * beams
+    dev, rows = logits.get_device(), batch * beams
     s0, s1, s2 = logits.stride()
     if s2 != 1 and vocab > 1 and rows:
         raise TypeError("logits must have contiguous rows")
