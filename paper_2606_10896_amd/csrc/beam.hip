@@ -26,6 +26,7 @@ namespace {
 using namespace kv;
 
 constexpr double kLog2eD = 1.4426950408889634;
+constexpr double kLn2D = 0.6931471805599453;
 constexpr int kRun = 2048;        // words of a run
 constexpr int kJoinWaves = 8;     // waves of a sequence's workgroup
 
@@ -39,8 +40,7 @@ struct BeamArgs {
   int64_t mask_stride;
   double scale;
   float c;                    // scale log2(e)
-  int beams, vocab, runs, m, eos;
-  int64_t rows;
+  int beams, vocab, runs, m, eos, rows;
   float2* part;               // [rows, runs]: maximum, sum
   float* out_score;
   int32_t* out_parent;
@@ -114,6 +114,10 @@ __device__ __forceinline__ int lanes_sum(int v) {
   v += (int)__builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
   return v;
 }
+// the lane's bit
+__device__ __forceinline__ int from_mask(uint64_t mask) {
+  return (int)(mask >> (threadIdx.x & 63) & 1);
+}
 // set bits of the lanes before
 __device__ __forceinline__ int below(uint64_t bits) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32),
@@ -132,25 +136,32 @@ struct Words {
   __device__ __forceinline__ static int at(int run, int step) {
     return run * kRun + (step * 64 + (int)(threadIdx.x & 63)) * N;
   }
-  // a run's words; all loads are issued before any is waited for
-  __device__ __forceinline__ static void load(const BeamArgs& a, const T* x, const uint32_t* mask,
-                                              int run, V* v) {
-    uint32_t bits[kSteps];
+  V v[kSteps];
+  uint32_t bits[kSteps];
+
+  // Issues the loads of a run.
+  __device__ __forceinline__ void fetch(const BeamArgs& a, const T* x, const uint32_t* mask, int run) {
     if (mask) {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) bits[i] = mask[min(at(run, i), a.vocab - 1) >> 5];
     }
+    if ((run + 1) * kRun <= a.vocab) {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const int p = at(run, i);
-      if (p + N <= a.vocab) {
-        v[i] = *reinterpret_cast<const Unaligned*>(x + p);
-      } else {
+      for (int i = 0; i < kSteps; ++i)
+        v[i] = __builtin_nontemporal_load(reinterpret_cast<const Unaligned*>(x + at(run, i)));
+    } else {
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        const int p = at(run, i);
 #pragma unroll
         for (int e = 0; e < N; ++e) v[i][e] = (T)-INFINITY;
+        if (p + N <= a.vocab) v[i] = *reinterpret_cast<const Unaligned*>(x + p);
       }
     }
-    const int last = a.vocab & -N;                      // the words of an incomplete vector
+  }
+  // The words of an incomplete vector, and those that are forbidden.
+  __device__ __forceinline__ void finish(const BeamArgs& a, const T* x, const uint32_t* mask, int run) {
+    const int last = a.vocab & -N;
     if (last < a.vocab && last / kRun == run) {
       V t;
 #pragma unroll
@@ -173,42 +184,57 @@ struct Words {
 };
 
 template <typename T>
-__device__ __forceinline__ const T* row_of(const BeamArgs& a, int64_t row) {
-  const int64_t b = row / a.beams;
+__device__ __forceinline__ const T* row_of(const BeamArgs& a, int row) {
+  const int b = (uint32_t)row / (uint32_t)a.beams;
   return (const T*)a.x + b * a.seq_stride + (row - b * a.beams) * a.beam_stride;
 }
-__device__ __forceinline__ const uint32_t* mask_of(const BeamArgs& a, int64_t row) {
+__device__ __forceinline__ const uint32_t* mask_of(const BeamArgs& a, int row) {
   return a.mask ? a.mask + row * a.mask_stride : nullptr;
+}
+
+// The power of 2 to which a run's sum is relative, by its largest logit: its exponent, rounded to a
+// whole number, so that joining runs does not round.  Past 2^123 (`large`) the logit itself, as there
+// every other logit's weight is 0.
+__device__ __forceinline__ bool large(const BeamArgs& a, float x) { return !(fabsf(x * a.c) < 1e37f); }
+__device__ __forceinline__ double unit_of(const BeamArgs& a, float x) {
+  return large(a, x) ? (double)x * (double)a.c : (double)rintf(x * a.c);
 }
 
 // A wave a run: its maximum and sum of exponentials.  A NaN or +infinity makes the sum NaN.
 template <typename T>
 __global__ __launch_bounds__(256) void k_beam_run(BeamArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t row = item / a.runs;
+  const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  const int row = (uint32_t)item / (uint32_t)a.runs, run = item - row * a.runs;
   if (row >= a.rows) return;
-  if (!finite(a.score[row]) || (a.done && a.done[row])) return;
-  constexpr int N = Words<T>::N, L = Words<T>::kSteps;
-  const int run = (int)(item - row * a.runs);
-  typename Words<T>::V v[L];
-  Words<T>::load(a, row_of<T>(a, row), mask_of(a, row), run, v);
+  const float score = a.score[row];
+  const int done = a.done ? a.done[row] : 0;       // both loads together
+  if (!finite(score) | (done != 0)) return;
+  typedef Words<T> W;
+  const T* x = row_of<T>(a, row);
+  const uint32_t* mask = mask_of(a, row);
+  W words;
+  words.fetch(a, x, mask, run);
+  words.finish(a, x, mask, run);
   float mx = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < L; ++i)
+  for (int i = 0; i < W::kSteps; ++i)
 #pragma unroll
-    for (int e = 0; e < N; ++e) mx = fmaxf(mx, (float)v[i][e]);
+    for (int e = 0; e < W::N; ++e) mx = fmaxf(mx, (float)words.v[i][e]);
   mx = wave_max(mx);
-  const float base = mx > -INFINITY ? mx : 0.f;
-  // the difference before the product: its rounding, not that of a large maximum's product
+  // exponents by one multiply-add, whose product is not rounded; 2^-64 is any factor that leaves
+  // the product exact
+  const bool far = large(a, mx);
+  const float c = far ? 0x1p-64f : a.c;
+  const float unit = !(mx > -INFINITY) ? 0.f : far ? mx * 0x1p-64f : rintf(mx * a.c);
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < L; ++i)
+  for (int i = 0; i < W::kSteps; ++i)
 #pragma unroll
-    for (int e = 0; e < N; ++e) sum[e & 3] += __builtin_amdgcn_exp2f(((float)v[i][e] - base) * a.c);
-  float z = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-  z = wave_sum(z);
-  if (lane == 0) a.part[item] = make_float2(mx, z);
+    for (int e = 0; e < W::N; ++e)
+      sum[e & 3] += __builtin_amdgcn_exp2f(fmaf((float)words.v[i][e], c, -unit));
+  const float z = wave_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+  if (lane == 0) a.part[(int64_t)row * a.runs + run] = make_float2(mx, z);
 }
 
 // ---------------------------------------------------------------- the best of many
@@ -283,17 +309,37 @@ __device__ __forceinline__ Picked pick(const uint64_t* v, int m) {
   return Picked{t, m - reach(t + 1), m};
 }
 
-// The place of a lane's number among the first n lanes': how many are larger, or equal and before.
-__device__ __forceinline__ int place_of(uint64_t v, int n) {
+// How many of a list of 64 numbers in LDS, of which v is number `lane`, are in front of it: larger, or
+// equal and before.  Every lane reads the same addresses, eight numbers a step; those from n on
+// are 0.
+__device__ __forceinline__ int place_of(const uint64_t* list, uint64_t v, int n) {
+  typedef uint64_t Two __attribute__((ext_vector_type(2)));
   int place = 0;
-  for (int i = 0; i < n; i += 4) {
+  for (int i = 0; i < n; i += 8) {
+    Two t[4];
 #pragma unroll
-    for (int k = i; k < i + 4; ++k) {                // past n: lanes of 0
-      const uint64_t other = lane_value(v, k);
-      place += other > v || (other == v && k < (int)(threadIdx.x & 63));
+    for (int k = 0; k < 4; ++k) t[k] = *reinterpret_cast<const Two*>(list + i + 2 * k);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint64_t u = t[k / 2][k % 2];
+      place += from_mask(__ballot(u > v) | (__ballot(u >= v) & ~1ull << (i + k)));
     }
   }
   return place;
+}
+// How many of a list of 64 numbers below 2^31 are larger than v; those from n on are 0.  (By the sign of
+// a difference: a comparison's result would pass through scalar registers, with a wait for each.)
+__device__ __forceinline__ int larger_than(const uint32_t* list, uint32_t v, int n) {
+  typedef uint32_t Four __attribute__((ext_vector_type(4)));
+  int count = 0;
+  for (int i = 0; i < n; i += 16) {
+    Four t[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) t[k] = *reinterpret_cast<const Four*>(list + i + 4 * k);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) count += (v - t[k / 4][k % 4]) >> 31;
+  }
+  return count;
 }
 
 // Is v among what was picked?  `seen`: numbers equal to `least` in the steps before.
@@ -323,7 +369,7 @@ struct Join {
   int kind[GMM_BEAM_MAX];              // 0: no candidate, 1: live, 2: finished
   uint32_t hi[64 * kLane], lo[64 * kLane];   // scores of the best runs so far, then of a chunk
   int run[64];                         // the best runs, in order
-  uint64_t list[64];                   // few runs while they are picked from
+  alignas(16) uint64_t list[64];       // few numbers while they are picked from
   int list_run[64];
   uint64_t least;
   int kept;
@@ -369,18 +415,18 @@ __device__ __forceinline__ void put_run(Join& s, int i, uint64_t key) {
 }
 
 // log Z of up to two beams of a wave, j and j + kJoinWaves: their loads go together
-__device__ __forceinline__ void join_beams(const BeamArgs& a, Join& s, int64_t row0, int j0) {
+__device__ __forceinline__ void join_beams(const BeamArgs& a, Join& s, int row0, int j0) {
   const int lane = threadIdx.x & 63;
   float sc[2], wt[2];
   int fin[2];
   float2 v[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int64_t row = row0 + min(j0 + i * kJoinWaves, a.beams - 1);
+    const int row = row0 + min(j0 + i * kJoinWaves, a.beams - 1);
     sc[i] = a.score[row];
     wt[i] = a.weight ? a.weight[row] : 1.f;
     fin[i] = a.done ? a.done[row] : 0;
-    v[i] = a.part[row * a.runs + min(lane, a.runs - 1)];
+    v[i] = a.part[(int64_t)row * a.runs + min(lane, a.runs - 1)];
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -390,19 +436,20 @@ __device__ __forceinline__ void join_beams(const BeamArgs& a, Join& s, int64_t r
     double logz = 0.0;
     float mx = -INFINITY;
     if (kind == 1) {
-      const float2* p = a.part + (row0 + j) * a.runs;
+      const float2* p = a.part + (int64_t)(row0 + j) * a.runs;
       float2 u = v[i];
       if (lane < a.runs) mx = u.x;
       for (int r = lane + 64; r < a.runs; r += 64) mx = fmaxf(mx, p[r].x);
       mx = wave_max(mx);
       double z = 0.0;
+      const double unit = unit_of(a, mx);
       for (int r = lane; r < a.runs; r += 64) {
         if (r >= 64) u = p[r];
         // a run without a word adds its sum, 0, or NaN
-        z += (double)(u.y * (u.x > -INFINITY ? __builtin_amdgcn_exp2f((u.x - mx) * a.c) : 1.f));
+        z += ldexp((double)u.y, u.x > -INFINITY ? (int)fmax(unit_of(a, u.x) - unit, -2000.0) : 0);
       }
       z = wave_sum(z);
-      logz = log(z);
+      logz = log(z) + (large(a, mx) ? 0.0 : (unit - (double)a.c * (double)mx) * kLn2D);
       if (!finite(mx) || !(z > 0.0)) kind = 0;       // no word, NaN or +infinity
     }
     if (lane == 0) {
@@ -430,23 +477,22 @@ __device__ __forceinline__ uint32_t taken(uint32_t more, uint32_t same, int ties
 // leaves few.
 __device__ __forceinline__ void pick_runs(const BeamArgs& a, Join& s, int base, int kept, int n) {
   const int lane = threadIdx.x & 63;
-  const int per = (n + 63) / 64 | 1, first = lane * per;
+  // as many of a lane as leave 6 m lanes: a lane's maximum is cheaper than its place
+  const int per = max((n + 63) / 64, min(kLane, n / (6 * a.m))) | 1, first = lane * per;
   const auto has = [&](int c) { return c < per && first + c < n; };
   uint32_t h[kLane], top = 0, more = 0, same = 0;
 #pragma unroll
+  for (int c = 0; c < kLane; ++c) h[c] = s.hi[min(first, 63 * kLane) + c];
+#pragma unroll
   for (int c = 0; c < kLane; ++c) {
-    h[c] = has(c) ? s.hi[first + c] : 0;
+    h[c] = has(c) ? h[c] : 0;
     top = max(top, h[c]);
   }
   // the m-th largest: the smallest of those that fewer than m are larger than
-  const int lanes = (n + per - 1) / per;
-  int larger = 0;
-  for (int i = 0; i < lanes; i += 4) {
-#pragma unroll
-    for (int k = i; k < i + 4; ++k)
-      larger += (uint32_t)__builtin_amdgcn_readlane((int)top, k) > top;
-  }
-  uint32_t least = ~wave_max(larger < a.m ? ~top : 0u);
+  uint32_t* tops = reinterpret_cast<uint32_t*>(s.list);
+  tops[lane] = top >> 1;
+  const int larger = larger_than(tops, top >> 1, (n + per - 1) / per);
+  uint32_t least = ~wave_max(larger < a.m ? ~(top & ~1u) : 0u);
   least = max(least, 1u);              // a number is not 0 in its upper half
 #pragma unroll
   for (int c = 0; c < kLane; ++c) more |= (uint32_t)(h[c] >= least) << c;
@@ -472,7 +518,8 @@ __device__ __forceinline__ void pick_runs(const BeamArgs& a, Join& s, int base, 
     s.list_run[at++] = i < kept ? s.run[i] : base + i - kept;
   }
   const uint64_t key = lane < all ? s.list[lane] : 0;
-  const int run = s.list_run[lane], place = place_of(key, all);
+  s.list[lane] = key;
+  const int run = s.list_run[lane], place = place_of(s.list, key, all);
   const bool in = lane < all && place < a.m;
   const uint64_t bal = __ballot(in), last = __ballot(in && place == a.m - 1);
   if (in) {
@@ -490,11 +537,11 @@ __device__ __forceinline__ void pick_runs(const BeamArgs& a, Join& s, int base, 
 
 // The m best runs of the sequence, in order, into s.run, their scores into s.hi / s.lo, their number
 // into s.kept, and the m-th one's score into s.least.
-__device__ __forceinline__ void best_runs(const BeamArgs& a, Join& s, int64_t row0) {
+__device__ __forceinline__ void best_runs(const BeamArgs& a, Join& s, int row0) {
   const int tid = threadIdx.x;
   const int runs = a.beams * a.runs;
   const float inv = 1.f / (float)a.runs;
-  const float2* part = a.part + row0 * a.runs;
+  const float2* part = a.part + (int64_t)row0 * a.runs;
   int kept = 0;
   uint64_t least = 1;
   for (int base = 0; base < runs; base += kChunk) {
@@ -548,7 +595,7 @@ template <typename T>
 __global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(BeamArgs a) {
   __shared__ Join s;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t row0 = (int64_t)blockIdx.x * a.beams;
+  const int row0 = blockIdx.x * a.beams;
   for (int j = w; j < a.beams; j += 2 * kJoinWaves) join_beams(a, s, row0, j);
   __syncthreads();
   best_runs(a, s, row0);
@@ -563,19 +610,21 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(BeamArgs a) {
   for (int q = w * s.kept / kJoinWaves; q < q1; ++q) {
     const int gid = __builtin_amdgcn_readfirstlane(s.run[q]);
     const int j = gid / a.runs, r = gid - j * a.runs;
-    typename W::V v[W::kSteps];
+    W words;
     uint32_t steps = 0;                      // with words that may count
     float least = -INFINITY;
     if (s.kind[j] == 2) {
       steps = 1;
     } else {
-      W::load(a, row_of<T>(a, row0 + j), mask_of(a, row0 + j), r, v);
+      const T* x = row_of<T>(a, row0 + j);
+      words.fetch(a, x, mask_of(a, row0 + j), r);
+      words.finish(a, x, mask_of(a, row0 + j), r);
       least = logit_of(a, s, j, floor);
 #pragma unroll
       for (int i = 0; i < W::kSteps; ++i) {
-        float mx = (float)v[i][0];
+        float mx = (float)words.v[i][0];
 #pragma unroll
-        for (int e = 1; e < W::N; ++e) mx = fmaxf(mx, (float)v[i][e]);
+        for (int e = 1; e < W::N; ++e) mx = fmaxf(mx, (float)words.v[i][e]);
         if (__ballot(mx >= least)) steps |= 1u << i;
       }
     }
@@ -587,10 +636,10 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(BeamArgs a) {
           buf[held] = Word{(uint64_t)s.hi[q] << 32 | s.lo[q], (uint32_t)j * a.vocab + a.eos, s.score[j]};
         ++held;
       } else {
-        typename W::V x = v[0];
+        typename W::V x = words.v[0];
 #pragma unroll
         for (int c = 1; c < W::kSteps; ++c)
-          if (c == i) x = v[c];
+          if (c == i) x = words.v[c];
         // in the order of the words: those of the lanes before, and of this one.  What passes
         // for its logit but has not the score is held as none.
         int at = held, n = 0;
@@ -654,7 +703,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(BeamArgs a) {
     total = p.count;
     if (lane < total) e = s.word[0][lane];
   }
-  const int place = place_of(e.key, total), found = __popcll(__ballot(e.key != 0));
+  s.list[lane] = e.key;
+  const int place = place_of(s.list, e.key, total), found = __popcll(__ballot(e.key != 0));
   const int64_t o = (int64_t)blockIdx.x * a.m;
   if (e.key != 0 && place < a.m) {
     const int j = (int)(e.at / (uint32_t)a.vocab), word = (int)(e.at - (uint32_t)j * a.vocab);
@@ -685,8 +735,8 @@ int64_t need(int32_t batch, int32_t beams, int32_t vocab) {
 
 template <typename T>
 int launch(const BeamArgs& a, int batch, hipStream_t st) {
-  hipLaunchKernelGGL((k_beam_run<T>), dim3((unsigned)cdiv(a.rows * a.runs, 4)), dim3(256), 0, st,
-                     a);
+  hipLaunchKernelGGL((k_beam_run<T>), dim3((unsigned)cdiv((int64_t)a.rows * a.runs, 4)), dim3(256),
+                     0, st, a);
   hipLaunchKernelGGL((k_beam_join<T>), dim3((unsigned)batch), dim3(64 * kJoinWaves), 0, st, a);
   return launch_status();
 }
@@ -734,7 +784,7 @@ int gmm_beam_select(const void* logits, int32_t dtype, int64_t seq_stride, int64
   a.runs = (int)cdiv(vocab, kRun);
   a.m = m;
   a.eos = eos;
-  a.rows = (int64_t)batch * beams;
+  a.rows = batch * beams;
   a.part = (float2*)ws;
   a.out_score = out_score;
   a.out_parent = out_parent;
