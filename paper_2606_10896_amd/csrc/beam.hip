@@ -114,6 +114,11 @@ __device__ __forceinline__ int lanes_sum(int v) {
   v += (int)__builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
   return v;
 }
+// What lanes of the wave wrote to LDS is read by others after it: in order, without a barrier.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 // the lane's bit
 __device__ __forceinline__ int from_mask(uint64_t mask) {
   return (int)(mask >> (threadIdx.x & 63) & 1);
@@ -491,7 +496,9 @@ __device__ __forceinline__ void pick_runs(const BeamArgs& a, Join& s, int base, 
   // the m-th largest: the smallest of those that fewer than m are larger than
   uint32_t* tops = reinterpret_cast<uint32_t*>(s.list);
   tops[lane] = top >> 1;
+  wave_sync();
   const int larger = larger_than(tops, top >> 1, (n + per - 1) / per);
+  wave_sync();
   uint32_t least = ~wave_max(larger < a.m ? ~(top & ~1u) : 0u);
   least = max(least, 1u);              // a number is not 0 in its upper half
 #pragma unroll
@@ -517,8 +524,10 @@ __device__ __forceinline__ void pick_runs(const BeamArgs& a, Join& s, int base, 
     s.list[at] = (uint64_t)s.hi[i] << 32 | s.lo[i];
     s.list_run[at++] = i < kept ? s.run[i] : base + i - kept;
   }
+  wave_sync();
   const uint64_t key = lane < all ? s.list[lane] : 0;
   s.list[lane] = key;
+  wave_sync();
   const int run = s.list_run[lane], place = place_of(s.list, key, all);
   const bool in = lane < all && place < a.m;
   const uint64_t bal = __ballot(in), last = __ballot(in && place == a.m - 1);
@@ -568,6 +577,7 @@ __device__ __forceinline__ void best_runs(const BeamArgs& a, Join& s, int row0) 
 __device__ __forceinline__ Picked keep_words(Word* buf, int n, int m) {
   constexpr int C = kBuffer / 64;
   const int lane = threadIdx.x & 63;
+  wave_sync();
   uint64_t v[C];
   Word e[C];
 #pragma unroll
@@ -587,6 +597,7 @@ __device__ __forceinline__ Picked keep_words(Word* buf, int n, int m) {
     if (in) buf[k + below(bal)] = e[c];
     k += __popcll(bal);
   }
+  wave_sync();
   return p;
 }
 
@@ -701,9 +712,11 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(BeamArgs a) {
       k += __popcll(bal);
     }
     total = p.count;
+    wave_sync();
     if (lane < total) e = s.word[0][lane];
   }
   s.list[lane] = e.key;
+  wave_sync();
   const int place = place_of(s.list, e.key, total), found = __popcll(__ballot(e.key != 0));
   const int64_t o = (int64_t)blockIdx.x * a.m;
   if (e.key != 0 && place < a.m) {
@@ -725,7 +738,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(BeamArgs a) {
 // ---------------------------------------------------------------- host
 bool shape_ok(int32_t batch, int32_t beams, int32_t vocab) {
   return beams <= GMM_BEAM_MAX && vocab <= GMM_BEAM_MAX_VOCAB &&
-         (int64_t)batch * beams <= (1 << 24) &&
+         (int64_t)batch * beams <= (1 << 24) && (int64_t)batch * 64 * kJoinWaves <= kMaxThreads &&
          (int64_t)batch * beams * cdiv(vocab, kRun) <= 4 * kMaxBlocks;
 }
 

@@ -598,7 +598,8 @@ int gmm_kv_fork(const gmm_kv_cache* cache, int32_t* ref, const int32_t* total,
     // the old tables are read while the new ones are written
     if (overlap(pages, table_bytes(batch, pages_stride, max_pages), pages_out,
                 table_bytes(rows, out_stride, out_max_pages)) ||
-        overlap(total, 4 * (int64_t)batch, total_out, 4 * (int64_t)rows))
+        overlap(total, 4 * (int64_t)batch, total_out, 4 * (int64_t)rows) ||
+        overlap(parent, 4 * (int64_t)rows, total_out, 4 * (int64_t)rows))
       return GMM_ERR_INVALID_ARG;
   }
   ForkArgs a{};

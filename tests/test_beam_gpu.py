@@ -241,3 +241,48 @@ def test_calls_on_two_streams():
     for o, w in zip(outs, want):
         for a, b in zip(o, w):
             assert torch.equal(a, b)
+
+
+def test_binding_checks_sizes_and_types():
+    x, s, _ = _inputs(2, 3, 100, "f32")
+    f = lambda *n: torch.empty(*n, device="cuda")
+    i = lambda *n: torch.empty(*n, dtype=torch.int32, device="cuda")
+    ws = gmm.beam_workspace(2, 3, 100)
+    good = dict(logits=x, score=s, out_score=f(2, 4), out_parent=i(2, 4), out_token=i(2, 4), ws=ws)
+    flag = torch.zeros(2, 3, dtype=torch.bool, device="cuda")
+    for kw, err in ((dict(logits=x[0]), TypeError), (dict(logits=x.double()), TypeError),
+                    (dict(logits=x.transpose(1, 2)), TypeError), (dict(score=s[:1]), ValueError),
+                    (dict(score=s.double()), TypeError), (dict(out_score=f(3, 4)), ValueError),
+                    (dict(out_parent=i(2, 3)), ValueError), (dict(weight=f(1, 3)), ValueError),
+                    (dict(mask=i(2, 2, 4)), ValueError), (dict(mask=i(2, 3, 3)), gmm.GMMError),
+                    (dict(done=flag), gmm.GMMError), (dict(done=flag.int()), TypeError),
+                    (dict(eos=100), gmm.GMMError), (dict(ws=ws[:0]), gmm.GMMError)):
+        with pytest.raises(err):
+            gmm.gmm_beam_select(**{**good, **kw})
+    gmm.gmm_beam_select(**good)
+
+
+@pytest.mark.parametrize("m", [1, 3, 16, 64])
+def test_many_words_of_one_size(m):
+    """More equal words than any list holds, in neighbouring and in scattered places, of one beam and
+    of several, behind some that are larger."""
+    vocab = 30011
+    x = torch.full((2, 4, vocab), -2.0, dtype=torch.bfloat16, device="cuda")
+    x[0, :, ::7] = 1.0
+    x[0, 1, 20001] = 1.5
+    x[0, 3, 5] = 1.25
+    x[1, 2, 100:9000] = 3.0
+    x[1, 0, 29000:] = 3.0
+    s = torch.full((2, 4), -1.0, device="cuda")
+    out = _select(x, s, m)
+    for b in range(2):
+        cand = []
+        for j in range(4):
+            z = float(torch.logsumexp(x[b, j].double(), 0))
+            top = torch.sort(x[b, j].double().cpu(), descending=True, stable=True)
+            cand += [(round(-1.0 + float(v) - z, 9), -j, -int(i))
+                     for v, i in zip(top.values[:m], top.indices[:m])]
+        cand = sorted(cand, reverse=True)[:m]
+        # keys of beams with different sums differ by far more than the sums' rounding
+        assert [(-c[1] + 4 * b, -c[2]) for c in cand] == \
+            list(zip(out[1][b].tolist(), out[2][b].tolist()))

@@ -432,3 +432,51 @@ def test_captured_step():
             assert torch.equal(t, w)
         (c.k.float().sum() + 1).item()
         assert short.item() == 0
+
+
+@pytest.mark.parametrize("rows", [3000, 65536])
+def test_fork_of_the_most_rows(rows):
+    """Every row forked twice, dropped or kept: counts of 3000 and 65,536 rows."""
+    c = _cache(2 * rows, boxes=False)
+    g = torch.Generator().manual_seed(rows)
+    pages = torch.randperm(2 * rows, generator=g).to(torch.int32).view(rows, 2).cuda()
+    total = torch.randint(0, 65, (rows,), generator=g).to(torch.int32).cuda()
+    parent = torch.randint(-2, rows, (rows,), generator=g).to(torch.int32).cuda()
+    named = lambda t: (t[:, None] + 31 >= torch.tensor([32, 64], device="cuda"))
+    ref = gmm.kv_pool(c)
+    ref[pages[named(total)].long()] = 1
+    nt, npg = torch.empty_like(total), torch.empty_like(pages)
+    gmm.gmm_kv_fork(c, ref, total, pages, parent, nt, npg)
+    ok = parent >= 0
+    wt = torch.where(ok, total[parent.clamp(min=0).long()], 0)
+    wp = torch.where(named(wt), pages[parent.clamp(min=0).long()], -1)
+    want = torch.bincount(wp[wp >= 0].long(), minlength=2 * rows).to(torch.int32)
+    assert torch.equal(nt, wt) and torch.equal(npg, wp) and torch.equal(ref, want)
+
+
+def test_binding_checks_sizes_and_types():
+    c, small = _cache(10), _cache(10, heads=2)
+    ref, ws = gmm.kv_pool(c), gmm.kv_pool_workspace(c, 2)
+    t, p, s = _i32([0, 0]), _i32([[0, 1, 2]] * 2), _i32([0])
+    nt, npg = _i32([0, 0]), _i32([[0, 1, 2]] * 2)
+    good = dict(ref=ref, total=t, pages=p, parent=_i32([0, 1]), total_out=nt, pages_out=npg)
+    for kw, err in ((dict(ref=ref[:9]), ValueError), (dict(ref=ref.float()), TypeError),
+                    (dict(total=_i32([0])), ValueError), (dict(total=_i32([0, 0, 0])), ValueError),
+                    (dict(pages=p.long()), TypeError), (dict(pages=p.t()), TypeError),
+                    (dict(parent=_i32([0])), ValueError), (dict(parent=[0, 1]), AttributeError),
+                    (dict(keep=_i32([1])), ValueError), (dict(pages_out=npg[:, :2]), gmm.GMMError),
+                    (dict(pages_out=p), gmm.GMMError), (dict(total_out=t), gmm.GMMError)):
+        with pytest.raises(err):
+            gmm.gmm_kv_fork(c, **{**good, **kw})
+    for args in ((_i32([0]), t, p, s), (t, t, p, s.long()), (t, t, p, s[:0])):
+        with pytest.raises((TypeError, ValueError)):
+            gmm.gmm_kv_grow(c, ref, *args, ws)
+    with pytest.raises(gmm.GMMError):
+        gmm.gmm_kv_grow(c, ref, t, t, p, s, ws[:256])
+    with pytest.raises(gmm.GMMError):
+        gmm.gmm_kv_copy(c, small, s, s)
+    with pytest.raises(ValueError):
+        gmm.gmm_kv_copy(c, c, s, _i32([0, 1]))
+    with pytest.raises(ValueError):
+        gmm.gmm_kv_compact(c, ref, t, p, ref[:5].clone(), s, ws)
+    assert (ref == 0).all()

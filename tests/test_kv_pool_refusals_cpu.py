@@ -97,6 +97,7 @@ def test_fork_refuses_tables_that_overlap(lib):
         assert _fork(lib, c, npg=P + off) == BAD, off
     for off in (0, 8, -8):
         assert _fork(lib, c, nt=P + off) == BAD, off
+        assert _fork(lib, c, parent=Q + 4096 + off, nt=Q + 4096) == BAD, off
 
 
 def test_workspaces(lib):
@@ -116,7 +117,7 @@ def test_workspaces(lib):
     for kw in (dict(ws=None), dict(ws=P + 16), dict(nb=need - 1)):
         assert _beam(lib, **kw) == WS, kw
     for a in ((0, 4, 1000), (2, 0, 1000), (2, 4, 0), (2, 65, 1000), (2, 4, (1 << 24) + 1),
-              (1 << 24, 2, 1000), (1 << 19, 64, 1000), (1 << 15, 64, 1 << 24)):
+              (1 << 24, 2, 1000), (1 << 19, 64, 1000), (1 << 15, 64, 1 << 24), (1 << 23, 1, 10)):
         assert lib.gmm_beam_workspace_bytes(*a) == 0, a
 
 
