@@ -28,7 +28,6 @@ using namespace kv;
 constexpr double kLog2eD = 1.4426950408889634;
 constexpr double kLn2D = 0.6931471805599453;
 constexpr int kRun = 2048;        // words of a run
-constexpr int kJoinWaves = 8;     // waves of a sequence's workgroup
 
 struct BeamArgs {
   const void* x;
@@ -129,6 +128,13 @@ __device__ __forceinline__ int below(uint64_t bits) {
                                    __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
 }
 
+// A word's logit in fp32.  (By its bits, of bf16: the compiler would take maxima in bf16, rounding each.)
+__device__ __forceinline__ float logit(float x) { return x; }
+__device__ __forceinline__ float logit(_Float16 x) { return (float)x; }
+__device__ __forceinline__ float logit(__bf16 x) {
+  return float_of((uint32_t)__builtin_bit_cast(uint16_t, x) << 16);
+}
+
 // 16 bytes of words: at an address that is a multiple of an element only, past the vocabulary
 // -inf, and -inf where the mask forbids
 template <typename T>
@@ -225,7 +231,7 @@ __global__ __launch_bounds__(256) void k_beam_run(BeamArgs a) {
 #pragma unroll
   for (int i = 0; i < W::kSteps; ++i)
 #pragma unroll
-    for (int e = 0; e < W::N; ++e) mx = fmaxf(mx, (float)words.v[i][e]);
+    for (int e = 0; e < W::N; ++e) mx = fmaxf(mx, logit(words.v[i][e]));
   mx = wave_max(mx);
   // exponents by one multiply-add, whose product is not rounded; 2^-64 is any factor that leaves
   // the product exact
@@ -237,7 +243,7 @@ __global__ __launch_bounds__(256) void k_beam_run(BeamArgs a) {
   for (int i = 0; i < W::kSteps; ++i)
 #pragma unroll
     for (int e = 0; e < W::N; ++e)
-      sum[e & 3] += __builtin_amdgcn_exp2f(fmaf((float)words.v[i][e], c, -unit));
+      sum[e & 3] += __builtin_amdgcn_exp2f(fmaf(logit(words.v[i][e]), c, -unit));
   const float z = wave_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
   if (lane == 0) a.part[(int64_t)row * a.runs + run] = make_float2(mx, z);
 }
@@ -358,12 +364,12 @@ __device__ __forceinline__ bool taken(const Picked& p, uint64_t v, int* seen) {
 
 constexpr int kChunk = 1024;           // runs looked at together
 constexpr int kLane = 1 + kChunk / 64; // of a lane: neighbours, odd for the banks of LDS
-constexpr int kBuffer = GMM_BEAM_MAX + 512;       // words that a wave holds
+constexpr int kBuffer = GMM_BEAM_MAX + 256;       // words that a wave holds
 
-struct Word {
-  uint64_t key;
-  uint32_t at;                         // beam * vocab + word
-  float x;
+// A wave's words so far: score, and beam * vocab + word.
+struct Found {
+  uint64_t key[kBuffer];
+  uint32_t at[kBuffer];
 };
 
 struct Join {
@@ -378,8 +384,12 @@ struct Join {
   int list_run[64];
   uint64_t least;
   int kept;
-  int count[kJoinWaves];
-  Word word[kJoinWaves][kBuffer];
+};
+
+template <int NW>
+struct JoinOf : Join {
+  int count[NW];
+  Found found[NW];
 };
 
 // l of a live beam's logit, from its difference to the largest: products of large logits would
@@ -419,7 +429,8 @@ __device__ __forceinline__ void put_run(Join& s, int i, uint64_t key) {
   s.lo[i] = (uint32_t)key;
 }
 
-// log Z of up to two beams of a wave, j and j + kJoinWaves: their loads go together
+// log Z of up to two beams of a wave, j and j + NW: their loads go together
+template <int NW>
 __device__ __forceinline__ void join_beams(const BeamArgs& a, Join& s, int row0, int j0) {
   const int lane = threadIdx.x & 63;
   float sc[2], wt[2];
@@ -427,7 +438,7 @@ __device__ __forceinline__ void join_beams(const BeamArgs& a, Join& s, int row0,
   float2 v[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int row = row0 + min(j0 + i * kJoinWaves, a.beams - 1);
+    const int row = row0 + min(j0 + i * NW, a.beams - 1);
     sc[i] = a.score[row];
     wt[i] = a.weight ? a.weight[row] : 1.f;
     fin[i] = a.done ? a.done[row] : 0;
@@ -435,7 +446,7 @@ __device__ __forceinline__ void join_beams(const BeamArgs& a, Join& s, int row0,
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int j = j0 + i * kJoinWaves;
+    const int j = j0 + i * NW;
     if (j >= a.beams) break;
     int kind = finite(sc[i]) && wt[i] > 0.f && finite(wt[i]) ? fin[i] ? 2 : 1 : 0;
     double logz = 0.0;
@@ -546,6 +557,7 @@ __device__ __forceinline__ void pick_runs(const BeamArgs& a, Join& s, int base, 
 
 // The m best runs of the sequence, in order, into s.run, their scores into s.hi / s.lo, their number
 // into s.kept, and the m-th one's score into s.least.
+template <int NW>
 __device__ __forceinline__ void best_runs(const BeamArgs& a, Join& s, int row0) {
   const int tid = threadIdx.x;
   const int runs = a.beams * a.runs;
@@ -556,7 +568,7 @@ __device__ __forceinline__ void best_runs(const BeamArgs& a, Join& s, int row0) 
   for (int base = 0; base < runs; base += kChunk) {
     if (!one_chunk(a)) {
       bool any = false;
-      for (int t = tid; t < min(kChunk, runs - base); t += 64 * kJoinWaves) {
+      for (int t = tid; t < min(kChunk, runs - base); t += 64 * NW) {
         const int i = base + t, j = (int)(((float)i + 0.5f) * inv);    // i / runs: exact below 2^21
         uint64_t k = run_key(a, s, j, i - j * a.runs, part[i].x);
         // an equal one is behind the m kept
@@ -574,19 +586,17 @@ __device__ __forceinline__ void best_runs(const BeamArgs& a, Join& s, int row0) 
 }
 
 // Leaves the m best of a wave's n words, in their order.
-__device__ __forceinline__ Picked keep_words(Word* buf, int n, int m) {
+__device__ __forceinline__ Picked keep_words(Found& f, int n, int m) {
   constexpr int C = kBuffer / 64;
   const int lane = threadIdx.x & 63;
   wave_sync();
   uint64_t v[C];
-  Word e[C];
+  uint32_t at[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    v[c] = 0;
-    if (c * 64 + lane < n) {
-      e[c] = buf[c * 64 + lane];
-      v[c] = e[c].key;
-    }
+    const bool in = c * 64 + lane < n;
+    v[c] = in ? f.key[c * 64 + lane] : 0;
+    at[c] = in ? f.at[c * 64 + lane] : 0;
   }
   const Picked p = pick<C>(v, m);
   int k = 0, seen = 0;
@@ -594,38 +604,43 @@ __device__ __forceinline__ Picked keep_words(Word* buf, int n, int m) {
   for (int c = 0; c < C; ++c) {
     const bool in = taken(p, v[c], &seen);
     const uint64_t bal = __ballot(in);
-    if (in) buf[k + below(bal)] = e[c];
+    if (in) {
+      f.key[k + below(bal)] = v[c];
+      f.at[k + below(bal)] = at[c];
+    }
     k += __popcll(bal);
   }
   wave_sync();
   return p;
 }
 
-// A workgroup a sequence: log Z of its beams, its m best runs, their m best words.
-template <typename T>
-__global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(BeamArgs a) {
-  __shared__ Join s;
+// A workgroup of NW waves a sequence: log Z of its beams, its m best runs, their m best words.
+template <typename T, int NW>
+__global__ __launch_bounds__(64 * NW, 4) void k_beam_join(BeamArgs a) {
+  __shared__ JoinOf<NW> s;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row0 = blockIdx.x * a.beams;
-  for (int j = w; j < a.beams; j += 2 * kJoinWaves) join_beams(a, s, row0, j);
+  for (int j = w; j < a.beams; j += 2 * NW) join_beams<NW>(a, s, row0, j);
   __syncthreads();
-  best_runs(a, s, row0);
+  best_runs<NW>(a, s, row0);
 
   // the words that reach the m-th best run's maximum; a wave takes neighbouring runs, so that
   // the waves' words, one after the other, are in order
   typedef Words<T> W;
-  Word* buf = s.word[w];
+  Found& buf = s.found[w];
   uint64_t floor = s.least;
   int held = 0;
-  const int q1 = (w + 1) * s.kept / kJoinWaves;
-  for (int q = w * s.kept / kJoinWaves; q < q1; ++q) {
+  const int q1 = (w + 1) * s.kept / NW;
+  for (int q = w * s.kept / NW; q < q1; ++q) {
     const int gid = __builtin_amdgcn_readfirstlane(s.run[q]);
     const int j = gid / a.runs, r = gid - j * a.runs;
     W words;
-    uint32_t steps = 0;                      // with words that may count
+    // parts of the run with words that may count: 256 neighbours, half of the lanes of 16-bit words
+    constexpr int kHalves = W::N / 4;
+    uint32_t parts = 0;
     float least = -INFINITY;
     if (s.kind[j] == 2) {
-      steps = 1;
+      parts = 1;
     } else {
       const T* x = row_of<T>(a, row0 + j);
       words.fetch(a, x, mask_of(a, row0 + j), r);
@@ -633,38 +648,46 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(BeamArgs a) {
       least = logit_of(a, s, j, floor);
 #pragma unroll
       for (int i = 0; i < W::kSteps; ++i) {
-        float mx = (float)words.v[i][0];
+        float mx = logit(words.v[i][0]);
 #pragma unroll
-        for (int e = 1; e < W::N; ++e) mx = fmaxf(mx, (float)words.v[i][e]);
-        if (__ballot(mx >= least)) steps |= 1u << i;
+        for (int e = 1; e < W::N; ++e) mx = fmaxf(mx, logit(words.v[i][e]));
+        const uint64_t bal = __ballot(mx >= least);
+        if constexpr (kHalves == 2)
+          parts |= (uint32_t)((uint32_t)bal != 0) << 2 * i | (uint32_t)(bal >> 32 != 0) << (2 * i + 1);
+        else
+          parts |= (uint32_t)(bal != 0) << i;
       }
     }
-    while (steps) {
-      const int i = __builtin_ctz(steps);
-      steps &= steps - 1;
+    while (parts) {
+      const int part = __builtin_ctz(parts), i = part / kHalves;
+      parts &= parts - 1;
       if (s.kind[j] == 2) {
-        if (lane == 0)
-          buf[held] = Word{(uint64_t)s.hi[q] << 32 | s.lo[q], (uint32_t)j * a.vocab + a.eos, s.score[j]};
+        if (lane == 0) {
+          buf.key[held] = (uint64_t)s.hi[q] << 32 | s.lo[q];
+          buf.at[held] = (uint32_t)j * a.vocab + a.eos;
+        }
         ++held;
       } else {
         typename W::V x = words.v[0];
 #pragma unroll
         for (int c = 1; c < W::kSteps; ++c)
           if (c == i) x = words.v[c];
+        const float from = kHalves == 1 || lane / 32 == part % kHalves ? least : INFINITY;
         // in the order of the words: those of the lanes before, and of this one.  What passes
         // for its logit but has not the score is held as none.
         int at = held, n = 0;
 #pragma unroll
         for (int e = 0; e < W::N; ++e) {
-          const uint64_t bal = __ballot((float)x[e] >= least);
+          const uint64_t bal = __ballot(logit(x[e]) >= from);
           at += below(bal);
           n += __popcll(bal);
         }
 #pragma unroll
         for (int e = 0; e < W::N; ++e) {
-          if ((float)x[e] >= least) {
-            const uint64_t key = key_of(a, s, j, (float)x[e]);
-            buf[at++] = Word{key < floor ? 0 : key, (uint32_t)j * a.vocab + W::at(r, i) + e, (float)x[e]};
+          if (logit(x[e]) >= from) {
+            const uint64_t key = key_of(a, s, j, logit(x[e]));
+            buf.key[at] = key < floor ? 0 : key;
+            buf.at[at++] = (uint32_t)j * a.vocab + W::at(r, i) + e;
           }
         }
         held += n;
@@ -682,50 +705,57 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(BeamArgs a) {
 
   // all waves' words into wave 0's lanes
   int total = 0;
-  for (int c = 0; c < kJoinWaves; ++c) total += s.count[c];
-  Word e{0, 0, 0.f};
+  for (int c = 0; c < NW; ++c) total += s.count[c];
+  uint64_t key = 0;
+  uint32_t word = 0;
   if (total <= 64) {
     int first = 0;
-    for (int c = 0; c < kJoinWaves; ++c) {
+    for (int c = 0; c < NW; ++c) {
       const int i = lane - first;
-      if (i >= 0 && i < s.count[c]) e = s.word[c][i];
+      if (i >= 0 && i < s.count[c]) {
+        key = s.found[c].key[i];
+        word = s.found[c].at[i];
+      }
       first += s.count[c];
     }
   } else {
-    uint64_t v[kJoinWaves];
-    Word all[kJoinWaves];
+    uint64_t v[NW];
+    uint32_t all[NW];
 #pragma unroll
-    for (int c = 0; c < kJoinWaves; ++c) {
-      v[c] = 0;
-      if (lane < s.count[c]) {
-        all[c] = s.word[c][lane];
-        v[c] = all[c].key;
-      }
+    for (int c = 0; c < NW; ++c) {
+      const bool in = lane < s.count[c];
+      v[c] = in ? s.found[c].key[lane] : 0;
+      all[c] = in ? s.found[c].at[lane] : 0;
     }
-    const Picked p = pick<kJoinWaves>(v, a.m);
+    const Picked p = pick<NW>(v, a.m);
     int k = 0, seen = 0;
 #pragma unroll
-    for (int c = 0; c < kJoinWaves; ++c) {
+    for (int c = 0; c < NW; ++c) {
       const bool in = taken(p, v[c], &seen);
       const uint64_t bal = __ballot(in);
-      if (in) s.word[0][k + below(bal)] = all[c];
+      if (in) {
+        buf.key[k + below(bal)] = v[c];
+        buf.at[k + below(bal)] = all[c];
+      }
       k += __popcll(bal);
     }
     total = p.count;
     wave_sync();
-    if (lane < total) e = s.word[0][lane];
+    key = lane < total ? buf.key[lane] : 0;
+    word = buf.at[lane];
   }
-  s.list[lane] = e.key;
+  s.list[lane] = key;
   wave_sync();
-  const int place = place_of(s.list, e.key, total), found = __popcll(__ballot(e.key != 0));
+  const int place = place_of(s.list, key, total), found = __popcll(__ballot(key != 0));
   const int64_t o = (int64_t)blockIdx.x * a.m;
-  if (e.key != 0 && place < a.m) {
-    const int j = (int)(e.at / (uint32_t)a.vocab), word = (int)(e.at - (uint32_t)j * a.vocab);
+  if (key != 0 && place < a.m) {
+    const int j = (int)(word / (uint32_t)a.vocab), v = (int)(word - (uint32_t)j * a.vocab);
     const bool fin = s.kind[j] == 2;
-    a.out_score[o + place] = fin ? e.x : (float)total_of(a, s, j, e.x);
+    // l from w l, whose rounding in 64 bits is far below that of the result
+    a.out_score[o + place] = fin ? s.score[j] : (float)(value_of(key) / s.weight[j]);
     a.out_parent[o + place] = (int32_t)(row0 + j);
-    a.out_token[o + place] = word;
-    if (a.out_done) a.out_done[o + place] = fin || word == a.eos;
+    a.out_token[o + place] = v;
+    if (a.out_done) a.out_done[o + place] = fin || v == a.eos;
   }
   if (lane >= found && lane < a.m) {
     a.out_score[o + lane] = -INFINITY;
@@ -738,7 +768,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void k_beam_join(BeamArgs a) {
 // ---------------------------------------------------------------- host
 bool shape_ok(int32_t batch, int32_t beams, int32_t vocab) {
   return beams <= GMM_BEAM_MAX && vocab <= GMM_BEAM_MAX_VOCAB &&
-         (int64_t)batch * beams <= (1 << 24) && (int64_t)batch * 64 * kJoinWaves <= kMaxThreads &&
+         (int64_t)batch * beams <= (1 << 24) && (int64_t)batch * 1024 <= kMaxThreads &&
          (int64_t)batch * beams * cdiv(vocab, kRun) <= 4 * kMaxBlocks;
 }
 
@@ -750,7 +780,13 @@ template <typename T>
 int launch(const BeamArgs& a, int batch, hipStream_t st) {
   hipLaunchKernelGGL((k_beam_run<T>), dim3((unsigned)cdiv((int64_t)a.rows * a.runs, 4)), dim3(256),
                      0, st, a);
-  hipLaunchKernelGGL((k_beam_join<T>), dim3((unsigned)batch), dim3(64 * kJoinWaves), 0, st, a);
+  const int most = a.beams > a.m ? a.beams : a.m;
+  const auto join = [&](auto kernel, int waves) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)batch), dim3(64 * waves), 0, st, a);
+  };
+  if (most <= 4) join(k_beam_join<T, 4>, 4);
+  else if (most <= 8) join(k_beam_join<T, 8>, 8);
+  else join(k_beam_join<T, 16>, 16);
   return launch_status();
 }
 
