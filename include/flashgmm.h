@@ -562,10 +562,12 @@ int gmm_kv_attend(const gmm_kv_cache* cache, const gmm_kv_batch* seqs, int64_t t
  *   gmm_beam_select -> gmm_kv_fork -> gmm_kv_grow -> gmm_kv_append ->
  *   gmm_kv_attend -> logits -> gmm_beam_select
  * Calls that change one pool (its counts, tables or pages) must be ordered on
- * one stream.  At most GMM_KV_MAX_ROWS rows in a call.
+ * one stream.  At most GMM_KV_MAX_ROWS rows in a call and GMM_KV_MAX_POOL
+ * pages of a cache.
  * ---------------------------------------------------------------------- */
 
 #define GMM_KV_MAX_ROWS 65536
+#define GMM_KV_MAX_POOL (1 << 26)
 #define GMM_BEAM_MAX 64
 #define GMM_BEAM_MAX_VOCAB (1 << 24)
 

@@ -98,8 +98,9 @@ __global__ __launch_bounds__(256) void k_kv_copy(CopyArgs a) {
 }
 
 // It is not: few workgroups with more in flight each.
-__global__ __launch_bounds__(1024) void k_kv_copy_some(CopyArgs a) {
-  copy_items<1024, 4>(a, blockIdx.x, gridDim.x);
+template <int kThreads, int kSteps>
+__global__ __launch_bounds__(kThreads) void k_kv_copy_some(CopyArgs a) {
+  copy_items<kThreads, kSteps>(a, blockIdx.x, gridDim.x);
 }
 
 // ---------------------------------------------------------------- fork
@@ -126,9 +127,16 @@ __device__ __forceinline__ void count(const ForkArgs& a, int page, int by) {
 
 // Is p among the first n parents?  The same answer in every thread.
 __device__ __forceinline__ bool named(const ForkArgs& a, int p, int n) {
-  bool hit = false;
-  for (int i = threadIdx.x; i < n; i += 256) hit |= a.parent[i] == p;
-  return __syncthreads_or(hit);
+  for (int i0 = 0; i0 < n; i0 += 4096) {
+    bool hit = false;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const int i = i0 + k * 256 + threadIdx.x;
+      hit |= i < n && a.parent[min(i, n - 1)] == p;
+    }
+    if (__syncthreads_or(hit)) return true;
+  }
+  return false;
 }
 
 // Workgroups of a new row copy its parent's entries, those of an old row without a child give up
@@ -206,24 +214,38 @@ __device__ __forceinline__ T group_sum(T v, T* tmp, T* all) {
 
 // Words of the pages from `first` on: wave w's words are those of its `words` x 64 pages in a
 // row, word i of them in lane i; a bit is set where the page is used.
-__device__ __forceinline__ uint64_t load_words(const int32_t* ref, int pages, int first, int words) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int base = first + w * words * 64 + lane;
+template <int kFlight>
+__device__ __forceinline__ uint64_t load_words(const int32_t* ref, int pages, int base, int words) {
+  const int lane = threadIdx.x & 63;
   uint64_t mine = 0;
-  for (int i = 0; i < words; i += 8) {
-    int v[8];                        // eight loads in flight
+  for (int i = 0; i < words; i += kFlight) {
+    int v[kFlight];                  // loads in flight
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = ref[min(base + (i + j) * 64, pages - 1)];
+    for (int j = 0; j < kFlight; ++j) v[j] = ref[min(base + (i + j) * 64, pages - 1)];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < kFlight; ++j) {
       const uint64_t bits = __ballot(i + j < words && base + (i + j) * 64 < pages && v[j] > 0);
       if (lane == i + j) mine = bits;
     }
   }
   return mine;
 }
+__device__ __forceinline__ uint64_t load_words(const int32_t* ref, int pages, int first, int words) {
+  const int base = first + (int)(threadIdx.x >> 6) * words * 64 + (int)(threadIdx.x & 63);
+  return words > 8 ? load_words<32>(ref, pages, base, words) : load_words<4>(ref, pages, base, words);
+}
 __device__ __forceinline__ int words_of(int pages) {
   return pages >= kSpan ? 64 : (pages + 64 * kWaves - 1) / (64 * kWaves);
+}
+
+// Used pages of the spans of 1024 `words` pages, a workgroup each.
+__global__ __launch_bounds__(64 * kWaves) void k_kv_count(const int32_t* ref, int pages, int words,
+                                                          int32_t* counts) {
+  __shared__ int tmp[kWaves];
+  int all;
+  group_sum((int)__popcll(load_words(ref, pages, (int)blockIdx.x * 64 * kWaves * words, words)), tmp,
+            &all);
+  if (threadIdx.x == 0) counts[blockIdx.x] = all;
 }
 
 // ---------------------------------------------------------------- grow
@@ -245,6 +267,7 @@ struct GrowArgs {
   int32_t* first;             // [cache pages] first row that writes into a shared page
   int32_t* writers;           // [cache pages] rows that do
   int32_t* free_list;         // [cache pages]
+  const int32_t* counts;      // used pages of every kSpan pages of a larger pool, or null
 };
 
 __device__ __forceinline__ int load_agent(const int32_t* p) {
@@ -366,6 +389,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_kv_grow(GrowArgs a) {
   int64_t have = 0;
   for (int first = 0; first < a.cache_pages && have < want; first += kSpan) {
     const int words = words_of(a.cache_pages - first);
+    if (a.counts && a.counts[first / kSpan] == min(kSpan, a.cache_pages - first)) continue;
     if (first > 0) bits = free_words(a, first, words);
     int all;
     const int rank = group_sum((int)__popcll(bits), tmp, &all);
@@ -422,96 +446,87 @@ struct CompactArgs {
   int batch, max_pages;
   int32_t* where;
   int32_t* used;
+  // workspace
   int32_t* count;             // pages moved
   int32_t* from;              // [cache pages / 2]
   int32_t* to;
+  int32_t* counts;            // [spans] used pages, not with one span
+  int words, spans;           // a workgroup has 1024 words pages
 };
 
-// With U used pages, those at U and above go to the free ones below, in order.
-__global__ __launch_bounds__(64 * kWaves) void k_kv_compact(CompactArgs a) {
+// With U used pages, those at U and above go to the free ones below, in order.  A workgroup a span
+// finds the places of its pages from the spans' counts: the k-th free page below U is to[k], the
+// k-th used one from U on from[k], which is noted as -2 - k until it has moved.
+__global__ __launch_bounds__(64 * kWaves) void k_kv_places(CompactArgs a) {
   __shared__ int tmp[kWaves];
-  __shared__ int holes, list[kList];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  // a pool of one span: its words and ranks stay in registers
-  const bool one = a.cache_pages <= kSpan;
-  int used = 0, all = 0, rank = 0;
-  uint64_t bits = 0;
-  for (int first = 0; first < a.cache_pages; first += kSpan) {
-    bits = load_words(a.ref, a.cache_pages, first, words_of(a.cache_pages - first));
-    rank = group_sum((int)__popcll(bits), tmp, &all);
-    used += all;
-  }
-  int moves = 0;
-  bool passed = false;                 // is `used` behind: moves is known then
-  // first the holes, then what fills them
-  for (int pass = 0; pass < 2; ++pass) {
-    int below_u = 0;                   // used pages before the span
-    for (int first = 0; first < a.cache_pages; first += kSpan) {
-      const int words = words_of(a.cache_pages - first);
-      if (!one) {
-        bits = load_words(a.ref, a.cache_pages, first, words);
-        rank = below_u + group_sum((int)__popcll(bits), tmp, &all);
-      }
-      if (!passed && used <= first + kSpan) {
-        // free pages below `used`: those before the word that holds it, and in it
-        const int p0 = first + (w * words + lane) * 64;
-        if (tid == 0) holes = used - (below_u + all);     // `used` at or behind the last word
-        __syncthreads();
-        if (lane < words && p0 <= used && used < p0 + 64)
-          holes = used - (rank + (int)__popcll(bits & ((1ull << (used - p0)) - 1)));
-        __syncthreads();
-        moves = holes;
-        passed = true;
-      }
-      for (int i = 0; i < words; ++i) {
-        const uint64_t b = lane_value(bits, i);
-        const int p = first + (w * words + i) * 64 + lane;
-        const int before = __builtin_amdgcn_readlane(rank, i) + below(b);
-        if (p >= a.cache_pages) continue;
-        const bool in = b >> lane & 1;
-        if (pass == 0) {
-          if (p < used && !in) {
-            const int k = p - before;
-            if (k < kList) list[k] = p;
-            a.to[k] = p;
-          }
-        } else {
-          int to = in ? p : -1;
-          if (p >= used && in) {
-            const int k = before - (used - moves);
-            to = k < kList ? list[k] : a.to[k];
-            a.from[k] = p;
-            a.ref[to] = a.ref[p];
-            a.ref[p] = 0;
-          }
-          a.where[p] = to;
-        }
-      }
-      below_u += all;
-    }
+  __shared__ int prefix[64 * kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, span = 64 * kWaves * a.words;
+  const int first = blockIdx.x * span;
+  const uint64_t bits = load_words(a.ref, a.cache_pages, first, a.words);
+  int used, all, rank = group_sum((int)__popcll(bits), tmp, &used);
+  int below_u;                         // used pages below U
+  uint64_t bits_u = bits;
+  int at_u = 0;                        // first page of the span that holds page U
+  if (a.spans > 1) {
+    const int before = group_sum(tid < a.spans ? a.counts[tid] : 0, tmp, &used);
+    prefix[tid] = before;
     __syncthreads();
+    rank += prefix[blockIdx.x];
+    at_u = min(used / span, a.spans - 1) * span;
+    bits_u = load_words(a.ref, a.cache_pages, at_u, a.words);
+    below_u = prefix[at_u / span];
+  } else {
+    below_u = 0;
   }
-  if (tid == 0) {
+  const int p0 = at_u + (w * a.words + lane) * 64;
+  if (lane >= a.words || p0 >= used) bits_u = 0;
+  else if (used - p0 < 64) bits_u &= (1ull << (used - p0)) - 1;
+  group_sum((int)__popcll(bits_u), tmp, &all);
+  below_u += all;
+  for (int i = 0; i < a.words; ++i) {
+    const uint64_t b = lane_value(bits, i);
+    const int p = first + (w * a.words + i) * 64 + lane;
+    const int before = __builtin_amdgcn_readlane(rank, i) + below(b);
+    if (p >= a.cache_pages) continue;
+    const bool in = b >> lane & 1;
+    int place = in ? p : -1;
+    if (p < used && !in) a.to[p - before] = p;
+    if (p >= used && in) {
+      a.from[before - below_u] = p;
+      place = -2 - (before - below_u);
+    }
+    a.where[p] = place;
+  }
+  if (blockIdx.x == 0 && tid == 0) {
     a.used[0] = used;
-    a.count[0] = moves;
+    a.count[0] = used - below_u;
   }
 }
 
-// The first `blocks` workgroups copy, the others rewrite the tables: a row, 1024 entries each.
-__global__ __launch_bounds__(1024) void k_kv_move(CopyArgs c, CompactArgs a, int blocks,
-                                                 int spans) {
+// The first `blocks` workgroups copy and note the new places, the others rewrite the tables: a part of
+// a row, an entry a thread.  A place that is being noted reads as either of two that say the same.
+template <int kThreads, int kSteps>
+__global__ __launch_bounds__(kThreads) void k_kv_move(CopyArgs c, CompactArgs a, int blocks,
+                                                      int spans) {
   if ((int)blockIdx.x < blocks) {
-    copy_items<1024, 4>(c, blockIdx.x, blocks);
+    const int moves = *a.count;
+    for (int i = blockIdx.x * kThreads + threadIdx.x; i < moves; i += blocks * kThreads) {
+      const int from = a.from[i], to = a.to[i];
+      a.where[from] = to;
+      a.ref[to] = a.ref[from];
+      a.ref[from] = 0;
+    }
+    copy_items<kThreads, kSteps>(c, blockIdx.x, blocks);
     return;
   }
   const int item = (int)blockIdx.x - blocks, row = item / spans;
-  const int e0 = (item - row * spans) * 1024;
-  const int n = min(pages_of(a.total[row], a.shift), a.max_pages);
-  if (const int e = e0 + threadIdx.x; e < n) {
-    const int p = a.pages[(int64_t)row * a.stride + e];
-    const int to = p >= 0 && p < a.cache_pages ? a.where[p] : -1;
-    if (to >= 0 && to != p) a.pages[(int64_t)row * a.stride + e] = to;
-  }
+  const int e = (item - row * spans) * kThreads + (int)threadIdx.x;
+  if (e >= min(pages_of(a.total[row], a.shift), a.max_pages)) return;
+  const int p = a.pages[(int64_t)row * a.stride + e];
+  if (p < 0 || p >= a.cache_pages) return;
+  const int place = a.where[p];
+  const int to = place < -1 ? a.to[-2 - place] : place;
+  if (to >= 0 && to != p) a.pages[(int64_t)row * a.stride + e] = to;
 }
 
 // ---------------------------------------------------------------- host
@@ -527,19 +542,24 @@ void set_copy(const gmm_kv_cache* src, const gmm_kv_cache* dst, CopyArgs* a) {
   a->heads = dst->heads;
 }
 
-// workgroups of a copy of up to `pairs` pages in items of `part` bytes
-int64_t copy_blocks(const CopyArgs& a, int64_t pairs, int part, int64_t most) {
-  const int64_t items = pairs * (2 * cdiv(a.bytes, part) + 1);
+// The number of pages to copy is known on the GPU: up to two workgroups a CU of 1024 threads, as many
+// threads in smaller ones where a page's keys leave most of 1024 idle.
+constexpr int kSmallPage = 8192;
+
+// workgroups for up to `pairs` pages, `units` of 16 bytes an item
+int64_t copy_blocks(const CopyArgs& a, int64_t pairs, int units) {
+  const int64_t items = pairs * (2 * cdiv(a.bytes, units * 16) + 1);
+  const int64_t most = a.bytes > kSmallPage ? 8 * kCUs : 32 * kCUs;
   return items < most ? items : most;
 }
 
 int64_t pool_need(const gmm_kv_cache* c, int32_t batch) {
-  return cdiv(256 + 4 * (3 * (int64_t)c->pages + 4 * (int64_t)batch + 64), 256) * 256;
+  return cdiv(256 + 4 * (3 * (int64_t)c->pages + 4 * (int64_t)batch + 64 + 1024), 256) * 256;
 }
 
 int check_tables(const gmm_kv_cache* c, int32_t batch, int32_t max_pages, int64_t stride) {
   if (batch < 1 || max_pages < 1 || stride < max_pages) return GMM_ERR_INVALID_ARG;
-  if ((int64_t)max_pages * c->page > (1 << 30) || batch > GMM_KV_MAX_ROWS || c->pages > (1 << 30))
+  if ((int64_t)max_pages * c->page > (1 << 30) || batch > GMM_KV_MAX_ROWS || c->pages > GMM_KV_MAX_POOL)
     return GMM_ERR_UNSUPPORTED;
   return GMM_OK;
 }
@@ -575,7 +595,9 @@ int gmm_kv_copy(const gmm_kv_cache* src, const gmm_kv_cache* dst, const int32_t*
   a.from = src_pages;
   a.to = dst_pages;
   a.n = (int)n;
-  hipLaunchKernelGGL(k_kv_copy, dim3((unsigned)copy_blocks(a, n, 4096, 1 << 20)), dim3(256), 0, stream, a);
+  const int64_t items = n * (2 * cdiv(a.bytes, 4096) + (a.dst.box != nullptr));
+  hipLaunchKernelGGL(k_kv_copy, dim3((unsigned)(items < (1 << 20) ? items : 1 << 20)), dim3(256), 0,
+                     stream, a);
   return launch_status();
 }
 
@@ -665,6 +687,13 @@ int gmm_kv_grow(const gmm_kv_cache* cache, int32_t* ref, const int32_t* held,
   a.first = a.cow + batch;
   a.writers = a.first + cache->pages;
   a.free_list = a.writers + cache->pages;
+  if (cache->pages > kSpan) {
+    // up to 1024 spans; full ones are passed over
+    int32_t* counts = a.free_list + cache->pages;
+    a.counts = counts;
+    hipLaunchKernelGGL(k_kv_count, dim3((unsigned)cdiv(cache->pages, kSpan)), dim3(64 * kWaves), 0,
+                       stream, ref, cache->pages, kSpan / (64 * kWaves), counts);
+  }
   if (batch <= kRows) hipLaunchKernelGGL(k_kv_grow<true>, dim3(1), dim3(kRows), 0, stream, a);
   else hipLaunchKernelGGL(k_kv_grow<false>, dim3(1), dim3(kRows), 0, stream, a);
   CopyArgs c{};
@@ -672,8 +701,12 @@ int gmm_kv_grow(const gmm_kv_cache* cache, int32_t* ref, const int32_t* held,
   c.from = a.from;
   c.to = a.to;
   c.count = a.count;
-  hipLaunchKernelGGL(k_kv_copy_some, dim3((unsigned)copy_blocks(c, batch, 65536, 8 * kCUs)),
-                     dim3(1024), 0, stream, c);
+  const auto copy = [&](auto kernel, int threads, int steps) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)copy_blocks(c, batch, threads * steps)), dim3(threads), 0,
+                       stream, c);
+  };
+  if (c.bytes > kSmallPage) copy(k_kv_copy_some<1024, 4>, 1024, 4);
+  else copy(k_kv_copy_some<256, 2>, 256, 2);
   return launch_status();
 }
 
@@ -701,18 +734,33 @@ int gmm_kv_compact(const gmm_kv_cache* cache, int32_t* ref, const int32_t* total
   a.count = (int32_t*)ws;
   a.from = a.count + 64;
   a.to = a.from + cache->pages;
-  hipLaunchKernelGGL(k_kv_compact, dim3(1), dim3(64 * kWaves), 0, stream, a);
+  a.counts = a.to + cache->pages;
+  // one span up to 16,384 pages; else spans of 4096, at most 1024 of them
+  a.words = (int)cdiv(cache->pages, 64 * kWaves);
+  if (a.words > 16) {
+    const int least = (int)cdiv(a.words, 1024);
+    a.words = least > 4 ? least : 4;
+  }
+  a.spans = (int)cdiv(cache->pages, 64 * kWaves * a.words);
   CopyArgs c{};
   set_copy(cache, cache, &c);
   c.from = a.from;
   c.to = a.to;
   c.count = a.count;
-  const int spans = (int)cdiv(max_pages, 1024);
-  const int64_t blocks = copy_blocks(c, cdiv(cache->pages, 2), 65536, 8 * kCUs);
-  if (blocks + (int64_t)batch * spans > kMaxBlocks / 4) return GMM_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL(k_kv_move, dim3((unsigned)(blocks + (int64_t)batch * spans)), dim3(1024), 0,
-                     stream, c, a, (int)blocks, spans);
-  return launch_status();
+  const auto move = [&](auto kernel, int threads, int steps) -> int {
+    const int64_t spans = cdiv(max_pages, threads);
+    const int64_t blocks = copy_blocks(c, cdiv(cache->pages, 2), threads * steps);
+    if ((blocks + batch * spans) * threads > kMaxThreads) return GMM_ERR_UNSUPPORTED;
+    if (a.spans > 1)
+      hipLaunchKernelGGL(k_kv_count, dim3((unsigned)a.spans), dim3(64 * kWaves), 0, stream, ref,
+                         cache->pages, a.words, a.counts);
+    hipLaunchKernelGGL(k_kv_places, dim3((unsigned)a.spans), dim3(64 * kWaves), 0, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks + batch * spans)), dim3(threads), 0, stream, c, a,
+                       (int)blocks, (int)spans);
+    return launch_status();
+  };
+  if (c.bytes > kSmallPage) return move(k_kv_move<1024, 4>, 1024, 4);
+  return move(k_kv_move<256, 2>, 256, 2);
 }
 
 }  // extern "C"

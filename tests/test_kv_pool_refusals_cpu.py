@@ -66,7 +66,7 @@ def test_caches(lib, call):
 def test_tables(lib, call):
     for kw, want in TABLES:
         assert call(lib, _cache(), **kw) == want, kw
-    assert call(lib, _cache(pages=(1 << 30) + 1)) == UNSUP
+    assert call(lib, _cache(pages=(1 << 26) + 1)) == UNSUP
 
 
 def test_copy(lib):
@@ -106,7 +106,7 @@ def test_workspaces(lib):
     for kw, _ in CACHES:
         assert size(_cache(**kw), 3) == 0
     assert size(c, 0) == 0 and size(c, ROWS + 1) == 0 and size(c, ROWS) > 0
-    assert size(_cache(pages=(1 << 30) + 1), 3) == 0
+    assert size(_cache(pages=(1 << 26) + 1), 3) == 0
     need = size(c, 3)
     assert need % 256 == 0
     assert size(_cache(pages=100), 3) >= 3 * 4 * 100
