@@ -231,7 +231,7 @@ __global__ __launch_bounds__(256) void k_beam_run(BeamArgs a) {
 #pragma unroll
   for (int i = 0; i < W::kSteps; ++i)
 #pragma unroll
-    for (int e = 0; e < W::N; ++e) mx = fmaxf(mx, logit(words.v[i][e]));
+    for (int e = 0; e < W::N; ++e) mx = fmaxf(mx, (float)words.v[i][e]);
   mx = wave_max(mx);
   // exponents by one multiply-add, whose product is not rounded; 2^-64 is any factor that leaves
   // the product exact
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(256) void k_beam_run(BeamArgs a) {
   for (int i = 0; i < W::kSteps; ++i)
 #pragma unroll
     for (int e = 0; e < W::N; ++e)
-      sum[e & 3] += __builtin_amdgcn_exp2f(fmaf(logit(words.v[i][e]), c, -unit));
+      sum[e & 3] += __builtin_amdgcn_exp2f(fmaf((float)words.v[i][e], c, -unit));
   const float z = wave_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
   if (lane == 0) a.part[(int64_t)row * a.runs + run] = make_float2(mx, z);
 }
