@@ -14,7 +14,7 @@ import torch
 
 import paper_2606_10896_amd as _base
 
-from .kv import _CP, _F64, _I32, _I64, _SZ, _VP, _dtype, _stream
+from .kv import _CP, _F64, _I32, _I64, _SZ, _VP, _dtype
 
 _TABLE = [_VP, _VP, _I32, _I32, _I64]                 # total, pages, rows, max_pages, stride
 
@@ -59,6 +59,10 @@ def _call(name, dev, *args):
         raise _base.GMMError(name, rc)
 
 
+def _stream(stream, dev):
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
 def _wrong(t, dtype, numel, name, dev):
     """The error of a tensor that is not a contiguous `dtype` one on device `dev`."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.is_contiguous()):
@@ -70,16 +74,16 @@ def _wrong(t, dtype, numel, name, dev):
 
 def _flat(t, dtype, numel, name, dev):
     """Address of a contiguous CUDA tensor of `numel` elements or more on device `dev`."""
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.is_contiguous() and \
-            t.get_device() == dev and t.numel() >= numel:
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == dev and \
+            t.is_contiguous() and t.numel() >= numel:
         return t.data_ptr()
     raise _wrong(t, dtype, numel, name, dev)
 
 
 def _table(total, pages, dev, names=("total", "pages")):
     """(total, pages, rows, max_pages, stride) of a table."""
-    if not (isinstance(pages, torch.Tensor) and pages.is_cuda and pages.dtype is torch.int32 and
-            pages.dim() == 2):
+    if not (isinstance(pages, torch.Tensor) and pages.dtype is torch.int32 and pages.dim() == 2 and
+            pages.is_cuda):
         raise TypeError(f"{names[1]} must be an int32 CUDA tensor [rows, max_pages]")
     (rows, width), (stride, inner) = pages.shape, pages.stride()
     if inner != 1 and width > 1:
@@ -126,7 +130,7 @@ def gmm_kv_copy(src, dst, src_pages, dst_pages, stream=None):
     if dst_pages.numel() != n:
         raise ValueError(f"{n} source pages, {dst_pages.numel()} destinations")
     _call("gmm_kv_copy", dev, src._ref, dst._ref, _flat(src_pages, torch.int32, n, "src_pages", dev),
-          _flat(dst_pages, torch.int32, n, "dst_pages", dev), n, _stream(stream, src.k))
+          _flat(dst_pages, torch.int32, n, "dst_pages", dev), n, _stream(stream, dev))
 
 
 def gmm_kv_fork(cache, ref, total, pages, parent, total_out, pages_out, keep=None, release=True,
@@ -141,7 +145,7 @@ def gmm_kv_fork(cache, ref, total, pages, parent, total_out, pages_out, keep=Non
     _call("gmm_kv_fork", dev, cache._ref, _flat(ref, torch.int32, cache.pages, "ref", dev),
           *_table(total, pages, dev), _flat(parent, torch.int32, rows, "parent", dev),
           None if keep is None else _flat(keep, torch.int32, rows, "keep", dev), rows,
-          1 if release else 0, new[0], new[1], new[3], new[4], _stream(stream, pages))
+          1 if release else 0, new[0], new[1], new[3], new[4], _stream(stream, dev))
 
 
 def gmm_kv_grow(cache, ref, held, total, pages, short_by, ws, stream=None):
@@ -152,7 +156,7 @@ def gmm_kv_grow(cache, ref, held, total, pages, short_by, ws, stream=None):
     tb = _table(total, pages, dev)
     _call("gmm_kv_grow", dev, cache._ref, _flat(ref, torch.int32, cache.pages, "ref", dev),
           _flat(held, torch.int32, tb[2], "held", dev), *tb,
-          _flat(short_by, torch.int32, 1, "short_by", dev), *_ws(ws, dev), _stream(stream, pages))
+          _flat(short_by, torch.int32, 1, "short_by", dev), *_ws(ws, dev), _stream(stream, dev))
 
 
 def gmm_kv_compact(cache, ref, total, pages, where, used, ws, stream=None):
@@ -161,7 +165,7 @@ def gmm_kv_compact(cache, ref, total, pages, where, used, ws, stream=None):
     dev = cache.k.get_device()
     _call("gmm_kv_compact", dev, cache._ref, _flat(ref, torch.int32, cache.pages, "ref", dev),
           *_table(total, pages, dev), _flat(where, torch.int32, cache.pages, "where", dev),
-          _flat(used, torch.int32, 1, "used", dev), *_ws(ws, dev), _stream(stream, pages))
+          _flat(used, torch.int32, 1, "used", dev), *_ws(ws, dev), _stream(stream, dev))
 
 
 def beam_workspace_bytes(batch, beams, vocab):
@@ -208,4 +212,4 @@ def gmm_beam_select(logits, score, out_score, out_parent, out_token, ws, done=No
           _flat(out_score, torch.float32, batch * m, "out_score", dev),
           _flat(out_parent, torch.int32, batch * m, "out_parent", dev),
           _flat(out_token, torch.int32, batch * m, "out_token", dev),
-          opt(out_done, torch.bool, batch * m, "out_done"), *_ws(ws, dev), _stream(stream, logits))
+          opt(out_done, torch.bool, batch * m, "out_done"), *_ws(ws, dev), _stream(stream, dev))
