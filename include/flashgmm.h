@@ -669,6 +669,7 @@ size_t gmm_beam_workspace_bytes(int32_t batch, int32_t beams, int32_t vocab);
  *   [batch, m]; -infinity, -1 and -1 where there are fewer continuations
  *   out_done [batch, m] bytes (null: not written; needed with done): the
  *   continuation is finished, by its beam or by the word eos
+ *   (with m = beams, out_score and out_done may be score and done themselves)
  * A word of logit -infinity is no continuation.  A beam with a NaN or +infinity
  * among its allowed logits has none; logits of forbidden words, of finished
  * beams and of beams without a score do not matter.

@@ -48,7 +48,9 @@ struct CopyArgs {
 };
 
 // Work items of a pair: `parts` of its keys, as many of its values, and its box.  A thread moves 16
-// bytes in each of kSteps steps, all loads before the stores, streamed past the caches.
+// bytes in each of kSteps steps, all loads before the stores, streamed past the caches.  Sizes within a
+// page are 32-bit: hipcc (ROCm 7.2) took the shorter of two uniform 64-bit lengths from a flag that its
+// comparison does not set, and an incomplete part was copied whole.
 template <int kThreads, int kSteps>
 __device__ __forceinline__ void copy_items(const CopyArgs& a, int block, int blocks) {
   typedef uint32_t V __attribute__((ext_vector_type(4)));
@@ -308,7 +310,7 @@ constexpr int kSlots = 2 * kRows;      // of their table of shared pages
 constexpr int kList = 4096;            // free pages kept in LDS
 
 // One workgroup takes all decisions: what a row needs, which free pages there are, who gets which.
-// Bound by the latency of that chain, 8.0 us for 512 rows that share pages, 5.8 for 9 rows and 1107
+// Bound by the latency of that chain, 8.0 us for 512 rows that share pages, 5.8 for 9 rows and 1108
 // pages, and by the counts' 64 bytes a clock of one CU (65,536 pages: 12 us, 8192: 6.5).
 // kFew: up to kRows rows, which stay in LDS; else they pass through the workspace (512 rows: 11 us).
 template <bool kFew>

@@ -286,3 +286,14 @@ def test_many_words_of_one_size(m):
         # keys of beams with different sums differ by far more than the sums' rounding
         assert [(-c[1] + 4 * b, -c[2]) for c in cand] == \
             list(zip(out[1][b].tolist(), out[2][b].tolist()))
+
+
+def test_scores_and_flags_in_place():
+    x, s, g = _inputs(40, 4, 3001, "bf16", seed=8)
+    done = (torch.rand(40, 4, generator=g) < 0.3).cuda()
+    want = _select(x, s, 4, done=done, eos=5)
+    parent, token = (torch.empty(40, 4, dtype=torch.int32, device="cuda") for _ in range(2))
+    gmm.gmm_beam_select(x, s, s, parent, token, gmm.beam_workspace(40, 4, 3001), done=done,
+                        out_done=done, eos=5)
+    for a, b in zip(want, (s, parent, token, done)):
+        assert torch.equal(a, b)
