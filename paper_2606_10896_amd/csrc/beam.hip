@@ -368,7 +368,7 @@ __device__ __forceinline__ bool taken(const Picked& p, uint64_t v, int* seen) {
 }
 
 constexpr int kChunk = 1024;           // runs looked at together
-constexpr int kLane = 1 + kChunk / 64; // of a lane: neighbours, odd for the banks of LDS
+constexpr int kLane = 1 + kChunk / 64; // and the best before: of a lane, odd for the banks of LDS
 constexpr int kBuffer = GMM_BEAM_MAX + 256;       // words that a wave holds
 
 // A wave's words so far: score, and beam * vocab + word.
@@ -383,12 +383,13 @@ struct Join {
   float top[GMM_BEAM_MAX];             // a beam's largest logit
   float score[GMM_BEAM_MAX];
   int kind[GMM_BEAM_MAX];              // 0: no candidate, 1: live, 2: finished
-  uint32_t hi[64 * kLane], lo[64 * kLane];   // scores of the best runs so far, then of a chunk
+  // scores of the best runs so far, then of a chunk of runs; at the end, of the waves' words
+  uint32_t hi[64 * kLane], lo[64 * kLane];
+  uint32_t word[64 * 16];
   int run[64];                         // the best runs, in order
-  // few numbers while they are picked from
-  alignas(16) uint64_t list[64];
+  alignas(16) uint64_t list[64];       // what few() leaves
   alignas(16) uint32_t tops[64];
-  int list_run[64];
+  int list_at[64];
   uint64_t least;
   int kept;
 };
@@ -495,29 +496,47 @@ __device__ __forceinline__ uint32_t taken(uint32_t more, uint32_t same, int ties
   return more | same;
 }
 
-// The best of the first n of s.hi / s.lo (`kept` runs, then those from `base` on), by one wave:
-// first those that reach the m-th largest of the lanes' maxima, in their upper halves; that
-// leaves few.
-__device__ __forceinline__ void pick_runs(const BeamArgs& a, Join& s, int base, int kept, int n) {
+// Up to 64 of the first n numbers of s.hi / s.lo, the m largest among them, by one wave: the numbers into
+// s.list, where they were into s.list_at, in order; returns how many.  First those that reach a
+// threshold in their upper halves.  Few results: the m-th largest of the lanes' maxima, which are m
+// of the numbers, found by counting (8 of 512: 1900 cycles; bit by bit 4500 where numbers are equal).
+// Many: built bit by bit until m numbers reach it and 64 at most (64 of 480: 6900 cycles; 14,000 by
+// maxima, as too many are left).
+__device__ __forceinline__ int few(Join& s, int n, int m) {
   const int lane = threadIdx.x & 63;
   // as many of a lane as leave 6 m lanes: a lane's maximum is cheaper than its place
-  const int per = max((n + 63) / 64, min(kLane, n / (6 * a.m))) | 1, first = lane * per;
+  const int per = max((n + 63) / 64, min(kLane, n / (6 * m))) | 1, first = lane * per;
   const auto has = [&](int c) { return c < per && first + c < n; };
-  uint32_t h[kLane], top = 0, more = 0, same = 0;
+  uint32_t h[kLane], hi = 0, more = 0, same = 0, least = 1;
 #pragma unroll
   for (int c = 0; c < kLane; ++c) h[c] = s.hi[min(first, 63 * kLane) + c];
 #pragma unroll
   for (int c = 0; c < kLane; ++c) {
     h[c] = has(c) ? h[c] : 0;
-    top = max(top, h[c]);
+    hi = max(hi, h[c]);
   }
-  // the m-th largest: the smallest of those that fewer than m are larger than
-  s.tops[lane] = top >> 1;
-  wave_sync();
-  const int larger = larger_than(s.tops, top >> 1, (n + per - 1) / per);
-  wave_sync();
-  uint32_t least = ~wave_max(larger < a.m ? ~(top & ~1u) : 0u);
-  least = max(least, 1u);              // a number is not 0 in its upper half
+  if (m <= 16) {
+    s.tops[lane] = hi >> 1;
+    wave_sync();
+    const int larger = larger_than(s.tops, hi >> 1, (n + per - 1) / per);
+    // the smallest of those that fewer than m are larger than; a number is not 0 in this half
+    least = max(~wave_max(larger < m ? ~(hi & ~1u) : 0u), 1u);
+  } else if (n > 64) {
+    uint32_t lo = 0;                   // the smallest's complement
+#pragma unroll
+    for (int c = 0; c < kLane; ++c) lo = max(lo, h[c] ? ~h[c] : 0u);
+    hi = wave_max(hi);
+    lo = ~wave_max(lo);
+    uint32_t step = hi == lo ? 0 : 0x80000000u >> __builtin_clz(hi ^ lo);
+    least = max(step ? hi & ~(2 * step - 1) : hi, 1u);
+    while (step) {
+      int k = 0;
+#pragma unroll
+      for (int c = 0; c < kLane; ++c) k += __popcll(__ballot(h[c] >= (least | step)));
+      if (k >= m) least |= step;
+      step = k >= m && k <= 64 ? 0 : step >> 1;
+    }
+  }
 #pragma unroll
   for (int c = 0; c < kLane; ++c) more |= (uint32_t)(h[c] >= least) << c;
   int upto = lanes_sum(__popc(more)), all = __builtin_amdgcn_readlane(upto, 63);
@@ -525,7 +544,7 @@ __device__ __forceinline__ void pick_runs(const BeamArgs& a, Join& s, int base, 
     uint64_t v[kLane];
 #pragma unroll
     for (int c = 0; c < kLane; ++c) v[c] = has(c) ? (uint64_t)h[c] << 32 | s.lo[first + c] : 0;
-    const Picked q = pick<kLane>(v, a.m);
+    const Picked q = pick<kLane>(v, m);
     more = 0;
 #pragma unroll
     for (int c = 0; c < kLane; ++c) {
@@ -536,18 +555,26 @@ __device__ __forceinline__ void pick_runs(const BeamArgs& a, Join& s, int base, 
     upto = lanes_sum(__popc(more));
     all = q.count;
   }
+  s.list[lane] = 0;
+  wave_sync();
   for (int at = upto - __popc(more); more; more &= more - 1) {
     const int i = first + __builtin_ctz(more);
     s.list[at] = (uint64_t)s.hi[i] << 32 | s.lo[i];
-    s.list_run[at++] = i < kept ? s.run[i] : base + i - kept;
+    s.list_at[at++] = i;
   }
   wave_sync();
-  const uint64_t key = lane < all ? s.list[lane] : 0;
-  s.list[lane] = key;
-  wave_sync();
-  const int run = s.list_run[lane], place = place_of(s.list, key, all);
+  return all;
+}
+
+// The best of the first n of s.hi / s.lo (`kept` runs, then those from `base` on), by one wave.
+__device__ __forceinline__ void pick_runs(const BeamArgs& a, Join& s, int base, int kept, int n) {
+  const int lane = threadIdx.x & 63, all = few(s, n, a.m);
+  const uint64_t key = s.list[lane];
+  const int i = lane < all ? s.list_at[lane] : 0, run = i < kept ? s.run[i] : base + i - kept;
+  const int place = place_of(s.list, key, all);
   const bool in = lane < all && place < a.m;
   const uint64_t bal = __ballot(in), last = __ballot(in && place == a.m - 1);
+  wave_sync();
   if (in) {
     const int at = below(bal);
     s.hi[at] = (uint32_t)(key >> 32);
@@ -688,25 +715,23 @@ __global__ __launch_bounds__(64 * NW, 4) void k_beam_join(BeamArgs a) {
 #pragma unroll
         for (int c = 1; c < W::kSteps; ++c)
           if (c == i) x = words.v[c];
-        const float from = kHalves == 1 || lane / 32 == part % kHalves ? least : INFINITY;
-        // in the order of the words: those of the lanes before, and of this one.  What passes
-        // for its logit but has not the score is held as none.
-        int at = held, n = 0;
+        // in the order of the words: those of the lanes before, then of this one.  What passes for
+        // its logit but has not the score is held as none.
+        uint32_t pass = 0;
 #pragma unroll
-        for (int e = 0; e < W::N; ++e) {
-          const uint64_t bal = __ballot(logit(x[e]) >= from);
-          at += below(bal);
-          n += __popcll(bal);
-        }
+        for (int e = 0; e < W::N; ++e) pass |= (uint32_t)(logit(x[e]) >= least) << e;
+        if (kHalves == 2 && lane / 32 != part % kHalves) pass = 0;
+        const int upto = lanes_sum(__popc(pass));
+        for (int at = held + upto - __popc(pass); pass; pass &= pass - 1) {
+          const int e = __builtin_ctz(pass);
+          float y = logit(x[0]);
 #pragma unroll
-        for (int e = 0; e < W::N; ++e) {
-          if (logit(x[e]) >= from) {
-            const uint64_t key = key_of(a, s, j, logit(x[e]));
-            buf.key[at] = key < floor ? 0 : key;
-            buf.at[at++] = (uint32_t)j * a.vocab + W::at(r, i) + e;
-          }
+          for (int c = 1; c < W::N; ++c) y = c == e ? logit(x[c]) : y;
+          const uint64_t key = key_of(a, s, j, y);
+          buf.key[at] = key < floor ? 0 : key;
+          buf.at[at++] = (uint32_t)j * a.vocab + W::at(r, i) + e;
         }
-        held += n;
+        held += __builtin_amdgcn_readlane(upto, 63);
       }
       if (held > GMM_BEAM_MAX) {
         const Picked p = keep_words(buf, held, a.m);
@@ -717,24 +742,33 @@ __global__ __launch_bounds__(64 * NW, 4) void k_beam_join(BeamArgs a) {
   }
   if (lane == 0) s.count[w] = held;
   __syncthreads();
-  if (w != 0) return;
 
-  // all waves' words into wave 0's lanes
-  int total = 0;
-  for (int c = 0; c < NW; ++c) total += s.count[c];
+  // all waves' words, one after the other, and of them the best by one wave
   uint64_t key = 0;
   uint32_t word = 0;
-  if (total <= 64) {
-    int first = 0;
-    for (int c = 0; c < NW; ++c) {
-      const int i = lane - first;
-      if (i >= 0 && i < s.count[c]) {
-        key = s.found[c].key[i];
-        word = s.found[c].at[i];
-      }
-      first += s.count[c];
+  const int upto = lanes_sum(lane < NW ? s.count[lane] : 0);
+  int total = __builtin_amdgcn_readlane(upto, NW - 1);
+  if (total <= 64 || NW > 8) {
+    if (lane < held) {
+      const int at = __builtin_amdgcn_readlane(upto, w) - held + lane;
+      s.hi[at] = (uint32_t)(buf.key[lane] >> 32);
+      s.lo[at] = (uint32_t)buf.key[lane];
+      s.word[at] = buf.at[lane];
     }
-  } else {
+    __syncthreads();
+    if (w != 0) return;
+    if (total <= 64) {
+      if (lane < total) {
+        key = (uint64_t)s.hi[lane] << 32 | s.lo[lane];
+        word = s.word[lane];
+      }
+    } else if constexpr (NW > 8) {
+      total = few(s, total, a.m);
+      key = s.list[lane];
+      word = lane < total ? s.word[s.list_at[lane]] : 0;
+    }
+  } else if constexpr (NW <= 8) {
+    if (w != 0) return;
     uint64_t v[NW];
     uint32_t all[NW];
 #pragma unroll
@@ -757,8 +791,10 @@ __global__ __launch_bounds__(64 * NW, 4) void k_beam_join(BeamArgs a) {
     }
     total = p.count;
     wave_sync();
-    key = lane < total ? buf.key[lane] : 0;
-    word = buf.at[lane];
+    if (lane < total) {
+      key = buf.key[lane];
+      word = buf.at[lane];
+    }
   }
   s.list[lane] = key;
   wave_sync();
