@@ -595,7 +595,7 @@ int gmm_kv_copy(const gmm_kv_cache* src, const gmm_kv_cache* dst, const int32_t*
  *   total [batch], pages [batch, max_pages] rows pages_stride apart (read)
  *   parent, keep [rows]; total_out [rows], pages_out [rows, out_max_pages],
  *   rows out_stride apart, out_max_pages >= max_pages: written whole; they must
- *   not overlap the old ones, nor total_out parent (refused)
+ *   not overlap the old ones, nor parent or keep (refused)
  * batch >= 1.  Every row looks through the parents: 9 us for 512 rows of two
  * pages, 16 for 4096, 0.12 ms for 16,384, 1.4 ms for 65,536.
  */
@@ -669,7 +669,8 @@ size_t gmm_beam_workspace_bytes(int32_t batch, int32_t beams, int32_t vocab);
  *   [batch, m]; -infinity, -1 and -1 where there are fewer continuations
  *   out_done [batch, m] bytes (null: not written; needed with done): the
  *   continuation is finished, by its beam or by the word eos
- *   (with m = beams, out_score and out_done may be score and done themselves)
+ *   (with m = beams, out_score may be score or weight, and out_done done; any
+ *   other overlap of these is refused)
  * A word of logit -infinity is no continuation.  A beam with a NaN or +infinity
  * among its allowed logits has none; logits of forbidden words, of finished
  * beams and of beams without a score do not matter.

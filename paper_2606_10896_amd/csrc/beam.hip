@@ -867,6 +867,13 @@ int gmm_beam_select(const void* logits, int32_t dtype, int64_t seq_stride, int64
   if (!logits || !score || !out_score || !out_parent || !out_token) return GMM_ERR_INVALID_ARG;
   // rows are read by elements of this size
   if ((uintptr_t)logits % (dtype == GMM_F32 ? 4 : 2)) return GMM_ERR_INVALID_ARG;
+  // a sequence's results may take the place of what was read for them, not of another's
+  const int64_t rows = (int64_t)batch * beams, places = (int64_t)batch * m;
+  const auto spoils = [&](const void* out, const void* in, int size) {
+    return out && in && !(out == in && m == beams) && overlap(out, places * size, in, rows * size);
+  };
+  if (spoils(out_score, score, 4) || spoils(out_score, weight, 4) || spoils(out_done, done, 1))
+    return GMM_ERR_INVALID_ARG;
   const int rc = check_kv_ws(ws, ws_bytes, need(batch, beams, vocab));
   if (rc != GMM_OK) return rc;
   BeamArgs a{};

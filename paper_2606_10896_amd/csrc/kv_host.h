@@ -40,6 +40,12 @@ inline int check_kv_ws(void* ws, size_t have, int64_t need) {
   return GMM_OK;
 }
 
+// do [a, a + na) and [b, b + nb) share a byte?
+inline bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+  const char *p = (const char*)a, *q = (const char*)b;
+  return p < q + nb && q < p + na;
+}
+
 }  // namespace kv
 
 #endif  // KV_HOST_H

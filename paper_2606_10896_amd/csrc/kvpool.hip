@@ -574,12 +574,6 @@ int check_tables(const gmm_kv_cache* c, int32_t batch, int32_t max_pages, int64_
   return GMM_OK;
 }
 
-// do [a, a + na) and [b, b + nb) share a byte?
-bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
-  const char *p = (const char*)a, *q = (const char*)b;
-  return p < q + nb && q < p + na;
-}
-
 int64_t table_bytes(int64_t rows, int64_t stride, int32_t max_pages) {
   return rows < 1 ? 0 : ((rows - 1) * stride + max_pages) * 4;
 }
@@ -627,11 +621,13 @@ int gmm_kv_fork(const gmm_kv_cache* cache, int32_t* ref, const int32_t* total,
         out_stride < out_max_pages)
       return GMM_ERR_INVALID_ARG;
     if ((int64_t)out_max_pages * cache->page > (1 << 30)) return GMM_ERR_UNSUPPORTED;
-    // the old tables are read while the new ones are written
-    if (overlap(pages, table_bytes(batch, pages_stride, max_pages), pages_out,
-                table_bytes(rows, out_stride, out_max_pages)) ||
-        overlap(total, 4 * (int64_t)batch, total_out, 4 * (int64_t)rows) ||
-        overlap(parent, 4 * (int64_t)rows, total_out, 4 * (int64_t)rows))
+    // what is read while the new tables are written
+    const int64_t wide = table_bytes(rows, out_stride, out_max_pages);
+    const auto hit = [&](const void* p, int64_t bytes) {
+      return p && (overlap(p, bytes, total_out, 4 * (int64_t)rows) || overlap(p, bytes, pages_out, wide));
+    };
+    if (hit(pages, table_bytes(batch, pages_stride, max_pages)) || hit(total, 4 * (int64_t)batch) ||
+        hit(parent, 4 * (int64_t)rows) || hit(keep, 4 * (int64_t)rows))
       return GMM_ERR_INVALID_ARG;
   }
   ForkArgs a{};

@@ -98,6 +98,10 @@ def test_fork_refuses_tables_that_overlap(lib):
     for off in (0, 8, -8):
         assert _fork(lib, c, nt=P + off) == BAD, off
         assert _fork(lib, c, parent=Q + 4096 + off, nt=Q + 4096) == BAD, off
+        assert _fork(lib, c, keep=Q + 4096 + off, nt=Q + 4096) == BAD, off
+        for name in ("total", "parent", "keep"):
+            assert _fork(lib, c, nt=Q + 8192, npg=Q + 4096, **{name: Q + 4096 + off}) == BAD, name
+    assert _fork(lib, c, nt=P + 16) == BAD             # into the old table of pages
 
 
 def test_workspaces(lib):
@@ -140,6 +144,22 @@ def test_select(lib):
                dict(batch=1 << 23)):
         assert _beam(lib, **kw) == UNSUP, kw
     assert _beam(lib, batch=0, x=None, score=None) == OK
+
+
+def test_select_refuses_results_over_what_it_reads(lib):
+    # scores, weights and flags: 2 x 4; the workspace is refused where they are not
+    for off in (4, -4, 28, -28):
+        assert _beam(lib, os=P + off, ws=None) == BAD, off
+        assert _beam(lib, weight=Q, os=Q + off, ws=None) == BAD, off
+    for off in (1, -1, 7, -7):
+        assert _beam(lib, done=Q, od=Q + off, eos=3, ws=None) == BAD, off
+    for off in (32, -32):
+        assert _beam(lib, os=P + off, ws=None) == WS, off
+    assert _beam(lib, done=Q, od=Q, eos=3, ws=None) == WS
+    # in place only with as many results as beams
+    assert _beam(lib, m=3, ws=None) == BAD
+    assert _beam(lib, m=3, os=Q, done=Q + 64, od=Q + 64, eos=3, ws=None) == BAD
+    assert _beam(lib, m=3, os=Q, ws=None) == WS
 
 
 def test_binding_refuses_what_is_no_gpu_tensor():
