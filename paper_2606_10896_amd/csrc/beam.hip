@@ -483,6 +483,7 @@ __device__ __forceinline__ void join_beams(const BeamArgs& a, Join& s, int row0,
       s.score[j] = sc[i];
       s.kind[j] = kind;
     }
+    wave_sync();                       // all of this is read by the other lanes
     if (one_chunk(a) && lane < a.runs) put_run(s, j * a.runs + lane, run_key(a, s, j, lane, v[i].x));
   }
 }
