@@ -39,6 +39,7 @@ struct BeamArgs {
   int64_t mask_stride;
   double scale;
   float c;                    // scale log2(e)
+  float above_c;              // the power of 2 above it
   int beams, vocab, runs, m, eos, rows;
   float2* part;               // [rows, runs]: maximum, sum
   float* out_score;
@@ -204,9 +205,10 @@ __device__ __forceinline__ const uint32_t* mask_of(const BeamArgs& a, int row) {
 }
 
 // The power of 2 to which a run's sum is relative, by its largest logit: its exponent, rounded to a
-// whole number, so that joining runs does not round.  Past 2^123 (`large`) the logit itself, as there
-// every other logit's weight is 0.
-__device__ __forceinline__ bool large(const BeamArgs& a, float x) { return !(fabsf(x * a.c) < 1e37f); }
+// whole number, so that joining runs does not round.  The product in fp32 is off by up to 32 below 2^30,
+// which the sum carries.  From there on (`large`) more than that, and the sum is relative to the logit
+// itself: the next smaller one is 2^-24 of it below, an exponent of -64, and its weight does not count.
+__device__ __forceinline__ bool large(const BeamArgs& a, float x) { return !(fabsf(x * a.c) < 0x1p30f); }
 __device__ __forceinline__ double unit_of(const BeamArgs& a, float x) {
   return large(a, x) ? (double)x * (double)a.c : (double)rintf(x * a.c);
 }
@@ -238,11 +240,12 @@ __global__ __launch_bounds__(256) void k_beam_run(BeamArgs a) {
 #pragma unroll
     for (int e = 0; e < W::N; ++e) mx = fmaxf(mx, (float)words.v[i][e]);
   mx = wave_max(mx);
-  // exponents by one multiply-add, whose product is not rounded; 2^-64 is any factor that leaves
-  // the product exact
+  // Exponents by one multiply-add, whose product is not rounded.  Of large logits those below the
+  // maximum need only be far from 0: a power of 2 leaves the maximum's product exact, that above
+  // the factor or, where products could pass the type's range (differences of 2^75 and more), 2^-64.
   const bool far = large(a, mx);
-  const float c = far ? 0x1p-64f : a.c;
-  const float unit = !(mx > -INFINITY) ? 0.f : far ? mx * 0x1p-64f : rintf(mx * a.c);
+  const float c = !far ? a.c : fabsf(mx) < 0x1p100f ? a.above_c : 0x1p-64f;
+  const float unit = !(mx > -INFINITY) ? 0.f : far ? mx * c : rintf(mx * c);
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < W::kSteps; ++i)
@@ -474,7 +477,7 @@ __device__ __forceinline__ void join_beams(const BeamArgs& a, Join& s, int row0,
       }
       z = wave_sum(z);
       logz = log(z) + (large(a, mx) ? 0.0 : (unit - (double)a.c * (double)mx) * kLn2D);
-      if (!finite(mx) || !(z > 0.0)) kind = 0;       // no word, NaN or +infinity
+      if (!finite(mx) || !(z > 0.0 && z < (double)INFINITY)) kind = 0;   // no word, NaN or +infinity
     }
     if (lane == 0) {
       s.logz[j] = logz;
@@ -888,6 +891,9 @@ int gmm_beam_select(const void* logits, int32_t dtype, int64_t seq_stride, int64
   a.mask_stride = mask_stride;
   a.scale = scale;
   a.c = (float)(scale * kLog2eD);
+  int above;
+  frexp(a.c, &above);
+  a.above_c = ldexpf(1.f, above);
   a.beams = beams;
   a.vocab = vocab;
   a.runs = (int)cdiv(vocab, kRun);
