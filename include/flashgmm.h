@@ -670,7 +670,8 @@ size_t gmm_beam_workspace_bytes(int32_t batch, int32_t beams, int32_t vocab);
  *   out_done [batch, m] bytes (null: not written; needed with done): the
  *   continuation is finished, by its beam or by the word eos
  *   (with m = beams, out_score may be score or weight, and out_done done; any
- *   other overlap of these is refused)
+ *   other overlap of results with these three or with each other is refused;
+ *   they must not overlap the logits, the mask or the workspace either)
  * A word of logit -infinity is no continuation.  A beam with a NaN or +infinity
  * among its allowed logits has none; logits of forbidden words, of finished
  * beams and of beams without a score do not matter.

@@ -880,6 +880,16 @@ int gmm_beam_select(const void* logits, int32_t dtype, int64_t seq_stride, int64
     return GMM_ERR_INVALID_ARG;
   const int rc = check_kv_ws(ws, ws_bytes, need(batch, beams, vocab));
   if (rc != GMM_OK) return rc;
+  // nor that of anything else that is read or written
+  const struct { const void* at; int64_t bytes; } all[] = {
+      {out_score, places * 4}, {out_done, places}, {out_parent, places * 4}, {out_token, places * 4},
+      {score, rows * 4}, {weight, rows * 4}, {done, rows}};
+  for (int i = 0; i < 4; ++i)
+    for (int j = i + 1; j < 7; ++j) {
+      const bool own_place = i == 0 ? j == 4 || j == 5 : i == 1 && j == 6;      // looked at above
+      if (!own_place && all[i].at && all[j].at && overlap(all[i].at, all[i].bytes, all[j].at, all[j].bytes))
+        return GMM_ERR_INVALID_ARG;
+    }
   BeamArgs a{};
   a.x = logits;
   a.seq_stride = seq_stride;
