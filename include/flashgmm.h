@@ -595,7 +595,7 @@ int gmm_kv_copy(const gmm_kv_cache* src, const gmm_kv_cache* dst, const int32_t*
  *   total [batch], pages [batch, max_pages] rows pages_stride apart (read)
  *   parent, keep [rows]; total_out [rows], pages_out [rows, out_max_pages],
  *   rows out_stride apart, out_max_pages >= max_pages: written whole; they must
- *   not overlap the old ones, nor parent or keep (refused)
+ *   not overlap the old ones, parent, keep, ref or each other (refused)
  * batch >= 1.  Every row looks through the parents: 9 us for 512 rows of two
  * pages, 16 for 4096, 0.12 ms for 16,384, 1.4 ms for 65,536.
  */

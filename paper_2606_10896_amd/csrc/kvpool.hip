@@ -621,13 +621,14 @@ int gmm_kv_fork(const gmm_kv_cache* cache, int32_t* ref, const int32_t* total,
         out_stride < out_max_pages)
       return GMM_ERR_INVALID_ARG;
     if ((int64_t)out_max_pages * cache->page > (1 << 30)) return GMM_ERR_UNSUPPORTED;
-    // what is read while the new tables are written
+    // what is read or counted while the new tables are written
     const int64_t wide = table_bytes(rows, out_stride, out_max_pages);
     const auto hit = [&](const void* p, int64_t bytes) {
       return p && (overlap(p, bytes, total_out, 4 * (int64_t)rows) || overlap(p, bytes, pages_out, wide));
     };
     if (hit(pages, table_bytes(batch, pages_stride, max_pages)) || hit(total, 4 * (int64_t)batch) ||
-        hit(parent, 4 * (int64_t)rows) || hit(keep, 4 * (int64_t)rows))
+        hit(parent, 4 * (int64_t)rows) || hit(keep, 4 * (int64_t)rows) ||
+        hit(ref, 4 * (int64_t)cache->pages) || overlap(total_out, 4 * (int64_t)rows, pages_out, wide))
       return GMM_ERR_INVALID_ARG;
   }
   ForkArgs a{};

@@ -5,8 +5,8 @@ import itertools
 import pytest
 
 import paper_2606_10896_amd as gmm
-from test_kv_refusals_cpu import BAD, WS
-from test_kv_pool_refusals_cpu import _beam
+from test_kv_refusals_cpu import BAD, WS, _cache
+from test_kv_pool_refusals_cpu import _beam, _fork
 
 BATCH, BEAMS, M = 2, 4, 3
 AT = {"score": 0x910000, "weight": 0x920000, "done": 0x930000, "os": 0x940000, "op": 0x950000,
@@ -49,3 +49,13 @@ def test_in_place_with_as_many_results_as_beams(lib):
             assert _select(lib, m=BEAMS, ws=None, **{out: AT[read]}) == WS, (out, read)
         else:
             assert _select(lib, m=BEAMS, **{out: AT[read]}) == BAD, (out, read)
+
+
+def test_a_forks_totals_and_tables(lib):
+    """New totals [3] and new tables [3, 4], and the counts [10 pages], at addresses of their own but
+    for one."""
+    at = dict(ref=0x910000, total=0x920000, pages=0x930000, parent=0x940000, nt=0x950000, npg=0x960000)
+    size = dict(ref=40, nt=12, npg=48)
+    for a, b in itertools.permutations(size, 2):
+        for off in (1 - size[a], 0, size[b] - 1):
+            assert _fork(lib, _cache(), **{**at, a: at[b] + off}) == BAD, (a, b, off)
