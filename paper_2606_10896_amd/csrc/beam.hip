@@ -420,14 +420,17 @@ __device__ __forceinline__ uint64_t run_key(const BeamArgs& a, const Join& s, in
 }
 
 // A logit below which no word of beam j has the score `floor`: the logit of that score in fp32, less
-// what its roundings may be (each of the four terms has a few units of 2^-24, of its size).  The
-// smallest number, which -infinity does not reach, if there is none.
+// what its roundings may be (each of the four terms has a few units of 2^-24, of its size; 2^-150 of a
+// product that has too few bits in fp32 is 2^-110 of l).  The smallest number, which -infinity does not
+// reach, if there is none, and for weights whose reciprocal or product may be past the range of fp32.
 __device__ __forceinline__ float logit_of(const BeamArgs& a, const Join& s, int j, uint64_t floor) {
-  if (floor <= 1) return -FLT_MAX;
-  const float l = (float)value_of(floor) * __builtin_amdgcn_rcpf((float)s.weight[j]);
+  const float w = (float)s.weight[j];
+  if (floor <= 1 || !(w >= 0x1p-40f && w <= 0x1p64f)) return -FLT_MAX;
+  const float l = (float)value_of(floor) * __builtin_amdgcn_rcpf(w);
   const float z = (float)s.logz[j], inv = __builtin_amdgcn_rcpf((float)a.scale);
   const float x = s.top[j] + ((l - s.score[j]) + z) * inv;
-  const float less = ((fabsf(l) + fabsf(s.score[j]) + fabsf(z)) * inv + fabsf(x)) * 0x1p-20f + 1e-30f;
+  const float less = ((fabsf(l) + fabsf(s.score[j]) + fabsf(z)) * 0x1p-20f + 1e-30f) * inv +
+                     fabsf(x) * 0x1p-20f;
   return x - less > -FLT_MAX ? x - less : -FLT_MAX;      // also for what is no number
 }
 

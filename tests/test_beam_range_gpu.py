@@ -92,3 +92,33 @@ def test_differences_past_the_types_range():
         out = _check(x, s, 2, scale=scale)
         assert out[1][0].tolist() == [0, 1] and out[2][0].tolist() == [77, best]
         assert float(out[0][0, 0]) == -11.5
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("weight", [1.5e-45, 1e-40, 1.2e-38, 1e-36, 1e-30, 1e-20, 1e20, 1e30, 8e37, 9e37,
+                                    1.6e38, 1.8e38, 3.4e38])
+def test_weights_of_every_size(weight, dtype):
+    """The threshold that a run's words have to reach is found in fp32, by a division by the weight."""
+    g = torch.Generator().manual_seed(11)
+    x = (torch.randn(3, 4, 9000, generator=g) * 3).to(TYPES[dtype]).cuda()
+    s = (-10 - 2 * torch.rand(3, 4, generator=g)).cuda()
+    s[2] = 0.0
+    w = (weight * (1 - 0.01 * torch.rand(3, 4, generator=g))).clamp(min=1.5e-45).cuda()
+    w[1] = torch.tensor([1.0, weight, 1e-3, weight])
+    for m in (2, 4, 16, 40):
+        _check(x, s, m, weight=w)
+        _check(x, s, m, weight=w, scale=1e-6)
+
+
+def test_weights_with_scores_next_to_0():
+    """A beam's likeliest word has nearly all of its mass: l is 0 or a few units of 2^-149 after
+    weighting, and so small that fp32 has no bits for its product with the weight."""
+    x = torch.full((1, 4, 9000), -1e4)
+    x[0, :, ::2500] = torch.tensor([0.0, -16.0, -17.0, -18.0])
+    s = -torch.tensor([[1.0, 1.3, 1.7, 2.1]])
+    for size in (1e-7, 1e-15, 1e-25, 1e-38, 1e-43):
+        for weight in (1e-38, 1e-30, 1e-20, 1e-10, 1.0, 1e38):
+            w = torch.full((1, 4), weight).cuda()
+            for m in (1, 2, 4, 9):
+                out = _check(x.cuda(), (s * size).cuda(), m, weight=w)
+                assert out[1][0, 0] == 0 and out[2][0, 0] == 0
