@@ -5,8 +5,8 @@ import itertools
 import pytest
 
 import paper_2606_10896_amd as gmm
-from test_kv_refusals_cpu import BAD, WS, _cache
-from test_kv_pool_refusals_cpu import _beam, _fork
+from test_kv_refusals_cpu import BAD, UNSUP, WS, _cache
+from test_kv_pool_refusals_cpu import _beam, _compact, _fork
 
 BATCH, BEAMS, M = 2, 4, 3
 AT = {"score": 0x910000, "weight": 0x920000, "done": 0x930000, "os": 0x940000, "op": 0x950000,
@@ -59,3 +59,11 @@ def test_a_forks_totals_and_tables(lib):
     for a, b in itertools.permutations(size, 2):
         for off in (1 - size[a], 0, size[b] - 1):
             assert _fork(lib, _cache(), **{**at, a: at[b] + off}) == BAD, (a, b, off)
+
+
+def test_compacting_refuses_tables_past_a_launch(lib):
+    rows = 65536
+    assert _compact(lib, _cache(), batch=rows, width=1 << 16, stride=1 << 16, ws=None) == WS
+    for heads in (2, 1):                               # large and small pages
+        cache = _cache(heads=heads, page=32, d=64)
+        assert _compact(lib, cache, batch=rows, width=1 << 16, stride=1 << 16) == UNSUP
