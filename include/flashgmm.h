@@ -618,7 +618,7 @@ size_t gmm_kv_pool_workspace_bytes(const gmm_kv_cache* cache, int32_t batch);
  * of the rows of this call that write into a page keeps it if no other entry
  * names it.  Free pages are given out from the lowest number on, row after
  * row, a row's copy before its further pages.  Rows with total[b] <= held[b]
- * stay as they are.
+ * stay as they are.  batch >= 1.
  * All or nothing: if the rows need more pages than are free, nothing changes,
  * and short_by (one int32, device) says how many are missing; 0 otherwise.  The
  * caller looks at it before appending, or knows from its own count of keys
@@ -636,7 +636,8 @@ int gmm_kv_grow(const gmm_kv_cache* cache, int32_t* ref, const int32_t* held,
  * [cache pages] says for every page where its contents are now (itself if it
  * did not move, -1 if it was free), for tables that are not in this call; used
  * (one int32, device) is U.  Every entry that counts must be in `pages` or be
- * rewritten by the caller.
+ * rewritten by the caller.  batch >= 1; batch times max_pages, rounded up to a
+ * multiple of 1024, below 2^32 - 2^21 (else GMM_ERR_UNSUPPORTED).
  */
 int gmm_kv_compact(const gmm_kv_cache* cache, int32_t* ref, const int32_t* total, int32_t* pages,
                    int32_t batch, int32_t max_pages, int64_t pages_stride, int32_t* where,

@@ -2,8 +2,9 @@
 // growing and compacting.
 //
 // ref[p] counts the table entries that name page p, over all tables; 0 is a free page.  Every
-// decision is taken on the GPU from the counts and tables, in an order that the sizes fix: the
-// only atomics are sums and minima of whole numbers, whose result does not depend on theirs.
+// decision is taken on the GPU from the counts and tables, in an order that the sizes fix: atomics
+// add and take minima of whole numbers, and give out slots of a hash table and of the list of copies,
+// whose order no result depends on.
 //
 // Free and used pages are ranked by words: 64 pages make one by one ballot, a lane keeps a word, and a
 // page's rank is a sum over words plus a bit count.
